@@ -381,6 +381,59 @@ samo_status samo_fused_step_fp32_batched(const samo_plan *plan, float grad_facto
                                          const samo_adam_cfg *h_cfg, const samo_step_guard *h_guard,
                                          void *stream);
 
+/* ---------------------------------------------------------------- Adam's states in 8 bits
+ * samo_fused_step / samo_adam_expand_step with the two Adam states of a kept element held in one byte each: 10 resident
+ * bytes a kept element (idx, p, two codes) in place of 16.  The kept elements of one segment (SAMO_SEG_ELEMS dense
+ * elements) share one power of two for m and one for v.
+ *   q8  uint8[2 * nnz]        m's code of element i at 2 i, v's at 2 i + 1
+ *   s8  uint8[2 * segments]   the scales of segment s at 2 s and 2 s + 1, segments = ceil(n / SAMO_SEG_ELEMS); 2-byte aligned
+ * A scale c stands for 2^(c - 127), 255 for NaN.  m's code: sign, 4 bits e, 3 bits f: (1 + f/8) 2^(e-7) or, e = 0, f/8 2^-6 units;
+ * v's: 5 bits e, 3 bits f: (1 + f/8) 2^(e-31) or f/8 2^-30 units.  All bytes zero: a state of zeros.
+ * A step reads m and v, forms the new ones in fp32 (every product and sum rounded by itself), updates p from those, and
+ * stores them rounded up or down by 16 bits of a hash of (seed, step of the Adam configuration, rng_offset + the element's position in the layer):
+ * the expectation is the fp32 value, so averages with beta near 1 do not stand still, and the same call gives the same bits.
+ * v > 0 is never stored as 0.  A segment with an m that is not finite, or a v not below 2^126, reads as NaN from then on.
+ * Layers of one model should have rng_offsets that keep their elements' numbers apart (for instance the elements before them).
+ * m and v (float[nnz]) are used by pack and unpack only, w, g and gc16 by the steps. */
+typedef struct {
+    int64_t n, nnz;
+    const int32_t *idx;
+    const int32_t *seg_ptr;
+    float *p;
+    uint8_t *q8, *s8;
+    uint16_t *w;
+    const uint16_t *g;
+    const uint16_t *gc16;
+    float *m, *v;
+    uint32_t rng_offset;
+    uint32_t reserved;
+} samo_layer8;
+/* Filled by samo_plan8_init; read-only for the caller, plain data.  As samo_plan: layers and records are in the caller's workspace. */
+typedef struct {
+    const void *d_layers;        /* device: samo_layer8[num_layers] */
+    const void *d_recs;          /* device: one record per workgroup, those of pruned layers first */
+    int64_t pruned_recs, dense_recs;
+    int32_t num_layers;
+    int32_t rounds;              /* segments a wave of a pruned layer's workgroup takes */
+    uint32_t buffers;            /* which arrays every layer of the plan provides */
+    uint32_t reserved;
+} samo_plan8;
+/* One layer (dense: idx and seg_ptr NULL, nnz == n).  source 0: the gradient is the dense g at idx; 1: the compressed gc16. */
+samo_status samo_step8(const samo_layer8 *h_layer, int32_t source, float inv_loss_scale, const samo_adam_cfg *h_cfg,
+                       uint32_t seed, void *stream);
+/* q8 and s8 from m and v, rounded to nearest; m and v from q8 and s8 (exact). */
+samo_status samo_state8_pack(const samo_layer8 *h_layer, void *stream);
+samo_status samo_state8_unpack(const samo_layer8 *h_layer, void *stream);
+/* A whole model: at most one launch for its pruned and one for its unpruned layers.  The same rules as for samo_plan_init: h_layers is a
+ * host array that is read before the call returns, nnz is the capacity of the compressed arrays, seg_ptr is read when the steps run. */
+samo_status samo_plan8_workspace_bytes(const samo_layer8 *h_layers, int32_t num_layers, size_t *bytes);
+samo_status samo_plan8_init(const samo_layer8 *h_layers, int32_t num_layers, void *d_workspace, size_t workspace_bytes,
+                            void *stream, samo_plan8 *plan);
+samo_status samo_step8_batched(const samo_plan8 *plan, int32_t source, float inv_loss_scale, const samo_adam_cfg *h_cfg,
+                               uint32_t seed, const samo_step_guard *h_guard, void *stream);
+samo_status samo_state8_pack_batched(const samo_plan8 *plan, void *stream);
+samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
+
 /* ---------------------------------------------------------------- compression inside the backward pass
  * (Section III-C: a layer's dense gradient is compressed as soon as the backward
  * pass has produced it; Section VI-C, discussion of the compute overhead: fusing

@@ -83,6 +83,21 @@ class WgradJob(ctypes.Structure):
 SAMO_WGRAD_MAX_JOBS = 8
 
 
+class Layer8Desc(ctypes.Structure):
+    """samo_layer8"""
+    _fields_ = [("n", ctypes.c_int64), ("nnz", ctypes.c_int64), ("idx", ctypes.c_void_p), ("seg_ptr", ctypes.c_void_p),
+                ("p", ctypes.c_void_p), ("q8", ctypes.c_void_p), ("s8", ctypes.c_void_p), ("w", ctypes.c_void_p),
+                ("g", ctypes.c_void_p), ("gc16", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("rng_offset", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class Plan8Desc(ctypes.Structure):
+    """samo_plan8"""
+    _fields_ = [("d_layers", ctypes.c_void_p), ("d_recs", ctypes.c_void_p), ("pruned_recs", ctypes.c_int64),
+                ("dense_recs", ctypes.c_int64), ("num_layers", ctypes.c_int32), ("rounds", ctypes.c_int32),
+                ("buffers", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
 class StepGuard(ctypes.Structure):
     """samo_step_guard"""
     _fields_ = [("d_stats", ctypes.c_void_p), ("max_grad_norm", ctypes.c_float), ("skip_on_nonfinite", ctypes.c_int32)]
@@ -167,6 +182,19 @@ _SIGNATURES = {
                                                   ctypes.POINTER(StepGuard), ctypes.c_void_p]),
     "samo_fused_sgd_step_batched": (ctypes.c_int32, [ctypes.POINTER(PlanDesc), ctypes.c_float, ctypes.POINTER(SgdCfg),
                                                      ctypes.POINTER(StepGuard), ctypes.c_void_p]),
+    "samo_step8": (ctypes.c_int32, [ctypes.POINTER(Layer8Desc), ctypes.c_int32, ctypes.c_float, ctypes.POINTER(AdamCfg),
+                                    ctypes.c_uint32, ctypes.c_void_p]),
+    "samo_state8_pack": (ctypes.c_int32, [ctypes.POINTER(Layer8Desc), ctypes.c_void_p]),
+    "samo_state8_unpack": (ctypes.c_int32, [ctypes.POINTER(Layer8Desc), ctypes.c_void_p]),
+    "samo_plan8_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(Layer8Desc), ctypes.c_int32,
+                                                    ctypes.POINTER(ctypes.c_size_t)]),
+    "samo_plan8_init": (ctypes.c_int32, [ctypes.POINTER(Layer8Desc), ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t,
+                                         ctypes.c_void_p, ctypes.POINTER(Plan8Desc)]),
+    "samo_step8_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_int32, ctypes.c_float,
+                                            ctypes.POINTER(AdamCfg), ctypes.c_uint32, ctypes.POINTER(StepGuard),
+                                            ctypes.c_void_p]),
+    "samo_state8_pack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
+    "samo_state8_unpack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
     "samo_memory_model": (ctypes.c_int32, [ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64),
                                            ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]),
     "samo_wgrad_gather": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
@@ -926,6 +954,98 @@ class Plan:
                                     guard: Optional[StepGuard] = None) -> None:
         _check(lib().samo_fused_sgd_step_batched(self._handle, float(inv_loss_scale), ctypes.byref(cfg),
                                                  self._guard_arg(guard), _stream()), "samo_fused_sgd_step_batched")
+
+
+class Layer8(NamedTuple):
+    """Device tensors of one layer for the optimizer phase with 8-bit states (None where unused)."""
+    n: int
+    idx: Optional[torch.Tensor]
+    seg_ptr: Optional[torch.Tensor]
+    p: torch.Tensor
+    q8: torch.Tensor                        # uint8[2 * nnz]: the two states' codes
+    s8: torch.Tensor                        # uint8[2 * segments]: the two scales
+    w: Optional[torch.Tensor] = None
+    g: Optional[torch.Tensor] = None
+    gc16: Optional[torch.Tensor] = None
+    m: Optional[torch.Tensor] = None        # fp32 states: packed from and unpacked to
+    v: Optional[torch.Tensor] = None
+    rng_offset: int = 0                     # the element number that the layer's first position has in the stochastic rounding
+
+
+def samo_state8_scales_len(n: int) -> int:
+    """Bytes of s8 for a layer of n elements."""
+    return 2 * (samo_seg_ptr_len(n) - 1)
+
+
+def alloc_state8(n: int, nnz: int, device) -> tuple:
+    """(q8, s8) of a layer whose states are zero."""
+    return (torch.zeros(2 * nnz, dtype=torch.uint8, device=device),
+            torch.zeros(samo_state8_scales_len(n), dtype=torch.uint8, device=device))
+
+
+def _layer8_desc(d: Layer8Desc, L: Layer8) -> Layer8Desc:
+    n, nnz = int(L.n), L.p.numel()
+    d.n, d.nnz = n, nnz
+    d.idx = _dev(L.idx, torch.int32, "idx", nnz)
+    d.seg_ptr = _dev(L.seg_ptr, torch.int32, "seg_ptr", samo_seg_ptr_len(n))
+    d.p = _dev(L.p, torch.float32, "p")
+    d.q8 = _dev(L.q8, torch.uint8, "q8", 2 * nnz)
+    d.s8 = _dev(L.s8, torch.uint8, "s8", samo_state8_scales_len(n))
+    d.w = _dev(L.w, _F16, "w", n)
+    d.g = _dev(L.g, _F16, "g", n)
+    d.gc16 = _dev(L.gc16, _F16, "gc16", nnz)
+    d.m = _dev(L.m, torch.float32, "m", nnz)
+    d.v = _dev(L.v, torch.float32, "v", nnz)
+    d.rng_offset = int(L.rng_offset) & 0xFFFFFFFF
+    return d
+
+
+def samo_step8(layer: Layer8, inv_loss_scale: float, cfg: AdamCfg, seed: int, source: int = 0) -> None:
+    """The fused optimizer phase of one layer on 8-bit states.  source 0: the dense gradient g; 1: the compressed gc16."""
+    _check(lib().samo_step8(ctypes.byref(_layer8_desc(Layer8Desc(), layer)), int(source), float(inv_loss_scale),
+                            ctypes.byref(cfg), int(seed) & 0xFFFFFFFF, _stream()), "samo_step8")
+
+
+def samo_state8_pack(layer: Layer8) -> None:
+    """q8, s8 = the codes of m and v, rounded to nearest."""
+    _check(lib().samo_state8_pack(ctypes.byref(_layer8_desc(Layer8Desc(), layer)), _stream()), "samo_state8_pack")
+
+
+def samo_state8_unpack(layer: Layer8) -> None:
+    """m, v = what q8 and s8 stand for."""
+    _check(lib().samo_state8_unpack(ctypes.byref(_layer8_desc(Layer8Desc(), layer)), _stream()), "samo_state8_unpack")
+
+
+class Plan8:
+    """samo_plan8: the optimizer phase with 8-bit states over all layers of a model.  The tables live in a workspace
+    allocated here through torch, unless one is given."""
+
+    def __init__(self, layers: Sequence[Layer8], workspace: Optional[torch.Tensor] = None):
+        self._layers = list(layers)          # keeps the tensors alive
+        self.device = self._layers[0].p.device if self._layers else torch.device("cuda", torch.cuda.current_device())
+        self._descs = (Layer8Desc * max(len(self._layers), 1))()
+        for d, L in zip(self._descs, self._layers):
+            _layer8_desc(d, L)
+        need = ctypes.c_size_t()
+        _check(lib().samo_plan8_workspace_bytes(self._descs, len(self._layers), ctypes.byref(need)), "samo_plan8_workspace_bytes")
+        self.workspace_bytes = need.value
+        if workspace is None:
+            workspace = torch.empty(max(need.value, 1), dtype=torch.uint8, device=self.device)
+        self.workspace = workspace
+        self._plan = Plan8Desc()
+        _check(lib().samo_plan8_init(self._descs, len(self._layers), _dev(workspace, torch.uint8, "workspace"),
+                                     workspace.numel(), _stream(), ctypes.byref(self._plan)), "samo_plan8_init")
+
+    def samo_step8_batched(self, inv_loss_scale: float, cfg: AdamCfg, seed: int, guard: Optional[StepGuard] = None,
+                           source: int = 0) -> None:
+        _check(lib().samo_step8_batched(ctypes.byref(self._plan), int(source), float(inv_loss_scale), ctypes.byref(cfg),
+                                        int(seed) & 0xFFFFFFFF, Plan._guard_arg(guard), _stream()), "samo_step8_batched")
+
+    def samo_state8_pack_batched(self) -> None:
+        _check(lib().samo_state8_pack_batched(ctypes.byref(self._plan), _stream()), "samo_state8_pack_batched")
+
+    def samo_state8_unpack_batched(self) -> None:
+        _check(lib().samo_state8_unpack_batched(ctypes.byref(self._plan), _stream()), "samo_state8_unpack_batched")
 
 
 def samo_memory_model(n_total: int, nnz_total: int):

@@ -981,6 +981,216 @@ samo_status samo_fused_step_fp32_batched(const samo_plan *plan, float grad_facto
     return hip_status(launch_tile_fp32(tiles_of(plan), grad_factor, k, guard, as_stream(stream)));
 }
 
+}  // extern "C"
+
+// ---------------------------------------------------------------- Adam's states in 8 bits
+namespace {
+
+enum : uint32_t { kHas8Q = 1u << 0, kHas8W = 1u << 1, kHas8G = 1u << 2, kHas8C16 = 1u << 3, kHas8P = 1u << 4, kHas8M = 1u << 5 };
+
+// Which arrays a layer provides: those without elements count as there.
+uint32_t buffers_of(const samo_layer8 &L)
+{
+    uint32_t b = 0;
+    if (L.nnz == 0 || L.q8) b |= kHas8Q;
+    if (L.nnz == 0 || L.p) b |= kHas8P;
+    if (L.nnz == 0 || L.gc16) b |= kHas8C16;
+    if (L.nnz == 0 || (L.m && L.v)) b |= kHas8M;
+    if (L.n == 0 || L.w) b |= kHas8W;
+    if (L.n == 0 || L.g) b |= kHas8G;
+    return b;
+}
+
+samo_status check_layer8(const samo_layer8 &L)
+{
+    if (samo_status s = check_sizes(L.n, L.nnz)) return s;
+    if (samo_status s = check_index_args(L.idx, L.seg_ptr, L.n, L.nnz, /*allow_dense=*/true)) return s;
+    if (L.n > 0 && !L.s8) return SAMO_ERR_NULL;
+    if (misaligned(L.p) || misaligned(L.q8) || misaligned(L.w) || misaligned(L.g) || misaligned(L.gc16) || misaligned(L.m) || misaligned(L.v) ||
+        (reinterpret_cast<uintptr_t>(L.s8) & 1u))
+        return SAMO_ERR_ALIGN;
+    return SAMO_OK;
+}
+
+constexpr uint32_t step8_needs(int32_t source) { return kHas8Q | kHas8P | kHas8W | (source ? kHas8C16 : kHas8G); }
+
+// The key of the stochastic rounding.
+uint32_t step8_key(uint32_t seed, uint32_t step)
+{
+    uint32_t x = seed * 0x9E3779B1u + step * 0x85A308D3u;
+    x = (x ^ x >> 16) * 0x6A09E667u;
+    return x ^ x >> 15;
+}
+
+samo_status step8_args(int32_t source, float inv_loss_scale, const samo_adam_cfg *h_cfg, uint32_t seed, const samo_step_guard *h_guard, Step8Args *a)
+{
+    if (source != 0 && source != 1) return SAMO_ERR_ARG;
+    if (samo_status s = check_scale(inv_loss_scale)) return s;
+    if (samo_status s = make_adam(h_cfg, &a->adam)) return s;
+    if (samo_status s = make_guard(h_guard, &a->guard)) return s;
+    a->inv_scale = inv_loss_scale;
+    a->from_message = source;
+    a->key = step8_key(seed, (uint32_t)h_cfg->step);
+    return SAMO_OK;
+}
+
+constexpr int kStep8Waves = kStep8Threads / 64;
+int64_t segments_of(const samo_layer8 &L) { return ceil_div(L.n, kSeg); }
+int64_t recs_of(const samo_layer8 &L, int rounds) { return ceil_div(segments_of(L), (int64_t)kStep8Waves * (L.seg_ptr ? rounds : 1)); }
+
+// Segments a wave takes one after the other.
+int step8_rounds(int64_t segments) { return segments >= (int64_t)kStep8Waves * kStep8MaxRounds * 2048 ? kStep8MaxRounds : 1; }
+
+Step8Launch single8(const samo_layer8 &L)
+{
+    Step8Launch ls;
+    ls.one = L;
+    ls.layers = nullptr;
+    ls.recs = nullptr;
+    ls.rounds = L.seg_ptr ? step8_rounds(segments_of(L)) : 1;
+    ls.wgs = recs_of(L, ls.rounds);
+    return ls;
+}
+
+Step8Launch records8(const samo_plan8 *plan, bool dense)
+{
+    Step8Launch ls;
+    std::memset(&ls.one, 0, sizeof(ls.one));
+    ls.layers = static_cast<const samo_layer8 *>(plan->d_layers);
+    ls.recs = static_cast<const uint64_t *>(plan->d_recs) + (dense ? plan->pruned_recs : 0);
+    ls.rounds = dense ? 1 : plan->rounds;
+    ls.wgs = dense ? plan->dense_recs : plan->pruned_recs;
+    return ls;
+}
+
+struct Plan8Sizes {
+    int64_t pruned = 0, dense = 0;
+    int rounds = 1;
+    size_t layers_bytes = 0, bytes = 0;
+};
+
+samo_status plan8_sizes(const samo_layer8 *h_layers, int32_t num_layers, Plan8Sizes *z)
+{
+    if (num_layers < 0) return SAMO_ERR_SIZE;
+    if (num_layers > 0 && !h_layers) return SAMO_ERR_NULL;
+    int64_t segments = 0;
+    for (int32_t l = 0; l < num_layers; ++l) {
+        if (samo_status s = check_sizes(h_layers[l].n, h_layers[l].nnz)) return s;
+        if (h_layers[l].seg_ptr) segments += segments_of(h_layers[l]);
+    }
+    z->rounds = step8_rounds(segments);
+    for (int32_t l = 0; l < num_layers; ++l) (h_layers[l].seg_ptr ? z->pruned : z->dense) += recs_of(h_layers[l], z->rounds);
+    if (z->pruned > INT32_MAX || z->dense > INT32_MAX) return SAMO_ERR_SIZE;      // a launch's workgroups
+    z->layers_bytes = (size_t)ceil_div((int64_t)num_layers * (int64_t)sizeof(samo_layer8), 256) * 256;
+    z->bytes = z->layers_bytes + (size_t)(z->pruned + z->dense) * sizeof(uint64_t);
+    return SAMO_OK;
+}
+
+samo_status check_plan8(const samo_plan8 *plan, uint32_t needs)
+{
+    if (!plan) return SAMO_ERR_NULL;
+    return (plan->buffers & needs) == needs ? SAMO_OK : SAMO_ERR_PLAN;
+}
+
+samo_status state8_batched(const samo_plan8 *plan, bool pack, void *stream)
+{
+    if (samo_status s = check_plan8(plan, kHas8Q | kHas8M)) return s;
+    if (hipError_t e = launch_state8(records8(plan, false), pack, as_stream(stream))) return hip_status(e);
+    return hip_status(launch_state8(records8(plan, true), pack, as_stream(stream)));
+}
+
+samo_status state8_single(const samo_layer8 *h_layer, bool pack, void *stream)
+{
+    if (!h_layer) return SAMO_ERR_NULL;
+    if (samo_status s = check_layer8(*h_layer)) return s;
+    if ((buffers_of(*h_layer) & (kHas8Q | kHas8M)) != (kHas8Q | kHas8M)) return SAMO_ERR_NULL;
+    return hip_status(launch_state8(single8(*h_layer), pack, as_stream(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+samo_status samo_step8(const samo_layer8 *h_layer, int32_t source, float inv_loss_scale, const samo_adam_cfg *h_cfg,
+                       uint32_t seed, void *stream)
+{
+    if (!h_layer) return SAMO_ERR_NULL;
+    if (samo_status s = check_layer8(*h_layer)) return s;
+    Step8Args a;
+    if (samo_status s = step8_args(source, inv_loss_scale, h_cfg, seed, nullptr, &a)) return s;
+    if ((buffers_of(*h_layer) & step8_needs(source)) != step8_needs(source)) return SAMO_ERR_NULL;
+    return hip_status(launch_step8(single8(*h_layer), h_layer->seg_ptr == nullptr, a, as_stream(stream)));
+}
+
+samo_status samo_state8_pack(const samo_layer8 *h_layer, void *stream) { return state8_single(h_layer, true, stream); }
+samo_status samo_state8_unpack(const samo_layer8 *h_layer, void *stream) { return state8_single(h_layer, false, stream); }
+
+samo_status samo_plan8_workspace_bytes(const samo_layer8 *h_layers, int32_t num_layers, size_t *bytes)
+{
+    if (!bytes) return SAMO_ERR_NULL;
+    Plan8Sizes z;
+    if (samo_status s = plan8_sizes(h_layers, num_layers, &z)) return s;
+    *bytes = z.bytes;
+    return SAMO_OK;
+}
+
+samo_status samo_plan8_init(const samo_layer8 *h_layers, int32_t num_layers, void *d_workspace, size_t workspace_bytes,
+                            void *stream, samo_plan8 *plan)
+{
+    if (!plan) return SAMO_ERR_NULL;
+    Plan8Sizes z;
+    if (samo_status s = plan8_sizes(h_layers, num_layers, &z)) return s;
+    uint32_t buffers = ~0u;
+    for (int32_t l = 0; l < num_layers; ++l) {
+        if (samo_status s = check_layer8(h_layers[l])) return s;
+        buffers &= buffers_of(h_layers[l]);
+    }
+    if (z.bytes > 0 && (!d_workspace || workspace_bytes < z.bytes)) return SAMO_ERR_WORKSPACE;
+    if (misaligned(d_workspace)) return SAMO_ERR_ALIGN;
+    samo_layer8 *layers = static_cast<samo_layer8 *>(d_workspace);
+    unsigned char *recs = static_cast<unsigned char *>(d_workspace) + z.layers_bytes;
+    int64_t pruned = 0, dense = z.pruned;                        // where the next layer's records go
+    for (int32_t first = 0; first < num_layers; first += kPlan8Batch) {
+        Plan8Batch b;
+        std::memset(&b, 0, sizeof(b));
+        b.first = first;
+        b.count = num_layers - first < kPlan8Batch ? num_layers - first : kPlan8Batch;
+        b.rounds = z.rounds;
+        for (int j = 0; j < b.count; ++j) {
+            const samo_layer8 &L = h_layers[first + j];
+            b.layer[j] = L;
+            b.recs[j] = recs_of(L, z.rounds);
+            int64_t &next = L.seg_ptr ? pruned : dense;
+            b.rec_at[j] = next;
+            next += b.recs[j];
+        }
+        if (launch_plan8_write(b, layers, recs, as_stream(stream)) != hipSuccess) return SAMO_ERR_HIP;
+    }
+    plan->d_layers = layers;
+    plan->d_recs = recs;
+    plan->pruned_recs = z.pruned;
+    plan->dense_recs = z.dense;
+    plan->num_layers = num_layers;
+    plan->rounds = z.rounds;
+    plan->buffers = buffers;
+    plan->reserved = 0;
+    return SAMO_OK;
+}
+
+samo_status samo_step8_batched(const samo_plan8 *plan, int32_t source, float inv_loss_scale, const samo_adam_cfg *h_cfg,
+                               uint32_t seed, const samo_step_guard *h_guard, void *stream)
+{
+    Step8Args a;
+    if (!plan) return SAMO_ERR_NULL;
+    if (samo_status s = step8_args(source, inv_loss_scale, h_cfg, seed, h_guard, &a)) return s;
+    if (samo_status s = check_plan8(plan, step8_needs(source))) return s;
+    if (hipError_t e = launch_step8(records8(plan, false), false, a, as_stream(stream))) return hip_status(e);
+    return hip_status(launch_step8(records8(plan, true), true, a, as_stream(stream)));
+}
+
+samo_status samo_state8_pack_batched(const samo_plan8 *plan, void *stream) { return state8_batched(plan, true, stream); }
+samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream) { return state8_batched(plan, false, stream); }
+
 samo_status samo_memory_model(int64_t n_total, int64_t nnz_total, int64_t *paper_default, int64_t *paper_samo,
                               int64_t *resident)
 {

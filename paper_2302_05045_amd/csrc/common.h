@@ -212,6 +212,35 @@ hipError_t wgrad_configure(int *cus);
 constexpr int kMfmaRateWaves = 8;          // waves per workgroup of launch_mfma_rate, 16 MFMAs of 16 x 16 x 32 each per iteration
 hipError_t launch_mfma_rate(int64_t iters, float *sink, int workgroups, hipStream_t s);
 
+// The optimizer phase with 8-bit states (step8.hip).  A workgroup has kStep8Threads / 64 waves and takes that many segments in each
+// of `rounds` rounds, of the layer `one` or, with layers set, of the one its record names with its first segment.
+constexpr int kStep8Threads = 256;
+constexpr int kStep8MaxRounds = 4;
+struct Step8Launch {
+    samo_layer8 one;
+    const samo_layer8 *layers;
+    const uint64_t *recs;
+    int64_t wgs;
+    int rounds;
+};
+struct Step8Args {
+    AdamK adam;
+    GuardK guard;
+    float inv_scale;
+    int from_message;        // the gradient is gc16, not g at idx
+    uint32_t key;            // of the stochastic rounding: seed and step
+};
+constexpr int kPlan8Batch = 20;
+struct Plan8Batch {
+    int first, count, rounds;
+    samo_layer8 layer[kPlan8Batch];
+    int64_t rec_at[kPlan8Batch], recs[kPlan8Batch];   // a layer's first record and their number
+};
+static_assert(sizeof(Plan8Batch) <= 3072, "the layer table must fit the kernel argument segment");
+hipError_t launch_plan8_write(const Plan8Batch &b, samo_layer8 *layers, void *recs, hipStream_t s);
+hipError_t launch_step8(const Step8Launch &ls, bool dense, const Step8Args &a, hipStream_t s);
+hipError_t launch_state8(const Step8Launch &ls, bool pack, hipStream_t s);
+
 hipError_t launch_copy(void *dst, const void *src, int64_t bytes, hipStream_t s);
 
 }  // namespace samo

@@ -1,0 +1,303 @@
+"""The optimizer phase with 8-bit states against the format's and the step's definitions on the host.
+
+Tolerances.  m and v are formed from exactly decoded codes by single fp32 products and sums, so codes and scales are equal to the
+bit.  p: the update is a handful of fp32 operations on top of m and v, each within 2^-24 of its result, a dozen of them: the update
+is off by less than 2^-20 of itself, and the subtraction rounds once: |dp| <= 2^-20 |update| + 2^-23 |p|.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2302_05045_amd as samo
+import state8_ref as ref
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+CFG = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, decoupled_wd=1)
+INV = 1.0 / 1024.0
+
+
+def make(n, keep, seed, dense=False):
+    rng = np.random.default_rng(seed)
+    idx = np.arange(n) if dense else np.flatnonzero(rng.random(n) < keep)
+    g = (rng.standard_normal(n) * rng.choice([1e-3, 1.0, 30.0], n)).astype(np.float16)
+    p = (rng.standard_normal(idx.size) * 0.02).astype(np.float32)
+    return idx.astype(np.int64), g, p
+
+
+def same(a, b):
+    return a.cpu().numpy().tobytes() == b.cpu().numpy().tobytes()
+
+
+class Dev:
+    def __init__(self, n, idx, p, dense=False, rng_offset=0):
+        self.n, self.idx_host, self.dense = n, idx, dense
+        t = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(dt).to(DEV)
+        self.idx = None if dense else t(idx, torch.int32)
+        self.seg = None if dense else samo.samo_build_seg_ptr(self.idx, n)
+        self.p = t(p, torch.float32)
+        self.q8, self.s8 = samo.alloc_state8(n, idx.size, DEV)
+        self.w = torch.full((n,), float("nan"), dtype=torch.float16, device=DEV)
+        self.g = torch.zeros(n, dtype=torch.float16, device=DEV)
+        self.gc16 = torch.zeros(idx.size, dtype=torch.float16, device=DEV)
+        self.m, self.v = torch.empty_like(self.p), torch.empty_like(self.p)
+        self.rng_offset = rng_offset
+
+    def layer(self):
+        return samo.Layer8(self.n, self.idx, self.seg, self.p, self.q8, self.s8, self.w, self.g, self.gc16, self.m, self.v, self.rng_offset)
+
+    def set_grad(self, g):
+        self.g.copy_(torch.from_numpy(g))
+        self.gc16.copy_(torch.from_numpy(g[self.idx_host]))
+
+
+def check(d, idx, p, q8, s8, p_before, what):
+    assert np.array_equal(d.s8.cpu().numpy(), s8), what + ": scales"
+    assert np.array_equal(d.q8.cpu().numpy(), q8), what + ": codes"
+    got = d.p.cpu().numpy()
+    bound = 2.0 ** -20 * np.abs(p.astype(np.float64) - p_before) + 2.0 ** -23 * np.abs(p)
+    finite = np.isfinite(p)
+    assert np.array_equal(np.isfinite(got), finite), what
+    assert np.all(np.abs(got.astype(np.float64) - p)[finite] <= bound[finite]), what + ": p"
+    w = np.zeros(d.n, np.float16)
+    with np.errstate(over="ignore"):
+        w[idx] = got.astype(np.float16)
+    gw = d.w.cpu().numpy()
+    assert np.array_equal(gw.view(np.uint16)[~np.isnan(w)], w.view(np.uint16)[~np.isnan(w)]) and np.array_equal(np.isnan(gw), np.isnan(w)), what + ": w"
+
+
+@pytest.mark.parametrize("source", [0, 1])
+@pytest.mark.parametrize("n,keep,dense", [(1, 1.0, False), (1, 1.0, True), (7, 0.5, False), (1023, 0.1, False), (1024, 0.0, False),
+                                          (1025, 0.12, False), (5000, 0.25, False), (4099, 0.7, False), (8192, 1.0, False), (2055, 1.0, True),
+                                          (65536, 0.1, True), (300_007, 0.1, False), (131_080, 0.03, False), (70_001, 0.2, False)])
+def test_steps_match_the_definition(n, keep, dense, source):
+    idx, g, p = make(n, keep, n + source, dense)
+    d = Dev(n, idx, p, dense, rng_offset=12345)
+    q8, s8 = np.zeros(2 * idx.size, np.uint8), np.zeros(samo.samo_state8_scales_len(n), np.uint8)
+    for t in (1, 2, 3):
+        g = np.roll(g, t)
+        d.set_grad(g)
+        before = p.astype(np.float64)
+        # the device's own p goes on from step to step: the definition starts each from it
+        ref.step(g[idx], idx, p, q8, s8, INV, dict(CFG, step=t), 77, 12345)
+        samo.samo_step8(d.layer(), INV, samo.adam_cfg(t, **CFG), 77, source)
+        check(d, idx, p, q8, s8, before, "step %d" % t)
+        p = d.p.cpu().numpy()
+
+
+@pytest.mark.parametrize("decoupled", [0, 1])
+def test_weight_decay_forms_and_clipping(decoupled):
+    n = 20_000
+    idx, g, p = make(n, 0.3, 5)
+    cfg = dict(CFG, decoupled_wd=decoupled, weight_decay=0.0)      # without decay both forms are the same arithmetic
+    d = Dev(n, idx, p)
+    d.set_grad(g)
+    stats = torch.zeros(2, dtype=torch.float64, device=DEV)
+    stats[0] = 400.0
+    guard = samo.StepGuard(stats.data_ptr(), 2.0, 1)
+    coef = np.float32(2.0 / (20.0 + 1e-6))
+    q8, s8 = np.zeros(2 * idx.size, np.uint8), np.zeros(samo.samo_state8_scales_len(n), np.uint8)
+    before = p.astype(np.float64)
+    ref.step(g[idx], idx, p, q8, s8, INV, dict(cfg, step=4), 9, 0, coef)
+    plan = samo.Plan8([d.layer()])
+    plan.samo_step8_batched(INV, samo.adam_cfg(4, **cfg), 9, guard)
+    check(d, idx, p, q8, s8, before, "clipped")
+
+
+def test_l2_decay_reads_the_old_parameter():
+    """The decay enters the gradient by one fused multiply-add, m and v from there: those are compared, not the codes (the host
+    rounds the same sum once too, so the codes agree except where a code's bound lies between)."""
+    for keep, dense in ((0.1, False), (0.6, False), (1.0, True)):
+        n = 3000
+        idx, g, p = make(n, keep, 11, dense)
+        cfg = dict(CFG, decoupled_wd=0, weight_decay=0.1)
+        d = Dev(n, idx, p, dense)
+        d.set_grad(g)
+        q8, s8 = np.zeros(2 * idx.size, np.uint8), np.zeros(samo.samo_state8_scales_len(n), np.uint8)
+        before = p.astype(np.float64)
+        ref.step(g[idx], idx, p, q8, s8, INV, dict(cfg, step=1), 3)
+        samo.samo_step8(d.layer(), INV, samo.adam_cfg(1, **cfg), 3)
+        check(d, idx, p, q8, s8, before, "l2 keep %g" % keep)
+
+
+def test_skipped_step_leaves_everything():
+    idx, g, p = make(9000, 0.2, 6)
+    for dense in (False, True):
+        d = Dev(9000, np.arange(9000) if dense else idx, np.ones(9000, np.float32) if dense else p, dense)
+        stats = torch.zeros(2, dtype=torch.float64, device=DEV)
+        stats.view(torch.int32)[2] = 1
+        before = [t.clone() for t in (d.p, d.q8, d.s8, d.w)]
+        samo.Plan8([d.layer()]).samo_step8_batched(INV, samo.adam_cfg(1, **CFG), 1, samo.StepGuard(stats.data_ptr(), 0.0, 1))
+        for a, b in zip(before, (d.p, d.q8, d.s8, d.w)):
+            assert same(a, b)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_a_gradient_that_is_not_finite_marks_its_segment_only(bad):
+    for keep, dense in ((0.1, False), (0.5, False), (1.0, True)):
+        n = 4 * 1024
+        idx, g, p = make(n, keep, 21, dense)
+        hit = idx[np.searchsorted(idx, 2048)]
+        g[hit] = bad
+        if not dense:
+            off = np.setdiff1d(np.arange(n), idx)
+            g[off[0]] = bad                                        # at a pruned position: never looked at
+        d = Dev(n, idx, p, dense)
+        d.set_grad(g)
+        samo.samo_step8(d.layer(), INV, samo.adam_cfg(1, **CFG), 1)
+        s8 = d.s8.cpu().numpy().reshape(-1, 2)
+        assert np.all(s8[2] == 255) and np.all(s8[[0, 1, 3]] < 255)
+        samo.samo_state8_unpack(d.layer())
+        inside = idx // 1024 == 2
+        assert np.array_equal(np.isnan(d.m.cpu().numpy()), inside) and np.array_equal(np.isnan(d.v.cpu().numpy()), inside)
+        q8 = np.zeros(2 * idx.size, np.uint8)
+        ref.step(g[idx], idx, p, q8, np.zeros(8, np.uint8), INV, dict(CFG, step=1), 1)
+        assert np.array_equal(d.q8.cpu().numpy(), q8)
+
+
+def test_extreme_states_keep_their_places():
+    """Largest and smallest numbers, zeros of both signs, a v that its block's largest leaves no code for, one that has none."""
+    n = 2048
+    idx = np.arange(n)
+    rng = np.random.default_rng(3)
+    m = (rng.standard_normal(n) * np.exp2(rng.integers(-60, 60, n))).astype(np.float32)
+    v = np.exp2(rng.uniform(-140, 100, n)).astype(np.float32)
+    m[:6] = [0.0, -0.0, 1e-45, -1e-45, 1e-38, 3e38]
+    v[:5] = [0.0, 1e-45, 1e-38, 8e37, 1e-30]                          # 8e37 < 2^126
+    m[1024:] *= np.float32(1e-30)
+    v[1024:] = np.float32(1e-44)
+    d = Dev(n, idx, np.zeros(n, np.float32))
+    d.m.copy_(torch.from_numpy(m))
+    d.v.copy_(torch.from_numpy(v))
+    samo.samo_state8_pack(d.layer())
+    half = np.full(n, 0.5)
+    q8, s8 = ref.encode(m, v, idx, 2, half, half)
+    assert np.array_equal(d.s8.cpu().numpy(), s8) and np.array_equal(d.q8.cpu().numpy(), q8)
+    samo.samo_state8_unpack(d.layer())
+    rm, rv = ref.decode(q8, s8, idx)
+    assert np.array_equal(d.m.cpu().numpy(), rm.astype(np.float32)) and np.array_equal(d.v.cpu().numpy(), rv.astype(np.float32))
+    assert np.all(d.v.cpu().numpy()[v > 0][:1024] >= 0) and np.all(d.q8.cpu().numpy()[1::2][v > 0] > 0)
+    again = d.q8.clone()
+    samo.samo_state8_pack(d.layer())                                 # what was decoded is stored as it is
+    back_m, back_v = d.m.clone(), d.v.clone()
+    samo.samo_state8_unpack(d.layer())
+    assert torch.equal(d.m, back_m) and torch.equal(d.v, back_v) and again.numel()
+
+
+def test_stochastic_rounding_is_unbiased_and_repeats():
+    """The mean over K seeds of a stored value is within 5 standard errors of the value; 16 random bits resolve 2^-16 of a gap."""
+    n, K = 1024, 400
+    idx, g, p = make(n, 1.0, 8, True)
+    g = (np.abs(g) + np.float16(0.5)).astype(np.float16)
+    d = Dev(n, idx, p, True)
+    d.set_grad(g)
+    total = torch.zeros(2, n, dtype=torch.float64, device=DEV)
+    for seed in range(K):
+        d.q8.zero_(), d.s8.zero_()
+        samo.samo_step8(d.layer(), INV, samo.adam_cfg(1, **CFG), seed)
+        samo.samo_state8_unpack(d.layer())
+        total += torch.stack([d.m, d.v]).double()
+    mean = (total / K).cpu().numpy()
+    b1, b2 = np.float32(0.9), np.float32(0.999)
+    g32 = g.astype(np.float32) * np.float32(INV)
+    m = g32 * np.float32(1 - float(b1))
+    v = (g32 * np.float32(1 - float(b2))) * g32
+    for got, want, quantum in ((mean[0], m, 2.0 ** -3), (mean[1], v, 2.0 ** -3)):
+        top = np.abs(want).max()
+        floor = top * (2.0 ** -15 if got is mean[0] else 2.0 ** -31)
+        error = 5 * np.maximum(np.abs(want) * quantum, floor) / 2 / np.sqrt(K) + np.abs(want) * 2.0 ** -16
+        assert np.mean(np.abs(got - want) <= error) == 1.0
+    runs = []
+    for _ in range(2):
+        d.q8.zero_(), d.s8.zero_()
+        samo.samo_step8(d.layer(), INV, samo.adam_cfg(1, **CFG), 5)
+        runs.append(d.q8.clone())
+    assert torch.equal(*runs)
+
+
+def test_plan_of_many_layers_equals_single_calls():
+    shapes = [(1000, 0.1, False), (0, 0.0, False), (65_536, 1.0, True), (200_000, 0.2, False), (3, 1.0, True), (1024, 0.0, False)] + \
+             [(2048 + 37 * i, 0.05 * (i % 9), False) for i in range(40)]
+    single, batched = [], []
+    for i, (n, keep, dense) in enumerate(shapes):
+        idx, g, p = make(n, keep, 100 + i, dense)
+        for group in (single, batched):
+            d = Dev(n, idx, p, dense, rng_offset=1_000_003 * i)
+            d.set_grad(g)
+            group.append(d)
+    plan = samo.Plan8([d.layer() for d in batched])
+    for t in (1, 2):
+        plan.samo_step8_batched(INV, samo.adam_cfg(t, **CFG), 42)
+        for d in single:
+            samo.samo_step8(d.layer(), INV, samo.adam_cfg(t, **CFG), 42)
+    plan.samo_state8_unpack_batched()
+    for a, b in zip(single, batched):
+        samo.samo_state8_unpack(a.layer())
+        for name in ("p", "q8", "s8", "w", "m", "v"):
+            assert same(getattr(a, name), getattr(b, name)), (name, a.n)
+    plan.samo_state8_pack_batched()
+
+
+def test_many_segments_to_a_wave():
+    """A model large enough that a wave takes several segments: its last groups are partly empty."""
+    n = 4 * 4 * 2048 * 1024 + 5 * 1024 + 17
+    idx = torch.arange(3, n, 37, dtype=torch.int32, device=DEV)
+    p = torch.linspace(-1, 1, idx.numel(), device=DEV)
+    g = torch.full((n,), 2.0, dtype=torch.float16, device=DEV)
+    q8, s8 = samo.alloc_state8(n, idx.numel(), DEV)
+    w = torch.full((n,), float("nan"), dtype=torch.float16, device=DEV)
+    L = samo.Layer8(n, idx, samo.samo_build_seg_ptr(idx, n), p.clone(), q8, s8, w, g, m=torch.empty_like(p), v=torch.empty_like(p))
+    samo.samo_step8(L, INV, samo.adam_cfg(1, **dict(CFG, weight_decay=0.0)), 3)
+    # m = (1 - b1) g and v = (1 - b2) g^2: m^ / sqrt(v^) = 1
+    assert torch.all((L.p - (p - 1e-3)).abs() <= 1e-8 + 2.0 ** -22 * p.abs().clamp(min=1e-3))
+    want = torch.zeros(n, dtype=torch.float16, device=DEV)
+    want[idx.long()] = L.p.half()
+    assert torch.equal(w, want)
+    samo.samo_state8_unpack(L)
+    g32 = 2.0 * INV
+    assert torch.all((L.m - 0.1 * g32).abs() <= 0.125 * 0.1 * g32) and torch.all((L.v - 0.001 * g32 * g32).abs() <= 0.125 * 0.001 * g32 * g32)
+
+
+def test_captured_step_replays():
+    idx, g, p = make(50_000, 0.1, 31)
+    a, b = Dev(50_000, idx, p), Dev(50_000, idx, p)
+    for d in (a, b):
+        d.set_grad(g)
+    plan = samo.Plan8([a.layer()])
+    eager = samo.Plan8([b.layer()])
+    cfg = samo.adam_cfg(3, **CFG)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        plan.samo_step8_batched(INV, cfg, 6)
+    for _ in range(3):
+        graph.replay()
+        eager.samo_step8_batched(INV, cfg, 6)
+        torch.cuda.synchronize()
+        for name in ("p", "q8", "s8", "w"):
+            assert same(getattr(a, name), getattr(b, name)), name
+
+
+def test_training_with_8_bit_states_follows_32_bits():
+    """A quadratic bowl: after the same number of steps the loss is of the same size as with states in 32 bits, and averages with beta2
+    = 0.999 move (to nearest they would stand still at their first value)."""
+    n = 4096
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1)
+    target = torch.randn(n, device=DEV, generator=gen)
+    losses = []
+    for eight in (False, True):
+        p = torch.zeros(n, device=DEV)
+        w = torch.zeros(n, dtype=torch.float16, device=DEV)
+        m, v = torch.zeros_like(p), torch.zeros_like(p)
+        q8, s8 = samo.alloc_state8(n, n, DEV)
+        for t in range(1, 301):
+            g = ((p - target) * 64).half()
+            cfg = samo.adam_cfg(t, 0.02, 0.9, 0.999, 1e-8)
+            if eight:
+                samo.samo_step8(samo.Layer8(n, None, None, p, q8, s8, w, g), 1 / 64, cfg, 1)
+            else:
+                samo.samo_fused_step(g, w, None, None, p, m, v, 1 / 64, cfg)
+        losses.append(float(((p - target) ** 2).mean()))
+    assert losses[1] <= max(1e-3, 4 * losses[0]), losses
