@@ -37,36 +37,30 @@ constexpr int kWaves = kStep8Threads / 64;
 
 __device__ __forceinline__ float as_float(uint32_t b) { return __builtin_bit_cast(float, b); }
 __device__ __forceinline__ uint32_t as_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
-// What a scale code stands for; 255: NaN.
-__device__ __forceinline__ float unit_of(uint32_t code) { return as_float(code == 255u ? 0x7FC00000u : code << 23); }
+// The bits that a block's scale adds to its elements' exponent fields: a quiet NaN's where the block is one, else none.
+__device__ __forceinline__ uint32_t nan_of(uint32_t scale) { return scale == 255u ? 0x7FC00000u : 0u; }
 
-__device__ __forceinline__ float decode_m(uint32_t code, float unit)
+// The codes are the leading bits of 32-bit numbers near the least normal one, where fp32's own subnormals are the format's: exponent and
+// three bits of mantissa begin at bit 20, and a power of two takes them to their place (m: 2^120, v: 2^96 and the scale).  One ldexp
+// does all of it, exactly in reading, with the one rounding of a value below the smallest normal number in writing.
+__device__ __forceinline__ float decode_m(uint32_t code, uint32_t scale, uint32_t nan)
 {
-    const float a = as_float((code & 127u) << 20) * 0x1p120f * unit;      // the exponent field moves into place: exact
-    return as_float(as_bits(a) ^ (code & 128u) << 24);
+    const uint32_t a = __builtin_bit_cast(uint32_t, ldexpf(as_float((code & 127u) << 20 | nan), (int)scale - 7));
+    return as_float((a & 0x7FFFFFFFu) | (code << 24 & 0x80000000u));
 }
-__device__ __forceinline__ float decode_v(uint32_t code, float unit) { return as_float(code << 20) * 0x1p96f * unit; }
-
-// a units in three bits of mantissa, up or down by 20 bits of noise; LEAST: the smallest normal number, kBase its fields.
-template <int LEAST_EXP>
-__device__ __forceinline__ uint32_t round8(float a, uint32_t noise)
-{
-    constexpr uint32_t kBase = (uint32_t)(127 + LEAST_EXP) << 3;
-    const float least = as_float((uint32_t)(127 + LEAST_EXP) << 23);
-    const bool small = a < least;
-    return ((as_bits(small ? a + least : a) + noise) >> 20) - (small ? kBase : kBase - 8u);
-}
+__device__ __forceinline__ float decode_v(uint32_t code, uint32_t scale, uint32_t nan) { return ldexpf(as_float(code << 20 | nan), (int)scale - 31); }
 
 // Scale codes from the block's largest exponent fields.
 __device__ __forceinline__ uint32_t scale_m(uint32_t top) { return top >= 255u ? 255u : top > 8u ? top - 7u : 1u; }
 __device__ __forceinline__ uint32_t scale_v(uint32_t top) { return top >= 253u ? 255u : top + 1u; }
 
-// Both codes of an element, m's in the low byte.
+// Both codes of an element, m's in the low byte: the 20 bits behind a code decide with the noise's whether it is the next one.
 __device__ __forceinline__ uint32_t encode(float m, float v, uint32_t sm, uint32_t sv, uint32_t noise_m, uint32_t noise_v)
 {
-    const uint32_t cm = round8<-6>(fabsf(m) * as_float((254u - sm) << 23), noise_m) | (as_bits(m) >> 24 & 128u);
-    uint32_t cv = round8<-30>(v * as_float((254u - sv) << 23), noise_v);
-    if (v > 0.f && cv == 0u) cv = 1u;
+    const uint32_t cm = ((as_bits(ldexpf(fabsf(m), 7 - (int)sm)) + noise_m) >> 20) | (as_bits(m) >> 24 & 128u);
+    uint32_t cv = (as_bits(ldexpf(v, 31 - (int)sv)) + noise_v) >> 20;
+    const uint32_t least = as_bits(v) < 1u ? as_bits(v) : 1u;            // v > 0 is never stored as 0
+    cv = cv > least ? cv : least;
     return (sm == 255u ? 0u : cm) | (sv == 255u ? 0u : cv << 8);
 }
 
@@ -96,12 +90,17 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t both)
     return (uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, a), 63);
 }
 
-// The exponent fields of |m| and v as the halves wave_max takes.
-__device__ __forceinline__ uint32_t exponents(float m, float v) { return (as_bits(m) >> 23 & 255u) | (as_bits(v) >> 23 & 255u) << 16; }
-__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
+// The largest |m| and v so far, as bits (those of a NaN are the largest of all), and both over the wave as exponent fields.
+struct Largest {
+    uint32_t m = 0, v = 0;
+    __device__ __forceinline__ void take(float a, float b)
+    {
+        const uint32_t am = as_bits(a) & 0x7FFFFFFFu, bv = as_bits(b) & 0x7FFFFFFFu;
+        m = m > am ? m : am;
+        v = v > bv ? v : bv;
+    }
+    __device__ __forceinline__ uint32_t fields() const { return wave_max(m >> 23 | (v >> 23) << 16); }
+};
 
 // The new states, in 32 bits: each product and sum rounded by itself, so that the codes do not hang on which of them a compiler fuses.
 __device__ __forceinline__ void new_states(float &m, float &v, float g, const AdamK &k)
@@ -115,7 +114,13 @@ __device__ __forceinline__ void new_states(float &m, float &v, float g, const Ad
 
 __device__ __forceinline__ float new_parameter(float p, float m, float v, const AdamK &k)
 {
-    float upd = m * k.rbc1 / (sqrtf(v * k.rbc2) + k.eps);
+    // the root and the quotient by the hardware's approximations (1 ulp each; the root's wants no subnormal number): the update is off by
+    // 2^-21 of itself, and the kernels, which the vector ALU bounds where little is pruned, have a fifth fewer instructions
+    const float s = v * k.rbc2;
+    const bool tiny = s < 0x1p-96f;
+    float root = __builtin_amdgcn_sqrtf(tiny ? s * 0x1p64f : s);
+    root = tiny ? root * 0x1p-32f : root;
+    float upd = m * k.rbc1 * __builtin_amdgcn_rcpf(root + k.eps);
     if (k.decoupled) upd = fmaf(k.wd, p, upd);
     return fmaf(-k.lr, upd, p);
 }
@@ -182,8 +187,8 @@ __device__ __forceinline__ void step_block(const samo_layer8 &L, int64_t seg, in
         code[e] = on ? reinterpret_cast<const uint16_t *>(L.q8)[lo + i] : 0u;
         gm[e] = on && from_message ? __builtin_bit_cast(_Float16, L.gc16[lo + i]) : (_Float16)0.f;
     }
-    const float um = unit_of(old_scale & 255u), uv = unit_of(old_scale >> 8);
-    uint32_t top = 0;
+    const uint32_t sm_old = old_scale & 255u, sv_old = old_scale >> 8, nan_m = nan_of(sm_old), nan_v = nan_of(sv_old);
+    Largest largest;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         if (!from_message) gm[e] = image[(at[e] - (int)first) & (kSeg - 1)];
@@ -191,14 +196,14 @@ __device__ __forceinline__ void step_block(const samo_layer8 &L, int64_t seg, in
         if (at[e] >= 0) {
             float g = ((float)gm[e] * inv_scale) * coef;
             if (k.l2) g = fmaf(k.wd, p[e], g);
-            m[e] = decode_m(code[e] & 255u, um);
-            v[e] = decode_v(code[e] >> 8, uv);
+            m[e] = decode_m(code[e] & 255u, sm_old, nan_m);
+            v[e] = decode_v(code[e] >> 8, sv_old, nan_v);
             new_states(m[e], v[e], g, k);
             p[e] = new_parameter(p[e], m[e], v[e], k);
         }
-        top = max_halves(top, exponents(m[e], v[e]));
+        largest.take(m[e], v[e]);
     }
-    top = wave_max(top);
+    const uint32_t top = largest.fields();
     const uint32_t sm = scale_m(top & 0xFFFFu), sv = scale_v(top >> 16);
     // the gradient has been read: the image of the new weights takes its place (a wave's LDS accesses keep their order)
     __builtin_amdgcn_wave_barrier();
@@ -227,23 +232,23 @@ __device__ __forceinline__ void step_long_block(const samo_layer8 &L, int64_t se
     const int lane = threadIdx.x & 63;
     const uint32_t old_scale = *reinterpret_cast<const uint16_t *>(L.s8 + 2 * seg);
     const int first = (int)(seg * kSeg);
-    const float um = unit_of(old_scale & 255u), uv = unit_of(old_scale >> 8);
+    const uint32_t sm_old = old_scale & 255u, sv_old = old_scale >> 8, nan_m = nan_of(sm_old), nan_v = nan_of(sv_old);
     auto states = [&](int i, int at, float p, float &m, float &v) {
         const _Float16 gm = from_message ? __builtin_bit_cast(_Float16, L.gc16[lo + i]) : image[(at - first) & (kSeg - 1)];
         const uint32_t code = reinterpret_cast<const uint16_t *>(L.q8)[lo + i];
         float g = ((float)gm * inv_scale) * coef;
         if (k.l2) g = fmaf(k.wd, p, g);
-        m = decode_m(code & 255u, um);
-        v = decode_v(code >> 8, uv);
+        m = decode_m(code & 255u, sm_old, nan_m);
+        v = decode_v(code >> 8, sv_old, nan_v);
         new_states(m, v, g, k);
     };
-    uint32_t top = 0;
+    Largest largest;
     for (int i = lane; i < count; i += 64) {
         float m, v;
         states(i, L.idx[lo + i], k.l2 ? L.p[lo + i] : 0.f, m, v);
-        top = max_halves(top, exponents(m, v));
+        largest.take(m, v);
     }
-    top = wave_max(top);
+    const uint32_t top = largest.fields();
     const uint32_t sm = scale_m(top & 0xFFFFu), sv = scale_v(top >> 16);
     for (int i = lane; i < count; i += 64) {
         const int at = L.idx[lo + i];
@@ -293,6 +298,18 @@ __device__ __forceinline__ void store_image(uint16_t *w, int64_t n, int64_t seg,
     for (int i = lane; i < (int)(n - first); i += 64) w[first + i] = __builtin_bit_cast(uint16_t, image[i]);
 }
 
+// The bounds of a group's segments in the compressed arrays, one to a lane: lane i holds the first entry of segment group + i, inside
+// the arrays whatever the table holds.
+__device__ __forceinline__ int group_bounds(const samo_layer8 &L, int64_t group, int64_t segments, int rounds)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t at = group + lane < segments ? group + lane : segments;
+    if (lane > kWaves * rounds) return 0;
+    if (!L.seg_ptr) return (int)(at * kSeg < L.n ? at * kSeg : L.n);
+    const int bound = L.seg_ptr[at];
+    return bound < 0 ? 0 : bound > (int)L.nnz ? (int)L.nnz : bound;
+}
+
 __global__ void __launch_bounds__(kStep8Threads, 6) step8_pruned_kernel(const Step8Launch ls, const Step8Args A)
 {
     __shared__ __attribute__((aligned(16))) _Float16 images[kWaves][kSeg];
@@ -301,14 +318,10 @@ __global__ void __launch_bounds__(kStep8Threads, 6) step8_pruned_kernel(const St
     if (skip) return;
     samo_layer8 L;
     const int64_t group = pick(ls, &L);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t segments = (L.n + kSeg - 1) / kSeg;
     _Float16 *image = images[wave];
-    // lane i: the first entry of segment group + i, inside the arrays whatever the table holds
-    const int64_t at = group + lane < segments ? group + lane : segments;
-    int bound = 0;
-    if (lane <= kWaves * ls.rounds && segments > 0) bound = L.seg_ptr[at];
-    bound = bound < 0 ? 0 : bound > (int)L.nnz ? (int)L.nnz : bound;
+    const int bound = group_bounds(L, group, segments, ls.rounds);
     for (int r = 0; r < ls.rounds; ++r) {
         const int mine = r * kWaves + wave;
         const int64_t seg = group + mine;
@@ -344,7 +357,7 @@ __global__ void __launch_bounds__(kStep8Threads, 4) step8_dense_kernel(const Ste
     float *params = L.p + first;
     uint16_t *codes = reinterpret_cast<uint16_t *>(L.q8) + first, *weights = L.w + first;
     const uint32_t old_scale = *reinterpret_cast<const uint16_t *>(L.s8 + 2 * seg);
-    const float um = unit_of(old_scale & 255u), uv = unit_of(old_scale >> 8);
+    const uint32_t sm_old = old_scale & 255u, sv_old = old_scale >> 8, nan_m = nan_of(sm_old), nan_v = nan_of(sv_old);
     float p[16], m[16], v[16];
     uint32_t g2[8], c2[8];                                   // two 16-bit values each
     auto place = [&](int e) { return full ? (e >> 3) * 512 + 8 * lane + (e & 7) : lane + 64 * e; };
@@ -372,20 +385,20 @@ __global__ void __launch_bounds__(kStep8Threads, 4) step8_dense_kernel(const Ste
             p[e + 1] = i2 < count ? params[i2] : 0.f;
         }
     }
-    uint32_t top = 0;
+    Largest largest;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const uint32_t code = c2[e / 2] >> (e & 1) * 16;
         float g = ((float)__builtin_bit_cast(_Float16, (uint16_t)(g2[e / 2] >> (e & 1) * 16)) * A.inv_scale) * coef;
         if (A.adam.l2) g = fmaf(A.adam.wd, p[e], g);
-        m[e] = decode_m(code & 255u, um);
-        v[e] = decode_v(code >> 8 & 255u, uv);
+        m[e] = decode_m(code & 255u, sm_old, nan_m);
+        v[e] = decode_v(code >> 8 & 255u, sv_old, nan_v);
         new_states(m[e], v[e], g, A.adam);
         if (!full && place(e) >= count) m[e] = v[e] = 0.f;
         p[e] = new_parameter(p[e], m[e], v[e], A.adam);
-        top = max_halves(top, exponents(m[e], v[e]));
+        largest.take(m[e], v[e]);
     }
-    top = wave_max(top);
+    const uint32_t top = largest.fields();
     const uint32_t sm = scale_m(top & 0xFFFFu), sv = scale_v(top >> 16);
     uint32_t w2[8];
 #pragma unroll
@@ -417,43 +430,97 @@ __global__ void __launch_bounds__(kStep8Threads, 4) step8_dense_kernel(const Ste
     if (lane == 0) *reinterpret_cast<uint16_t *>(L.s8 + 2 * seg) = (uint16_t)(sm | sv << 8);
 }
 
-// m and v in 32 bits from the codes, or the codes from m and v rounded to nearest; a wave to a segment.
-template <bool PACK>
-__global__ void __launch_bounds__(kStep8Threads) state8_kernel(const Step8Launch ls)
+// m and v in 32 bits from the codes; a wave to a segment, whose first 128 elements are asked for before the last round's are stored.
+__global__ void __launch_bounds__(kStep8Threads) unpack8_kernel(const Step8Launch ls)
 {
     samo_layer8 L;
     const int64_t group = pick(ls, &L);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t segments = (L.n + kSeg - 1) / kSeg;
-    for (int r = 0; r < ls.rounds; ++r) {
-        const int64_t seg = group + r * kWaves + wave;
-        if (seg >= segments) break;
-        int64_t lo = seg * kSeg, hi = lo + kSeg < L.n ? lo + kSeg : L.n;
-        if (L.seg_ptr) {
-            lo = L.seg_ptr[seg];
-            hi = L.seg_ptr[seg + 1];
-            lo = lo < 0 ? 0 : lo > L.nnz ? L.nnz : lo;
-            hi = hi > L.nnz ? L.nnz : hi;
-            hi = hi - lo > kSeg ? lo + kSeg : hi;
-        }
-        uint16_t *codes = reinterpret_cast<uint16_t *>(L.q8);
-        uint16_t *scales = reinterpret_cast<uint16_t *>(L.s8 + 2 * seg);
-        if (PACK) {
-            uint32_t top = 0;
-            for (int64_t i = lo + lane; i < hi; i += 64) top = max_halves(top, exponents(L.m[i], L.v[i]));
-            top = wave_max(top);
-            const uint32_t sm = scale_m(top & 0xFFFFu), sv = scale_v(top >> 16);
-            for (int64_t i = lo + lane; i < hi; i += 64) codes[i] = (uint16_t)encode(L.m[i], L.v[i], sm, sv, 1u << 19, 1u << 19);
-            if (lane == 0) *scales = (uint16_t)(sm | sv << 8);
-        } else {
-            const uint32_t scale = *scales;
-            const float um = unit_of(scale & 255u), uv = unit_of(scale >> 8);
-            for (int64_t i = lo + lane; i < hi; i += 64) {
-                const uint32_t code = codes[i];
-                L.m[i] = decode_m(code & 255u, um);
-                L.v[i] = decode_v(code >> 8, uv);
+    const uint16_t *codes = reinterpret_cast<const uint16_t *>(L.q8);
+    if (!L.seg_ptr) {                                        // a whole segment: eight elements to a lane and half
+        const int64_t seg = group + wave;
+        if (seg >= segments) return;
+        const uint32_t scale = *reinterpret_cast<const uint16_t *>(L.s8 + 2 * seg);
+        const uint32_t sm = scale & 255u, sv = scale >> 8, nan_m = nan_of(sm), nan_v = nan_of(sv);
+        const int64_t first = seg * kSeg;
+        if (first + kSeg <= L.n) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t at = first + 256 * j + 4 * lane;
+                const u32x2 two = *reinterpret_cast<const u32x2 *>(codes + at);
+                f32x4 m, v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t code = two[e / 2] >> (e & 1) * 16;
+                    m[e] = decode_m(code & 255u, sm, nan_m);
+                    v[e] = decode_v(code >> 8 & 255u, sv, nan_v);
+                }
+                __builtin_nontemporal_store(m, reinterpret_cast<f32x4 *>(L.m + at));
+                __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(L.v + at));
             }
+            return;
         }
+        for (int64_t i = first + lane; i < L.n; i += 64) {
+            const uint32_t code = codes[i];
+            L.m[i] = decode_m(code & 255u, sm, nan_m);
+            L.v[i] = decode_v(code >> 8, sv, nan_v);
+        }
+        return;
+    }
+    const int bound = group_bounds(L, group, segments, ls.rounds);
+    const uint32_t scales = lane < kWaves * ls.rounds && group + lane < segments ? *reinterpret_cast<const uint16_t *>(L.s8 + 2 * (group + lane)) : 0u;
+    constexpr int kAhead = 2;
+    uint32_t code[kStep8MaxRounds][kAhead];
+#pragma unroll
+    for (int r = 0; r < kStep8MaxRounds; ++r) {              // everything of ordinary segments is asked for at once
+        const int mine = r * kWaves + wave;
+        const int lo = __builtin_amdgcn_readlane(bound, mine), hi = __builtin_amdgcn_readlane(bound, mine + 1);
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) code[r][e] = r < ls.rounds && lo + lane + 64 * e < hi ? codes[lo + lane + 64 * e] : 0u;
+    }
+#pragma unroll
+    for (int r = 0; r < kStep8MaxRounds; ++r) {
+        if (r >= ls.rounds) break;
+        const int mine = r * kWaves + wave;
+        const int lo = __builtin_amdgcn_readlane(bound, mine), hi = __builtin_amdgcn_readlane(bound, mine + 1);
+        const uint32_t scale = (uint32_t)__builtin_amdgcn_readlane((int)scales, mine);
+        const uint32_t sm = scale & 255u, sv = scale >> 8, nan_m = nan_of(sm), nan_v = nan_of(sv);
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int i = lo + lane + 64 * e;
+            if (i >= hi) continue;
+            L.m[i] = decode_m(code[r][e] & 255u, sm, nan_m);
+            L.v[i] = decode_v(code[r][e] >> 8, sv, nan_v);
+        }
+        for (int i = lo + lane + 64 * kAhead; i < hi; i += 64) {
+            const uint32_t c = codes[i];
+            L.m[i] = decode_m(c & 255u, sm, nan_m);
+            L.v[i] = decode_v(c >> 8, sv, nan_v);
+        }
+    }
+}
+
+// The codes from m and v, rounded to nearest; a wave to a segment.
+__global__ void __launch_bounds__(kStep8Threads) pack8_kernel(const Step8Launch ls)
+{
+    samo_layer8 L;
+    const int64_t group = pick(ls, &L);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t segments = (L.n + kSeg - 1) / kSeg;
+    const int bound = group_bounds(L, group, segments, ls.rounds);
+    uint16_t *codes = reinterpret_cast<uint16_t *>(L.q8);
+    for (int r = 0; r < ls.rounds; ++r) {
+        const int mine = r * kWaves + wave;
+        const int64_t seg = group + mine;
+        if (seg >= segments) break;
+        const int lo = __builtin_amdgcn_readlane(bound, mine), hi = __builtin_amdgcn_readlane(bound, mine + 1);
+        Largest largest;
+        for (int i = lo + lane; i < hi; i += 64) largest.take(L.m[i], L.v[i]);
+        const uint32_t top = largest.fields();
+        const uint32_t sm = scale_m(top & 0xFFFFu), sv = scale_v(top >> 16);
+        for (int i = lo + lane; i < hi; i += 64) codes[i] = (uint16_t)encode(L.m[i], L.v[i], sm, sv, 1u << 19, 1u << 19);
+        if (lane == 0) *reinterpret_cast<uint16_t *>(L.s8 + 2 * seg) = (uint16_t)(sm | sv << 8);
     }
 }
 
@@ -492,8 +559,8 @@ hipError_t launch_step8(const Step8Launch &ls, bool dense, const Step8Args &a, h
 hipError_t launch_state8(const Step8Launch &ls, bool pack, hipStream_t s)
 {
     if (ls.wgs <= 0) return hipSuccess;
-    if (pack) hipLaunchKernelGGL(state8_kernel<true>, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls);
-    else hipLaunchKernelGGL(state8_kernel<false>, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls);
+    if (pack) hipLaunchKernelGGL(pack8_kernel, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls);
+    else hipLaunchKernelGGL(unpack8_kernel, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls);
     return hipGetLastError();
 }
 
