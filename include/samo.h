@@ -415,7 +415,7 @@ typedef struct {
     int64_t pruned_recs, dense_recs;
     int32_t num_layers;
     int32_t rounds;              /* segments a wave of a pruned layer's workgroup takes */
-    uint32_t buffers;            /* which arrays every layer of the plan provides */
+    uint32_t buffers;            /* which arrays every layer of the plan provides; bit 31: a pruned layer keeps a fifth and more */
     uint32_t reserved;
 } samo_plan8;
 /* One layer (dense: idx and seg_ptr NULL, nnz == n).  source 0: the gradient is the dense g at idx; 1: the compressed gc16. */

@@ -986,7 +986,8 @@ samo_status samo_fused_step_fp32_batched(const samo_plan *plan, float grad_facto
 // ---------------------------------------------------------------- Adam's states in 8 bits
 namespace {
 
-enum : uint32_t { kHas8Q = 1u << 0, kHas8W = 1u << 1, kHas8G = 1u << 2, kHas8C16 = 1u << 3, kHas8P = 1u << 4, kHas8M = 1u << 5 };
+enum : uint32_t { kHas8Q = 1u << 0, kHas8W = 1u << 1, kHas8G = 1u << 2, kHas8C16 = 1u << 3, kHas8P = 1u << 4, kHas8M = 1u << 5,
+                 kHas8All = (1u << 6) - 1u, kWide8 = 1u << 31 };
 
 // Which arrays a layer provides: those without elements count as there.
 uint32_t buffers_of(const samo_layer8 &L)
@@ -1041,6 +1042,9 @@ int64_t recs_of(const samo_layer8 &L, int rounds) { return ceil_div(segments_of(
 // Segments a wave takes one after the other.
 int step8_rounds(int64_t segments) { return segments >= (int64_t)kStep8Waves * kStep8MaxRounds * 2048 ? kStep8MaxRounds : 1; }
 
+// Whether the blocks of a pruned layer hold more than 256 elements often enough for the kernel made for those.
+bool wide_blocks(const samo_layer8 &L) { return L.seg_ptr && (double)L.nnz > 0.21 * (double)L.n; }
+
 Step8Launch single8(const samo_layer8 &L)
 {
     Step8Launch ls;
@@ -1049,6 +1053,7 @@ Step8Launch single8(const samo_layer8 &L)
     ls.recs = nullptr;
     ls.rounds = L.seg_ptr ? step8_rounds(segments_of(L)) : 1;
     ls.wgs = recs_of(L, ls.rounds);
+    ls.wide = wide_blocks(L);
     return ls;
 }
 
@@ -1060,6 +1065,7 @@ Step8Launch records8(const samo_plan8 *plan, bool dense)
     ls.recs = static_cast<const uint64_t *>(plan->d_recs) + (dense ? plan->pruned_recs : 0);
     ls.rounds = dense ? 1 : plan->rounds;
     ls.wgs = dense ? plan->dense_recs : plan->pruned_recs;
+    ls.wide = (plan->buffers & kWide8) != 0;
     return ls;
 }
 
@@ -1140,10 +1146,12 @@ samo_status samo_plan8_init(const samo_layer8 *h_layers, int32_t num_layers, voi
     if (!plan) return SAMO_ERR_NULL;
     Plan8Sizes z;
     if (samo_status s = plan8_sizes(h_layers, num_layers, &z)) return s;
-    uint32_t buffers = ~0u;
+    uint32_t buffers = kHas8All;
+    bool wide = false;
     for (int32_t l = 0; l < num_layers; ++l) {
         if (samo_status s = check_layer8(h_layers[l])) return s;
         buffers &= buffers_of(h_layers[l]);
+        wide |= wide_blocks(h_layers[l]);
     }
     if (z.bytes > 0 && (!d_workspace || workspace_bytes < z.bytes)) return SAMO_ERR_WORKSPACE;
     if (misaligned(d_workspace)) return SAMO_ERR_ALIGN;
@@ -1172,7 +1180,7 @@ samo_status samo_plan8_init(const samo_layer8 *h_layers, int32_t num_layers, voi
     plan->dense_recs = z.dense;
     plan->num_layers = num_layers;
     plan->rounds = z.rounds;
-    plan->buffers = buffers;
+    plan->buffers = buffers | (wide ? kWide8 : 0u);
     plan->reserved = 0;
     return SAMO_OK;
 }

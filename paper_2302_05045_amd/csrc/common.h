@@ -222,6 +222,7 @@ struct Step8Launch {
     const uint64_t *recs;
     int64_t wgs;
     int rounds;
+    int wide;                // a layer of the launch keeps a fifth and more
 };
 struct Step8Args {
     AdamK adam;

@@ -45,8 +45,7 @@ __device__ __forceinline__ uint32_t nan_of(uint32_t scale) { return scale == 255
 // does all of it, exactly in reading, with the one rounding of a value below the smallest normal number in writing.
 __device__ __forceinline__ float decode_m(uint32_t code, uint32_t scale, uint32_t nan)
 {
-    const uint32_t a = __builtin_bit_cast(uint32_t, ldexpf(as_float((code & 127u) << 20 | nan), (int)scale - 7));
-    return as_float((a & 0x7FFFFFFFu) | (code << 24 & 0x80000000u));
+    return as_float(as_bits(ldexpf(as_float((code & 127u) << 20 | nan), (int)scale - 7)) | (code << 24 & 0x80000000u));
 }
 __device__ __forceinline__ float decode_v(uint32_t code, uint32_t scale, uint32_t nan) { return ldexpf(as_float(code << 20 | nan), (int)scale - 31); }
 
@@ -57,11 +56,12 @@ __device__ __forceinline__ uint32_t scale_v(uint32_t top) { return top >= 253u ?
 // Both codes of an element, m's in the low byte: the 20 bits behind a code decide with the noise's whether it is the next one.
 __device__ __forceinline__ uint32_t encode(float m, float v, uint32_t sm, uint32_t sv, uint32_t noise_m, uint32_t noise_v)
 {
+    const uint32_t there = (sm == 255u ? 0u : 0xFFu) | (sv == 255u ? 0u : 0xFF00u);
     const uint32_t cm = ((as_bits(ldexpf(fabsf(m), 7 - (int)sm)) + noise_m) >> 20) | (as_bits(m) >> 24 & 128u);
     uint32_t cv = (as_bits(ldexpf(v, 31 - (int)sv)) + noise_v) >> 20;
     const uint32_t least = as_bits(v) < 1u ? as_bits(v) : 1u;            // v > 0 is never stored as 0
     cv = cv > least ? cv : least;
-    return (sm == 255u ? 0u : cm) | (sv == 255u ? 0u : cv << 8);
+    return (cv << 8 | (cm & 255u)) & there;
 }
 
 // 32 well mixed bits of the element's number and the call's key: shifts and odd multipliers in turn (the golden ratio's digits, those of
@@ -114,14 +114,11 @@ __device__ __forceinline__ void new_states(float &m, float &v, float g, const Ad
 
 __device__ __forceinline__ float new_parameter(float p, float m, float v, const AdamK &k)
 {
-    // the root and the quotient by the hardware's approximations (1 ulp each; the root's wants no subnormal number): the update is off by
-    // 2^-21 of itself, and the kernels, which the vector ALU bounds where little is pruned, have a fifth fewer instructions
-    const float s = v * k.rbc2;
-    const bool tiny = s < 0x1p-96f;
-    float root = __builtin_amdgcn_sqrtf(tiny ? s * 0x1p64f : s);
-    root = tiny ? root * 0x1p-32f : root;
-    float upd = m * k.rbc1 * __builtin_amdgcn_rcpf(root + k.eps);
-    if (k.decoupled) upd = fmaf(k.wd, p, upd);
+    // The root and the quotient by the hardware's approximations (1 ulp each): the update is off by 2^-21 of itself, and the kernels, whose
+    // vector ALU is nearly as busy as HBM where little is pruned, have a fifth fewer instructions.  2^-120 keeps the root's argument
+    // above the subnormal numbers, which it does not take; it is the root of v that is below 2^-48 without it.
+    const float root = __builtin_amdgcn_sqrtf(fmaf(v, k.rbc2, 0x1p-120f));
+    const float upd = fmaf(k.decoupled ? k.wd : 0.f, p, m * k.rbc1 * __builtin_amdgcn_rcpf(root + k.eps));
     return fmaf(-k.lr, upd, p);
 }
 
@@ -169,7 +166,7 @@ __device__ __forceinline__ int64_t pick(const Step8Launch &ls, samo_layer8 *L)
 // Kept elements [lo, lo + count) of the segment that the wave owns, E to a lane.
 template <int E>
 __device__ __forceinline__ void step_block(const samo_layer8 &L, int64_t seg, int lo, int count, _Float16 *image, bool from_message,
-                                           const AdamK &k, float inv_scale, float coef, uint32_t key)
+                                           const AdamK &k, float factor, uint32_t key)
 {
     const int lane = threadIdx.x & 63;
     const uint32_t old_scale = *reinterpret_cast<const uint16_t *>(L.s8 + 2 * seg);
@@ -194,7 +191,7 @@ __device__ __forceinline__ void step_block(const samo_layer8 &L, int64_t seg, in
         if (!from_message) gm[e] = image[(at[e] - (int)first) & (kSeg - 1)];
         m[e] = v[e] = 0.f;
         if (at[e] >= 0) {
-            float g = ((float)gm[e] * inv_scale) * coef;
+            float g = (float)gm[e] * factor;
             if (k.l2) g = fmaf(k.wd, p[e], g);
             m[e] = decode_m(code[e] & 255u, sm_old, nan_m);
             v[e] = decode_v(code[e] >> 8, sv_old, nan_v);
@@ -227,7 +224,7 @@ __device__ __forceinline__ void step_block(const samo_layer8 &L, int64_t seg, in
 // The same for any count: the largest exponents first, then the step, each pass four elements to a lane at a time.  (What the second
 // pass reads again, the first one has left in the caches.)
 __device__ __forceinline__ void step_long_block(const samo_layer8 &L, int64_t seg, int lo, int count, _Float16 *image, bool from_message,
-                                             const AdamK &k, float inv_scale, float coef, uint32_t key)
+                                             const AdamK &k, float factor, uint32_t key)
 {
     const int lane = threadIdx.x & 63;
     const uint32_t old_scale = *reinterpret_cast<const uint16_t *>(L.s8 + 2 * seg);
@@ -236,7 +233,7 @@ __device__ __forceinline__ void step_long_block(const samo_layer8 &L, int64_t se
     auto states = [&](int i, int at, float p, float &m, float &v) {
         const _Float16 gm = from_message ? __builtin_bit_cast(_Float16, L.gc16[lo + i]) : image[(at - first) & (kSeg - 1)];
         const uint32_t code = reinterpret_cast<const uint16_t *>(L.q8)[lo + i];
-        float g = ((float)gm * inv_scale) * coef;
+        float g = (float)gm * factor;
         if (k.l2) g = fmaf(k.wd, p, g);
         m = decode_m(code & 255u, sm_old, nan_m);
         v = decode_v(code >> 8, sv_old, nan_v);
@@ -310,11 +307,13 @@ __device__ __forceinline__ int group_bounds(const samo_layer8 &L, int64_t group,
     return bound < 0 ? 0 : bound > (int)L.nnz ? (int)L.nnz : bound;
 }
 
-__global__ void __launch_bounds__(kStep8Threads, 6) step8_pruned_kernel(const Step8Launch ls, const Step8Args A)
+// WIDE: for layers that keep a fifth and more, whose blocks pass 256 elements: twice the registers, four workgroups to a compute unit.
+template <bool WIDE>
+__global__ void __launch_bounds__(kStep8Threads, WIDE ? 4 : 6) step8_pruned_kernel(const Step8Launch ls, const Step8Args A)
 {
     __shared__ __attribute__((aligned(16))) _Float16 images[kWaves][kSeg];
     bool skip;
-    const float coef = guard(A.guard, &skip);
+    const float factor = A.inv_scale * guard(A.guard, &skip);
     if (skip) return;
     samo_layer8 L;
     const int64_t group = pick(ls, &L);
@@ -331,9 +330,11 @@ __global__ void __launch_bounds__(kStep8Threads, 6) step8_pruned_kernel(const St
         const int lo = __builtin_amdgcn_readlane(bound, mine);
         int count = __builtin_amdgcn_readlane(bound, mine + 1) - lo;
         count = count < 0 ? 0 : count > kSeg ? kSeg : count;
-        if (count <= 128) step_block<2>(L, seg, lo, count, image, A.from_message, A.adam, A.inv_scale, coef, A.key);
-        else if (count <= 256) step_block<4>(L, seg, lo, count, image, A.from_message, A.adam, A.inv_scale, coef, A.key);
-        else step_long_block(L, seg, lo, count, image, A.from_message, A.adam, A.inv_scale, coef, A.key);
+        if (count <= 128) step_block<2>(L, seg, lo, count, image, A.from_message, A.adam, factor, A.key);
+        else if (count <= 256) step_block<4>(L, seg, lo, count, image, A.from_message, A.adam, factor, A.key);
+        else if (WIDE && count <= 512) step_block<8>(L, seg, lo, count, image, A.from_message, A.adam, factor, A.key);
+        else if (WIDE) step_block<16>(L, seg, lo, count, image, A.from_message, A.adam, factor, A.key);
+        else step_long_block(L, seg, lo, count, image, A.from_message, A.adam, factor, A.key);
         __builtin_amdgcn_wave_barrier();
         store_image(L.w, L.n, seg, image);
         __builtin_amdgcn_wave_barrier();
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kStep8Threads, 6) step8_pruned_kernel(const St
 __global__ void __launch_bounds__(kStep8Threads, 4) step8_dense_kernel(const Step8Launch ls, const Step8Args A)
 {
     bool skip;
-    const float coef = guard(A.guard, &skip);
+    const float factor = A.inv_scale * guard(A.guard, &skip);
     if (skip) return;
     samo_layer8 L;
     const int64_t seg = pick(ls, &L) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(kStep8Threads, 4) step8_dense_kernel(const Ste
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const uint32_t code = c2[e / 2] >> (e & 1) * 16;
-        float g = ((float)__builtin_bit_cast(_Float16, (uint16_t)(g2[e / 2] >> (e & 1) * 16)) * A.inv_scale) * coef;
+        float g = (float)__builtin_bit_cast(_Float16, (uint16_t)(g2[e / 2] >> (e & 1) * 16)) * factor;
         if (A.adam.l2) g = fmaf(A.adam.wd, p[e], g);
         m[e] = decode_m(code & 255u, sm_old, nan_m);
         v[e] = decode_v(code >> 8 & 255u, sv_old, nan_v);
@@ -552,7 +553,8 @@ hipError_t launch_step8(const Step8Launch &ls, bool dense, const Step8Args &a, h
 {
     if (ls.wgs <= 0) return hipSuccess;
     if (dense) hipLaunchKernelGGL(step8_dense_kernel, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls, a);
-    else hipLaunchKernelGGL(step8_pruned_kernel, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls, a);
+    else if (ls.wide) hipLaunchKernelGGL(step8_pruned_kernel<true>, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls, a);
+    else hipLaunchKernelGGL(step8_pruned_kernel<false>, dim3((unsigned)ls.wgs), dim3(kStep8Threads), 0, s, ls, a);
     return hipGetLastError();
 }
 
