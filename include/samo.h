@@ -434,6 +434,40 @@ samo_status samo_step8_batched(const samo_plan8 *plan, int32_t source, float inv
 samo_status samo_state8_pack_batched(const samo_plan8 *plan, void *stream);
 samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
 
+/* ---------------------------------------------------------------- attention of a transformer layer
+ * What lies between the QKV projection and the output projection (Section V trains GPT models), forward and backward; the
+ * gradients it leaves in the QKV projection's output gradient are the dY of samo_wgrad_gather.
+ * A samo_heads is a tokens x heads x dim fp16 tensor: element (t, h, d) at d_data[t * row + h * head + d].  row and head are
+ * multiples of 8 and not negative, d_data is 16-byte aligned: a slice of a packed projection will do.
+ * q, out, dout and dq have `heads` heads, k, v, dk and dv kv_heads, a divisor of it: query head h reads head h / (heads / kv_heads).
+ * Sequences lie end to end: sequence s of `batch` holds the tokens start[s] .. start[s + 1] - 1 of q_start and k_start (device,
+ * int32[batch + 1], ascending from 0 up; read when the kernels run; tokens behind the last start are not touched).  Both NULL: batch is 1
+ * and the sequence is all tokens.  max_q and max_k: at least the longest sequence's tokens (rows behind them are not computed).
+ *   S = scale q k^T;  out = softmax(S) v;  lse = log sum exp S, float[heads * q_tokens], head by head (natural logarithm)
+ * causal != 0: the last query of a sequence sees all of its keys, query i key j if j <= i + k_len - q_len and, with window > 0, only
+ * the last `window` of those.  A query that sees no key has out = 0, lse = -infinity and no gradient.  scale > 0.
+ * dim is a multiple of 8 up to 128; lengths from 0.  P = exp(S - lse) and dS = P (dP - delta) are rounded to fp16 where they enter a product
+ * (as the tensors themselves are), sums and softmax are fp32; the order of the sums is fixed.  Masked scores are replaced, so a key
+ * that is not finite does not reach a query that does not see its tile of 64 keys; within a tile a value that is not finite does (0 times it).
+ * Backward: dq, dk, dv from dout and the forward pass's q, k, v, out, lse; d_workspace: samo_attention_workspace_bytes, 16-byte aligned. */
+typedef struct {
+    void *d_data;
+    int64_t row, head;
+} samo_heads;
+typedef struct {
+    samo_heads q, k, v, out;
+    float *d_lse;
+    samo_heads dout, dq, dk, dv;                     /* backward only */
+    const int32_t *d_q_start, *d_k_start;
+    int64_t q_tokens, k_tokens;
+    int32_t batch, heads, kv_heads, dim, max_q, max_k;
+    float scale;
+    int32_t causal, window;
+} samo_attention_desc;
+samo_status samo_attention(const samo_attention_desc *h_desc, void *stream);
+samo_status samo_attention_workspace_bytes(const samo_attention_desc *h_desc, size_t *bytes);
+samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- compression inside the backward pass
  * (Section III-C: a layer's dense gradient is compressed as soon as the backward
  * pass has produced it; Section VI-C, discussion of the compute overhead: fusing

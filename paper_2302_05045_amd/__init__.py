@@ -98,6 +98,21 @@ class Plan8Desc(ctypes.Structure):
                 ("buffers", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
+class Heads(ctypes.Structure):
+    """samo_heads"""
+    _fields_ = [("d_data", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class AttentionDesc(ctypes.Structure):
+    """samo_attention_desc"""
+    _fields_ = [("q", Heads), ("k", Heads), ("v", Heads), ("out", Heads), ("d_lse", ctypes.c_void_p),
+                ("dout", Heads), ("dq", Heads), ("dk", Heads), ("dv", Heads),
+                ("d_q_start", ctypes.c_void_p), ("d_k_start", ctypes.c_void_p), ("q_tokens", ctypes.c_int64),
+                ("k_tokens", ctypes.c_int64), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("causal", ctypes.c_int32), ("window", ctypes.c_int32)]
+
+
 class StepGuard(ctypes.Structure):
     """samo_step_guard"""
     _fields_ = [("d_stats", ctypes.c_void_p), ("max_grad_norm", ctypes.c_float), ("skip_on_nonfinite", ctypes.c_int32)]
@@ -195,6 +210,10 @@ _SIGNATURES = {
                                             ctypes.c_void_p]),
     "samo_state8_pack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
     "samo_state8_unpack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
+    "samo_attention": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_void_p]),
+    "samo_attention_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
+    "samo_attention_backward": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_void_p, ctypes.c_size_t,
+                                                 ctypes.c_void_p]),
     "samo_memory_model": (ctypes.c_int32, [ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64),
                                            ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]),
     "samo_wgrad_gather": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
@@ -1046,6 +1065,79 @@ class Plan8:
 
     def samo_state8_unpack_batched(self) -> None:
         _check(lib().samo_state8_unpack_batched(ctypes.byref(self._plan), _stream()), "samo_state8_unpack_batched")
+
+
+def _heads(t: torch.Tensor, name: str, shape: Optional[tuple] = None) -> Heads:
+    """samo_heads of a (tokens, heads, dim) fp16 tensor on the GPU whose last dimension is contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a tensor on the GPU" % name)
+    if t.dtype != _F16 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise TypeError("%s must be a 3-D float16 tensor (tokens, heads, dim) whose last dimension is contiguous" % name)
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError("%s has shape %s, needs %s" % (name, tuple(t.shape), shape))
+    row, head = t.stride(0), t.stride(1)                  # a dimension of one element may have any stride
+    return Heads(t.data_ptr() if t.numel() else None, row if t.shape[0] > 1 else 0, head if t.shape[1] > 1 else 0)
+
+
+def _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k) -> AttentionDesc:
+    d = AttentionDesc()
+    d.q, d.k = _heads(q, "q"), _heads(k, "k")
+    q_tokens, heads, dim = q.shape
+    k_tokens, kv_heads, k_dim = k.shape
+    if k_dim != dim:
+        raise ValueError("q has heads of %d, k of %d" % (dim, k_dim))
+    d.v, d.out = _heads(v, "v", tuple(k.shape)), _heads(out, "out", tuple(q.shape))
+    if not isinstance(lse, torch.Tensor) or not lse.is_cuda or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise TypeError("lse must be a contiguous float32 tensor on the GPU")
+    if tuple(lse.shape) != (heads, q_tokens):
+        raise ValueError("lse has shape %s, needs %s" % (tuple(lse.shape), (heads, q_tokens)))
+    d.d_lse = lse.data_ptr() if lse.numel() else None
+    if (q_start is None) != (k_start is None):
+        raise ValueError("q_start and k_start are given together or not at all")
+    d.batch = 1
+    if q_start is not None:
+        d.batch = q_start.numel() - 1
+        d.d_q_start = _dev(q_start, torch.int32, "q_start", 2)
+        d.d_k_start = _dev(k_start, torch.int32, "k_start", d.batch + 1)
+    d.q_tokens, d.k_tokens, d.heads, d.kv_heads, d.dim = q_tokens, k_tokens, heads, kv_heads, dim
+    d.max_q = q_tokens if max_q is None else int(max_q)
+    d.max_k = k_tokens if max_k is None else int(max_k)
+    d.scale = float(scale) if scale is not None else dim ** -0.5
+    d.causal, d.window = int(bool(causal)), int(window)
+    return d
+
+
+def samo_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                   causal: bool = True, window: int = 0, scale: Optional[float] = None,
+                   q_start: Optional[torch.Tensor] = None, k_start: Optional[torch.Tensor] = None,
+                   max_q: Optional[int] = None, max_k: Optional[int] = None) -> None:
+    """out = softmax(scale q k^T + mask) v and lse, its rows' log-sum-exp, over packed sequences.
+
+    q, out: (tokens, heads, dim), k, v: (tokens, kv_heads, dim) fp16, strided as slices of a packed projection are; lse: float32
+    (heads, tokens).  q_start, k_start: int32 (sequences + 1) on the GPU, the sequences' first tokens; none: one sequence.
+    max_q, max_k: the longest sequence's tokens (default: all tokens).  scale: default 1 / sqrt(dim)."""
+    d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)
+    _check(lib().samo_attention(ctypes.byref(d), _stream()), "samo_attention")
+
+
+def samo_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                            lse: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, causal: bool = True,
+                            window: int = 0, scale: Optional[float] = None, q_start: Optional[torch.Tensor] = None,
+                            k_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None,
+                            max_k: Optional[int] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """dq, dk, dv of samo_attention with the same arguments, from dout and what the forward pass left in out and lse.
+
+    workspace (uint8, 4 * heads * tokens bytes) is in use until the stream has passed the call; without one the call takes
+    it from torch's allocator."""
+    d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)
+    d.dout, d.dq = _heads(dout, "dout", tuple(q.shape)), _heads(dq, "dq", tuple(q.shape))
+    d.dk, d.dv = _heads(dk, "dk", tuple(k.shape)), _heads(dv, "dv", tuple(k.shape))
+    need = 4 * q.shape[0] * q.shape[1]
+    if workspace is None and need:
+        workspace = _capture_scratch(need)
+    _check(lib().samo_attention_backward(ctypes.byref(d), _dev(workspace, torch.uint8, "workspace"),
+                                         workspace.numel() if workspace is not None else 0, _stream()),
+           "samo_attention_backward")
 
 
 def samo_memory_model(n_total: int, nnz_total: int):

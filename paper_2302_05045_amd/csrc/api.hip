@@ -1199,6 +1199,102 @@ samo_status samo_step8_batched(const samo_plan8 *plan, int32_t source, float inv
 samo_status samo_state8_pack_batched(const samo_plan8 *plan, void *stream) { return state8_batched(plan, true, stream); }
 samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream) { return state8_batched(plan, false, stream); }
 
+}  // extern "C"
+
+// ---------------------------------------------------------------- attention
+namespace {
+
+constexpr int kMaxHeadDim = 128;
+
+samo_status check_heads(const samo_heads &t, int64_t tokens)
+{
+    if (tokens == 0) return SAMO_OK;
+    if (!t.d_data) return SAMO_ERR_NULL;
+    if (misaligned(t.d_data)) return SAMO_ERR_ALIGN;
+    if (t.row < 0 || t.head < 0 || t.row % 8 || t.head % 8) return SAMO_ERR_SIZE;
+    return SAMO_OK;
+}
+
+samo_status check_attention(const samo_attention_desc *d, bool backward, AttnArgs *a)
+{
+    if (!d) return SAMO_ERR_NULL;
+    if (d->q_tokens < 0 || d->q_tokens > INT32_MAX || d->k_tokens < 0 || d->k_tokens > INT32_MAX) return SAMO_ERR_SIZE;
+    if (d->batch < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->dim < 8 || d->dim > kMaxHeadDim || d->dim % 8)
+        return SAMO_ERR_SIZE;
+    if (d->max_q < 0 || d->max_k < 0 || d->max_q > d->q_tokens || d->max_k > d->k_tokens) return SAMO_ERR_SIZE;
+    if ((!d->d_q_start || !d->d_k_start) && (d->d_q_start || d->d_k_start || d->batch != 1)) return SAMO_ERR_ARG;
+    if ((reinterpret_cast<uintptr_t>(d->d_q_start) | reinterpret_cast<uintptr_t>(d->d_k_start) | reinterpret_cast<uintptr_t>(d->d_lse)) & 3u)
+        return SAMO_ERR_ALIGN;
+    if (!(std::isfinite(d->scale) && d->scale > 0.f) || d->window < 0 || (d->window > 0 && !d->causal)) return SAMO_ERR_ARG;
+    if (d->q_tokens > 0 && !d->d_lse) return SAMO_ERR_NULL;
+    // a launch's workgroups, 128 rows of a head each, fit 31 bits
+    if (ceil_div(d->max_q, 128) * d->batch * d->heads > INT32_MAX / 2 || ceil_div(d->max_k, 128) * d->batch * d->kv_heads > INT32_MAX / 2)
+        return SAMO_ERR_SIZE;
+    const samo_heads *of_q[] = {&d->q, &d->out, &d->dout, &d->dq}, *of_k[] = {&d->k, &d->v, &d->dk, &d->dv};
+    for (int i = 0; i < (backward ? 4 : 2); ++i) {
+        if (samo_status s = check_heads(*of_q[i], d->q_tokens)) return s;
+        if (samo_status s = check_heads(*of_k[i], d->k_tokens)) return s;
+    }
+    std::memset(a, 0, sizeof(*a));
+    a->q = static_cast<const _Float16 *>(d->q.d_data); a->q_row = d->q.row; a->q_head = d->q.head;
+    a->k = static_cast<const _Float16 *>(d->k.d_data); a->k_row = d->k.row; a->k_head = d->k.head;
+    a->v = static_cast<const _Float16 *>(d->v.d_data); a->v_row = d->v.row; a->v_head = d->v.head;
+    a->out = static_cast<_Float16 *>(d->out.d_data); a->out_row = d->out.row; a->out_head = d->out.head;
+    a->lse = d->d_lse;
+    if (backward) {
+        a->dout = static_cast<const _Float16 *>(d->dout.d_data); a->dout_row = d->dout.row; a->dout_head = d->dout.head;
+        a->dq = static_cast<_Float16 *>(d->dq.d_data); a->dq_row = d->dq.row; a->dq_head = d->dq.head;
+        a->dk = static_cast<_Float16 *>(d->dk.d_data); a->dk_row = d->dk.row; a->dk_head = d->dk.head;
+        a->dv = static_cast<_Float16 *>(d->dv.d_data); a->dv_row = d->dv.row; a->dv_head = d->dv.head;
+    }
+    a->q_start = d->d_q_start;
+    a->k_start = d->d_k_start;
+    a->q_tokens = d->q_tokens;
+    a->k_tokens = d->k_tokens;
+    a->batch = d->batch;
+    a->heads = d->heads;
+    a->kv_heads = d->kv_heads;
+    a->group = d->heads / d->kv_heads;
+    a->dim = d->dim;
+    a->max_q = d->max_q;
+    a->max_k = d->max_k;
+    a->causal = d->causal != 0;
+    a->window = d->window;
+    a->scale = d->scale;
+    return SAMO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+samo_status samo_attention(const samo_attention_desc *h_desc, void *stream)
+{
+    AttnArgs a;
+    if (samo_status s = check_attention(h_desc, false, &a)) return s;
+    return hip_status(launch_attention(a, as_stream(stream)));
+}
+
+samo_status samo_attention_workspace_bytes(const samo_attention_desc *h_desc, size_t *bytes)
+{
+    if (!h_desc || !bytes) return SAMO_ERR_NULL;
+    if (h_desc->heads < 1 || h_desc->q_tokens < 0 || h_desc->q_tokens > INT32_MAX) return SAMO_ERR_SIZE;
+    *bytes = (size_t)h_desc->heads * (size_t)h_desc->q_tokens * sizeof(float);
+    return SAMO_OK;
+}
+
+samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    AttnArgs a;
+    size_t need = 0;
+    if (samo_status s = check_attention(h_desc, true, &a)) return s;
+    if (samo_status s = samo_attention_workspace_bytes(h_desc, &need)) return s;
+    if (need > 0 && (!d_workspace || workspace_bytes < need)) return SAMO_ERR_WORKSPACE;
+    if (misaligned(d_workspace)) return SAMO_ERR_ALIGN;
+    a.delta = static_cast<float *>(d_workspace);
+    return hip_status(launch_attention_backward(a, as_stream(stream)));
+}
+
 samo_status samo_memory_model(int64_t n_total, int64_t nnz_total, int64_t *paper_default, int64_t *paper_samo,
                               int64_t *resident)
 {

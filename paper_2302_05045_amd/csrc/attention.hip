@@ -1,0 +1,566 @@
+// Softmax attention over packed sequences and its backward pass, which recomputes the probabilities: what lies between the QKV
+// projection and the output projection of a transformer layer.  Per sequence and head
+//   S = scale Q K^T with the masked places at -inf,  lse = log sum exp S,  P = exp(S - lse),  O = P V
+//   delta = rowsum(dO O),  dV = P^T dO,  dP = dO V^T,  dS = P (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q
+// No matrix of scores exists in memory: the forward pass keeps lse, one number a row, and the backward pass forms S again.
+//
+// Bound by the matrix units (fp16 products, fp32 sums), with the LDS reads of their operands and, in the softmax, the vector ALU close
+// behind.  What the kernels share:
+//  - A wave owns 32 rows of one side (queries; keys for dK, dV) whose operands stay in its registers; the other side comes
+//    in tiles of 64 rows through LDS, two tiles in turn, copied past the registers while the other is multiplied.
+//  - Scores are formed transposed where the wave owns queries: S^T = K Q^T puts a query into a lane's column, so the softmax is a
+//    maximum and a sum over a lane's own registers and one exchange between the wave's halves.  An accumulator register holds rows
+//    8 (i / 4) + 4 half + i % 4 of the block: eight of them in a row are, as they are, the operand of the next product over 16 of
+//    those rows, as long as the other operand is read in the same order -- and the transposing LDS read takes any four rows.
+//    So P and dS go from one product to the next without leaving the registers.
+//  - A tile's LDS rows are 128 or 256 bytes; 16-byte piece c of row r lies at c ^ swizzle(r), which spreads both kinds of read, 16
+//    rows by one piece and 4 rows by 64 bytes, over all banks.
+//  - Workgroups are dealt to the 8 XCDs in contiguous runs, a head's workgroups together: they share its other side in one L2.
+// P and dS are rounded to fp16 for the products they enter, as Q, K, V and dO are: 2^-11 of themselves; statistics and all sums are fp32.
+// dQ and dK, dV are formed by two kernels, each of which forms S and dP: 7 products for the 5 that one kernel would need, but every
+// sum has one owner and one order, so the same call gives the same bits (with additions to dQ in memory it would not).
+#include "common.h"
+#include "lds_copy.h"
+
+namespace samo {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kAttnThreads = 256, kWaveRows = 32, kTileRows = 64;
+constexpr int kOwnRows = kAttnThreads / 64 * kWaveRows;           // 128
+constexpr float kLog2e = 1.4426950408889634f;
+
+// KS: steps of 16 that a head's dim takes; 32 x 32 blocks, bytes of an LDS row, 16-byte pieces of one, bytes of a tile.
+constexpr int blocks_of(int ks) { return (ks + 1) / 2; }
+constexpr int pitch_of(int ks) { return ks <= 4 ? 128 : 256; }
+constexpr int tile_bytes(int ks) { return kTileRows * pitch_of(ks); }
+
+template <int PITCH>
+__device__ __forceinline__ int swizzle(int row)
+{
+    return PITCH == 256 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+}
+
+// A sequence's rows of one operand, at one head.
+struct Rows {
+    const _Float16 *base;
+    int64_t stride;          // elements from row to row
+    int count, dim;
+};
+
+// The wave's share of a tile: rows first .. first + 63 to LDS; what is behind the rows or the dim is zero.
+template <int PITCH>
+__device__ __forceinline__ void copy_tile(const Rows &R, int first, unsigned lds_at)
+{
+    constexpr int kPieces = PITCH / 16, kRowsPer = 64 / kPieces, kCopies = kTileRows / kRowsPer / 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+        const int copy = wave * kCopies + i, row = copy * kRowsPer + lane / kPieces;
+        const int piece = (lane % kPieces) ^ swizzle<PITCH>(row);
+        const bool there = first + row < R.count && piece * 8 < R.dim;
+        const void *from = there ? static_cast<const void *>(R.base + (int64_t)(first + row) * R.stride + piece * 8) : zero_row;
+        dma16(from, lds_at + copy * 1024);
+    }
+}
+
+// Operand with the tile's rows as its rows (32 of them from row 32 block) and 16 columns from 16 ks.
+template <int PITCH>
+__device__ __forceinline__ half8 read_rows(const unsigned char *tile, int block, int ks)
+{
+    const int lane = threadIdx.x & 63, row = lane & 31;
+    return *reinterpret_cast<const half8 *>(tile + (block * 32 + row) * PITCH + (((2 * ks + (lane >> 5)) ^ swizzle<PITCH>(row)) << 4));
+}
+
+// Operand with the tile's columns 32 db .. as its rows, over the tile's rows 16 step .. in the order an accumulator holds them.
+template <int PITCH>
+__device__ __forceinline__ half8 read_columns(const unsigned char *tile, int step, int db)
+{
+    const int lane = threadIdx.x & 63, i = lane & 15, half = lane >> 5;
+    const int piece = 4 * db + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+    const int row = 4 * half + (i >> 2);                       // and row + 8
+    const unsigned char *at = tile + step * 16 * PITCH + (i & 1) * 8;
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS short4v *)(LDS_AS unsigned char *)(at + row * PITCH + ((piece ^ swizzle<PITCH>(row)) << 4)));
+    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (LDS_AS short4v *)(LDS_AS unsigned char *)(at + (row + 8) * PITCH + ((piece ^ swizzle<PITCH>(row + 8)) << 4)));
+    const short8v q = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return __builtin_bit_cast(half8, q);
+}
+
+// The wave's own rows as operand columns, straight from memory: row (lane & 31), 8 elements of every step's 16.
+template <int KS>
+__device__ __forceinline__ void load_own(const Rows &R, int first, half8 (&own)[KS])
+{
+    const int lane = threadIdx.x & 63, row = first + (lane & 31), half = lane >> 5;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int col = 16 * ks + 8 * half;
+        half8 x = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (row < R.count && col < R.dim) x = *reinterpret_cast<const half8 *>(R.base + (int64_t)row * R.stride + col);
+        own[ks] = x;
+    }
+}
+
+// x of the other half of the wave, lane by lane.
+__device__ __forceinline__ float other_half(float x)
+{
+    const auto two = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? two[0] : two[1]);
+}
+
+__device__ __forceinline__ half8 to_half8(const f32x16 &x, int at)
+{
+    half8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)x[at + e];
+    return h;
+}
+
+// Row of a 32 x 32 accumulator's register i.
+__device__ __forceinline__ int acc_row(int i) { return 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (i & 3); }
+
+// Column (lane & 31) of a transposed result, times factor, as row `row` of a tensor.
+template <int DB>
+__device__ __forceinline__ void store_own(_Float16 *base, int64_t stride, int row, int count, int dim, const f32x16 (&acc)[DB], float factor)
+{
+    if (row >= count) return;
+    _Float16 *to = base + (int64_t)row * stride;
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * db + 8 * g + 4 * half;
+            if (d >= dim) continue;
+            half4 h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = (_Float16)(acc[db][4 * g + e] * factor);
+            *reinterpret_cast<half4 *>(to + d) = h;
+        }
+}
+
+template <int N>
+__device__ __forceinline__ void clear(f32x16 (&acc)[N])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
+}
+
+// One sequence: where its rows begin and how many there are, inside the tensors whatever the tables hold.
+struct Sequence {
+    int64_t q0, k0;
+    int q_len, k_len;
+};
+__device__ __forceinline__ void bounds_of(const int32_t *start, int b, int64_t tokens, int64_t &first, int &len)
+{
+    int64_t lo = 0, hi = tokens;
+    if (start) {
+        lo = start[b];
+        hi = start[b + 1];
+        lo = lo < 0 ? 0 : lo > tokens ? tokens : lo;
+        hi = hi < lo ? lo : hi > tokens ? tokens : hi;
+    }
+    first = lo;
+    len = (int)(hi - lo);
+}
+__device__ __forceinline__ Sequence sequence_of(const AttnArgs &A, int b)
+{
+    Sequence s;
+    bounds_of(A.q_start, b, A.q_tokens, s.q0, s.q_len);
+    bounds_of(A.k_start, b, A.k_tokens, s.k0, s.k_len);
+    return s;
+}
+
+// The workgroup's sequence, head and tile of own rows; tiles of a head run backwards (the last queries see the most keys).
+__device__ __forceinline__ bool pick_tile(int heads, int batch, int tiles, int &b, int &head, int &tile)
+{
+    const int items = batch * heads * tiles, per_xcd = (items + 7) / 8;
+    const int item = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per_xcd || item >= items) return false;
+    const int of_head = item / tiles;
+    tile = tiles - 1 - (item - of_head * tiles);
+    b = of_head / heads;
+    head = of_head - b * heads;
+    return true;
+}
+
+// Which keys a query sees: first_key(query) .. end_key(query) - 1, all of them without `causal`; and which queries see a key.
+struct Mask {
+    bool causal;
+    int shift, window, q_len, k_len;         // window 2^30: none
+    __device__ __forceinline__ int first_key(int query) const { return causal ? query + shift - window + 1 : 0; }
+    __device__ __forceinline__ int end_key(int query) const { return causal ? min(query + shift + 1, k_len) : k_len; }
+    __device__ __forceinline__ int first_query(int key) const { return causal ? key - shift : 0; }
+    __device__ __forceinline__ int end_query(int key) const { return causal ? min(key - shift + window, q_len) : q_len; }
+    // whether all of / any of a block of queries and keys (first and last of each) are seen
+    __device__ __forceinline__ bool all(int q0, int q1, int k0, int k1) const { return k1 < k_len && (!causal || (k1 <= q0 + shift && k0 > q1 + shift - window)); }
+    __device__ __forceinline__ bool any(int q0, int q1, int k0, int k1) const { return !causal || (k0 <= q1 + shift && k1 > q0 + shift - window); }
+};
+// The numbers from .. end - 1 by one comparison.
+struct Span {
+    int from;
+    unsigned count;
+    __device__ __forceinline__ Span(int first, int end) : from(first), count(end > first ? (unsigned)(end - first) : 0u) {}
+    __device__ __forceinline__ bool holds(int x) const { return (unsigned)(x - from) < count; }
+};
+__device__ __forceinline__ Mask mask_of(const AttnArgs &A, const Sequence &s)
+{
+    Mask m;
+    m.causal = A.causal != 0;
+    m.shift = s.k_len - s.q_len;
+    m.window = A.window > 0 ? min(A.window, 1 << 30) : 1 << 30;
+    m.q_len = s.q_len;
+    m.k_len = s.k_len;
+    return m;
+}
+
+// The tiles of keys that any of the queries q0 .. q1 sees: [first, end) in rows, first a multiple of the tile.
+__device__ __forceinline__ void key_range(const Mask &M, int q0, int q1, int k_len, int &first, int &end)
+{
+    first = 0;
+    end = k_len;
+    if (M.causal) {
+        const int last = q1 + M.shift + 1, begin = q0 + M.shift - M.window + 1;
+        end = last < end ? last : end;
+        first = begin > 0 ? begin / kTileRows * kTileRows : 0;
+    }
+}
+
+// The forward pass.
+template <int KS>
+__global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnArgs A)
+{
+    constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
+    int b, head, tile;
+    if (!pick_tile(A.heads, A.batch, A.tiles, b, head, tile)) return;
+    const Sequence seq = sequence_of(A, b);
+    if (tile * kOwnRows >= seq.q_len) return;
+    const Mask M = mask_of(A, seq);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int q_first = tile * kOwnRows, q_last = min(q_first + kOwnRows, seq.q_len) - 1;
+    const int w_first = q_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.q_len) - 1;   // of the wave; none where last < first
+    const int query = w_first + (lane & 31);
+    const int kv = head / A.group;
+    const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
+    const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
+    const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
+    int k_first, k_end;
+    key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
+    const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
+
+    if (k_first < k_end) {
+        copy_tile<PITCH>(K, k_first, lds_at);
+        copy_tile<PITCH>(V, k_first, lds_at + 2 * kTile);
+    }
+    half8 own[KS];
+    load_own<KS>(Q, w_first, own);
+    const Span seen(M.first_key(query), M.end_key(query));
+    f32x16 out[DB];
+    clear(out);
+    const float c = A.scale * kLog2e;
+    float top = -INFINITY, sum = 0.f;                        // top: what the exponents are taken against, within 8 of the largest so far
+    int buffer = 0;
+    for (int k0 = k_first; k0 < k_end; k0 += kTileRows, buffer ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        meet();                                              // the tile is there, and the other one has been read by every wave
+        if (k0 + kTileRows < k_end) {
+            copy_tile<PITCH>(K, k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
+            copy_tile<PITCH>(V, k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
+        }
+        if (w_last < w_first || !M.any(w_first, w_last, k0, k0 + kTileRows - 1)) continue;
+        const unsigned char *kt = lds + buffer * kTile, *vt = lds + (2 + buffer) * kTile;
+        f32x16 s[2];
+        clear(s);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(kt, kb, ks), own[ks], s[kb], 0, 0, 0);
+        if (!M.all(w_first, w_last, k0, k0 + kTileRows - 1)) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kb][i] = seen.holds(k0 + 32 * kb + acc_row(i)) ? s[kb][i] : -INFINITY;
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) most = fmaxf(most, s[i >> 4][i & 15]);
+        most = fmaxf(most, other_half(most));
+        // Only where a row's largest score passes what its exponents are taken against by 2^8 are the sums so far brought down: P stays
+        // below 2^8 otherwise, which fp16 holds as well as numbers below 1.
+        if (__ballot(most * c > top * c + 8.f)) {
+            const float next = fmaxf(top, most);
+            const float down = next == top ? 1.f : __builtin_amdgcn_exp2f((top - next) * c);
+            top = next;
+            sum *= down;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) out[db][i] *= down;
+        }
+        const float against = top == -INFINITY ? 0.f : top * c;       // a row that has seen no key yet
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -against));
+                sum += s[kb][i];
+            }
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            const half8 p = to_half8(s[step >> 1], 8 * (step & 1));
+#pragma unroll
+            for (int db = 0; db < DB; ++db) out[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(vt, step, db), p, out[db], 0, 0, 0);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    sum += other_half(sum);
+    const float factor = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;      // a row that sees no key: zero; NaN stays
+    store_own<DB>(A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, query, seq.q_len, A.dim, out, factor);
+    if (lane < 32 && query < seq.q_len) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : top * A.scale + __logf(sum);
+}
+
+// dQ, and delta on the way.
+template <int KS>
+__global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const AttnArgs A)
+{
+    constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];
+    int b, head, tile;
+    if (!pick_tile(A.heads, A.batch, A.tiles, b, head, tile)) return;
+    const Sequence seq = sequence_of(A, b);
+    if (tile * kOwnRows >= seq.q_len) return;
+    const Mask M = mask_of(A, seq);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int q_first = tile * kOwnRows, q_last = min(q_first + kOwnRows, seq.q_len) - 1;
+    const int w_first = q_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.q_len) - 1;
+    const int query = w_first + (lane & 31);
+    const int kv = head / A.group;
+    const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
+    const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
+    const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
+    const Rows DO = {A.dout + seq.q0 * A.dout_row + head * A.dout_head, A.dout_row, seq.q_len, A.dim};
+    const Rows O = {A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, seq.q_len, A.dim};
+    int k_first, k_end;
+    key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
+    const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
+    if (k_first < k_end) {
+        copy_tile<PITCH>(K, k_first, lds_at);
+        copy_tile<PITCH>(V, k_first, lds_at + 2 * kTile);
+    }
+    half8 own[KS], down[KS];
+    load_own<KS>(Q, w_first, own);
+    load_own<KS>(DO, w_first, down);
+    float delta = 0.f;
+    {
+        half8 o[KS];
+        load_own<KS>(O, w_first, o);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)o[ks][e], (float)down[ks][e], delta);
+        delta += other_half(delta);
+    }
+    const int64_t stat = (int64_t)head * A.q_tokens + seq.q0 + query;
+    const float c = A.scale * kLog2e;
+    float lse = 0.f;
+    if (query < seq.q_len) {
+        lse = A.lse[stat] * kLog2e;
+        if (lane < 32) A.delta[stat] = delta;
+    }
+    const Span seen(M.first_key(query), M.end_key(query));
+    f32x16 acc[DB];
+    clear(acc);
+    int buffer = 0;
+    for (int k0 = k_first; k0 < k_end; k0 += kTileRows, buffer ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        meet();
+        if (k0 + kTileRows < k_end) {
+            copy_tile<PITCH>(K, k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
+            copy_tile<PITCH>(V, k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
+        }
+        const unsigned char *kt = lds + buffer * kTile, *vt = lds + (2 + buffer) * kTile;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int k1 = k0 + 32 * kb;
+            if (k1 >= seq.k_len || w_last < w_first || !M.any(w_first, w_last, k1, k1 + 31)) continue;
+            f32x16 s[1], dp[1];
+            clear(s);
+            clear(dp);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(kt, kb, ks), own[ks], s[0], 0, 0, 0);
+                dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(vt, kb, ks), down[ks], dp[0], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse)) * (dp[0][i] - delta);
+            if (!M.all(w_first, w_last, k1, k1 + 31)) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[0][i] = seen.holds(k1 + acc_row(i)) ? s[0][i] : 0.f;
+            }
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                const half8 ds = to_half8(s[0], 8 * step);
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(kt, 2 * kb + step, db), ds, acc[db], 0, 0, 0);
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    store_own<DB>(A.dq + seq.q0 * A.dq_row + head * A.dq_head, A.dq_row, query, seq.q_len, A.dim, acc, A.scale);
+}
+
+// lse, or delta, of the 64 queries of a tile to LDS, by one wave; what is behind the rows as `behind`.
+__device__ __forceinline__ void copy_stats(const float *from, int first, int count, const float *behind, unsigned lds_at)
+{
+    const int at = first + (threadIdx.x & 63);
+    const float *p = at < count ? from + at : behind;
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(p), "s"(lds_at) : "memory");
+}
+__device__ const float infinite_lse[1] = {INFINITY};         // a probability of zero
+
+// dK and dV: a wave owns 32 keys, the queries of every head that shares them come by.
+template <int KS>
+__global__ void __launch_bounds__(kAttnThreads, KS <= 6 ? 2 : 1) attention_dkv_kernel(const AttnArgs A)
+{
+    constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // Q, dO; two tiles each
+    __shared__ __attribute__((aligned(16))) float stats[2][2][kTileRows];         // lse, delta
+    int b, kv, tile;
+    if (!pick_tile(A.kv_heads, A.batch, A.tiles, b, kv, tile)) return;
+    tile = A.tiles - 1 - tile;                               // the first keys are seen by the most queries
+    const Sequence seq = sequence_of(A, b);
+    if (tile * kOwnRows >= seq.k_len) return;
+    const Mask M = mask_of(A, seq);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int k_first = tile * kOwnRows, k_last = min(k_first + kOwnRows, seq.k_len) - 1;
+    const int w_first = k_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.k_len) - 1;
+    const int key = w_first + (lane & 31);
+    const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
+    const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
+    // the queries that see any of the workgroup's keys
+    int q_first = 0, q_end = seq.q_len;
+    if (M.causal) {
+        const int begin = k_first - M.shift;
+        q_first = begin > 0 ? begin / kTileRows * kTileRows : 0;
+        const int64_t end = (int64_t)k_last - M.shift + M.window;
+        q_end = end < q_end ? (int)(end > 0 ? end : 0) : q_end;
+    }
+    const int tiles = q_end > q_first ? (q_end - q_first + kTileRows - 1) / kTileRows : 0;
+    const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds, stats_at = (unsigned)(size_t)(LDS_AS unsigned char *)stats;
+    auto bring = [&](int shared, int t, int buffer) {
+        const int head = kv * A.group + shared, first = q_first + t * kTileRows;
+        const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
+        const Rows DO = {A.dout + seq.q0 * A.dout_row + head * A.dout_head, A.dout_row, seq.q_len, A.dim};
+        copy_tile<PITCH>(Q, first, lds_at + buffer * kTile);
+        copy_tile<PITCH>(DO, first, lds_at + (2 + buffer) * kTile);
+        const int64_t stat = (int64_t)head * A.q_tokens + seq.q0;
+        if (wave == 0) copy_stats(A.lse + stat, first, seq.q_len, infinite_lse, stats_at + buffer * 2 * kTileRows * 4);
+        if (wave == 1) copy_stats(A.delta + stat, first, seq.q_len, reinterpret_cast<const float *>(zero_row), stats_at + (buffer * 2 + 1) * kTileRows * 4);
+    };
+    if (tiles > 0) bring(0, 0, 0);
+    half8 own[KS], ownv[KS];
+    load_own<KS>(K, w_first, own);
+    load_own<KS>(V, w_first, ownv);
+    const Span seen(M.first_query(key), M.end_query(key));
+    f32x16 dk[DB], dv[DB];
+    clear(dk);
+    clear(dv);
+    const float c = A.scale * kLog2e;
+    int buffer = 0;
+    for (int shared = 0; shared < A.group; ++shared)
+        for (int t = 0; t < tiles; ++t, buffer ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            meet();
+            if (t + 1 < tiles) bring(shared, t + 1, buffer ^ 1);
+            else if (shared + 1 < A.group) bring(shared + 1, 0, buffer ^ 1);
+            const unsigned char *qt = lds + buffer * kTile, *dot = lds + (2 + buffer) * kTile;
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+                const int q1 = q_first + t * kTileRows + 32 * qb;
+                if (q1 >= seq.q_len || w_last < w_first || !M.any(q1, q1 + 31, w_first, w_last)) continue;
+                f32x16 s[1], dp[1];
+                clear(s);
+                clear(dp);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
+                    dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), ownv[ks], dp[0], 0, 0, 0);
+                }
+                const int half = lane >> 5;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][32 * qb + 8 * g + 4 * half]);
+                    const f32x4 delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][32 * qb + 8 * g + 4 * half]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = 4 * g + e;
+                        s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
+                        dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
+                    }
+                }
+                if (!M.all(q1, q1 + 31, w_first, w_last)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const bool on = seen.holds(q1 + acc_row(i));
+                        s[0][i] = on ? s[0][i] : 0.f;
+                        dp[0][i] = on ? dp[0][i] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int step = 0; step < 2; ++step) {
+                    const half8 p = to_half8(s[0], 8 * step), ds = to_half8(dp[0], 8 * step);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(dot, 2 * qb + step, db), p, dv[db], 0, 0, 0);
+                        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(qt, 2 * qb + step, db), ds, dk[db], 0, 0, 0);
+                    }
+                }
+            }
+        }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    store_own<DB>(A.dk + seq.k0 * A.dk_row + kv * A.dk_head, A.dk_row, key, seq.k_len, A.dim, dk, A.scale);
+    store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
+}
+
+enum { kForward, kDq, kDkv };
+
+template <int KS>
+hipError_t launch_dim(int which, const AttnArgs &a, dim3 grid, hipStream_t s)
+{
+    if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
+    else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
+    else hipLaunchKernelGGL((attention_dkv_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch(int which, AttnArgs a, int64_t rows, int heads, hipStream_t s)
+{
+    a.tiles = (int)ceil_div(rows, kOwnRows);
+    const int64_t items = (int64_t)a.batch * heads * a.tiles;
+    if (items == 0) return hipSuccess;
+    const dim3 grid((unsigned)(ceil_div(items, 8) * 8));
+    switch ((a.dim + 15) / 16) {                             // padded: a kernel for each of the sizes in use, and the next one up for the others
+    case 1: case 2: return launch_dim<2>(which, a, grid, s);
+    case 3: case 4: return launch_dim<4>(which, a, grid, s);
+    case 5: return launch_dim<5>(which, a, grid, s);
+    case 6: return launch_dim<6>(which, a, grid, s);
+    default: return launch_dim<8>(which, a, grid, s);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_attention(const AttnArgs &a, hipStream_t s) { return launch(kForward, a, a.max_q, a.heads, s); }
+
+hipError_t launch_attention_backward(const AttnArgs &a, hipStream_t s)
+{
+    if (hipError_t e = launch(kDq, a, a.max_q, a.heads, s)) return e;       // delta first: the other kernel reads it
+    return launch(kDkv, a, a.max_k, a.kv_heads, s);
+}
+
+}  // namespace samo

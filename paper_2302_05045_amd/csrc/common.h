@@ -242,6 +242,21 @@ hipError_t launch_plan8_write(const Plan8Batch &b, samo_layer8 *layers, void *re
 hipError_t launch_step8(const Step8Launch &ls, bool dense, const Step8Args &a, hipStream_t s);
 hipError_t launch_state8(const Step8Launch &ls, bool pack, hipStream_t s);
 
+// Attention (attention.hip): tensors of tokens x heads x dim, a row's elements adjacent, strides in elements.
+struct AttnArgs {
+    const _Float16 *q, *k, *v, *dout;
+    _Float16 *out, *dq, *dk, *dv;
+    float *lse, *delta;                     // heads x q_tokens
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head, dout_row, dout_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
+    const int32_t *q_start, *k_start;       // batch + 1 each, NULL: one sequence of all tokens
+    int64_t q_tokens, k_tokens;
+    int batch, heads, kv_heads, group, dim, max_q, max_k, causal, window;
+    int tiles;                              // of own rows a head, set by the launch
+    float scale;
+};
+hipError_t launch_attention(const AttnArgs &a, hipStream_t s);
+hipError_t launch_attention_backward(const AttnArgs &a, hipStream_t s);
+
 hipError_t launch_copy(void *dst, const void *src, int64_t bytes, hipStream_t s);
 
 }  // namespace samo

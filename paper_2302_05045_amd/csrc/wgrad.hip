@@ -51,17 +51,11 @@
 #include <type_traits>
 
 #include "common.h"
+#include "lds_copy.h"
 #include "runs.h"
 
 namespace samo {
 namespace {
-
-#define LDS_AS __attribute__((address_space(3)))
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef short short4v __attribute__((ext_vector_type(4)));
-typedef short short8v __attribute__((ext_vector_type(8)));
 
 constexpr int kWgThreads = 512;
 constexpr int kRowPitch = 1024 + 32;                 // an LDS row is one copy instruction's 1 KiB; with the pad eight consecutive
@@ -116,36 +110,6 @@ struct WgradBatch {
 constexpr int kOutPartial = 3;
 constexpr int kResidentShape = 512;         // SAMO_KNOB_WGRAD_TILE: 128 x 128 tiles, four workgroups to a compute unit
 constexpr int kMaxSplits = 64;              // what SAMO_KNOB_WGRAD_SPLIT may ask for; the rule takes up to 16
-
-__device__ __attribute__((aligned(16))) const unsigned char wgrad_zero_row[16] = {0};
-
-// One copy instruction: the wave's 64 x 16 bytes from the lanes' global addresses to LDS at
-// lds_byte_addr + 16 * lane.  It writes M0, a register the compiler reserves and does not let an
-// asm statement declare as clobbered; nothing else in these kernels makes the compiler use M0 (no
-// register arrays indexed at run time, no other LDS-direct or GWS operation).
-__device__ __forceinline__ void dma16(const void *g, unsigned lds_byte_addr)
-{
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(lds_byte_addr) : "memory");
-}
-
-// The same with the global addresses as a scalar base plus a 32-bit offset per lane.  A scalar
-// register that a vector instruction has written (the compiler may have parked the base in one) must
-// not be read by a memory instruction for five cycles: the wait states in front cover that.
-__device__ __forceinline__ void dma16_from(const void *base, unsigned lane_offset, unsigned lds_byte_addr)
-{
-    asm volatile("s_nop 3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_offset), "s"(base), "s"(lds_byte_addr)
-                 : "memory");
-}
-
-// 8 tokens of one feature for an MFMA lane: two transposing reads of one token of four LDS rows each,
-// the rows' tokens `step` bytes apart.
-__device__ __forceinline__ half8 read_fragment(const unsigned char *p, int step)
-{
-    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS short4v *)(LDS_AS unsigned char *)p);
-    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS short4v *)(LDS_AS unsigned char *)(p + step));
-    const short8v q = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    return __builtin_bit_cast(half8, q);
-}
 
 // Workgroups are dealt round-robin to the 8 XCDs: each XCD gets a contiguous run of tiles so
 // that the tiles sharing operand panels, and neighbouring runs of idx, meet in one L2.  Within
@@ -275,7 +239,7 @@ struct RunPass {
         cols = A.in - col0 < tile_cols ? A.in - col0 : tile_cols;
         // by a scalar load without a branch, which travels with the first copies (await): a vector load of a uniform value, and a load behind a
         // branch, are waited for at once (7856 x 4632, 106 tokens, 20 % kept 28.9 -> 29.7 us)
-        const int32_t *last = A.idx ? A.seg_ptr + ((unsigned)A.out * (unsigned)A.in + (kSeg - 1)) / kSeg : reinterpret_cast<const int32_t *>(wgrad_zero_row);
+        const int32_t *last = A.idx ? A.seg_ptr + ((unsigned)A.out * (unsigned)A.in + (kSeg - 1)) / kSeg : reinterpret_cast<const int32_t *>(zero_row);
         counted = *(const __attribute__((address_space(4))) int32_t *)last;
 #pragma unroll
         for (int i = 0; i < kLooks; ++i) {
@@ -461,13 +425,6 @@ __device__ __forceinline__ void wait_copies(int64_t younger)
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 }
 
-// A bare workgroup barrier: what has to be complete before it is waited for explicitly.
-__device__ __forceinline__ void meet()
-{
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // The main loop: acc += the wave's OB x IB blocks of 16 x 16 of a tile of COLS <= TILE columns.  A stage is 32
 // LDS rows, row j < 16 row_tokens(TILE) consecutive tokens of X (room for TILE features each), row 16 + j
 // the same tokens of dY.
@@ -519,7 +476,7 @@ __device__ __forceinline__ void multiply_tile(const WgradArgs &A, int row0, int 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t token = s * kTokens + first_token + kRowTokens * i + sub;
-            dma16(token < A.tokens ? gbase + token * row_bytes + f_bytes : wgrad_zero_row, dst + i * kRowPitch);
+            dma16(token < A.tokens ? gbase + token * row_bytes + f_bytes : zero_row, dst + i * kRowPitch);
         }
     };
 #pragma unroll
@@ -817,8 +774,8 @@ __global__ void __launch_bounds__(kResidentThreads, 4) wgrad_resident_kernel(con
         for (int i = 0; i < 2; ++i) {
             const int64_t token = (int64_t)s * kTokens + first_token + kRowTokens * i + sub;
             const bool there = token < A.tokens;
-            dma16(there ? xbase + token * x_bytes + xf : wgrad_zero_row, x_rows + slot + i * kRowPitch);
-            dma16(there ? ybase + token * y_bytes + yf : wgrad_zero_row, y_rows + slot + i * kRowPitch);
+            dma16(there ? xbase + token * x_bytes + xf : zero_row, x_rows + slot + i * kRowPitch);
+            dma16(there ? ybase + token * y_bytes + yf : zero_row, y_rows + slot + i * kRowPitch);
         }
     };
     // Wave w gathers rows 32 w .. 32 w + 31; in two parts where old values take registers too.

@@ -1,0 +1,249 @@
+"""Attention, forward and backward, against the definition in 64 bits.
+
+Tolerances.  The tensors are fp16 (u = 2^-11 relative, rounding to nearest), the sums fp32 in some order.  P enters the second product
+rounded to fp16, so a row of out is off by at most u sum_j P_j |v_j| + u |out| and the fp32 sums' share, for which a quarter of u is
+granted: |d out| <= 1.25 u A + u |out| with A = sum_j P_j |v_j|.  lse: the scores are exact products summed in fp32: 2^-23 (dim + 8) S with
+S the largest sum of magnitudes of a score, and a few operations at the end, 2^-20.  Gradients: P and dS are rounded to fp16, dP - delta is off by what
+out's rounding to fp16 makes of delta (u sum_d |dO out|) and the fp32 sums; each bound is that of the products' terms taken as magnitudes, with
+P (|dP| + |delta| + u-terms) in the place of |dS|: |d| <= 3 u B + u |result| + 2^-24 (the smallest fp16 step, for each of dS's roundings among
+the subnormal numbers: times the sum of the other factor's magnitudes).  Every bound is element by element.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2302_05045_amd as samo
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -11
+
+
+def seen_of(n, m, causal, window):
+    i = torch.arange(n, device=DEV)[:, None] + (m - n)
+    j = torch.arange(m, device=DEV)[None, :]
+    seen = torch.ones((n, m), dtype=torch.bool, device=DEV)
+    if causal:
+        seen = j <= i
+        if window:
+            seen &= j > i - window
+    return seen
+
+
+def reference(q, k, v, do, scale, seen):
+    """One head of one sequence in 64 bits: results and the magnitudes of their bounds."""
+    q, k, v, do = (t.double() for t in (q, k, v, do))
+    s = torch.where(seen, q @ k.T * scale, -math.inf)
+    lse = torch.logsumexp(s, 1)
+    p = torch.where(seen, torch.exp(s - torch.where(torch.isinf(lse), 0.0, lse)[:, None]), 0.0)
+    out = p @ v
+    dp = do @ v.T
+    delta = (do * out).sum(1, keepdim=True)
+    ds = p * (dp - delta)
+    size = p * (do.abs() @ v.abs().T + (do * out).abs().sum(1, keepdim=True)) + 2.0 ** -25 / U * seen
+    r = dict(out=out, lse=lse, dq=ds @ k * scale, dk=ds.T @ q * scale, dv=p.T @ do)
+    b = dict(out=p @ v.abs() + 2.0 ** -25 / U * (seen.double() @ v.abs()), dq=size @ k.abs() * scale, dk=size.T @ q.abs() * scale,
+             dv=(p + 2.0 ** -25 / U * seen).T @ do.abs(), s=(q.abs() @ k.abs().T * scale).amax(1) if k.shape[0] else torch.zeros(q.shape[0], device=DEV))
+    return r, b
+
+
+def check(lens_q, lens_k, heads, kv_heads, dim, causal, window, seed=0, layout="packed", std=1.0, dstd=1.0, slack=0, fix=None, scale=None):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    tq, tk = sum(lens_q), sum(lens_k)
+    rnd = lambda *s, a=std: (torch.randn(s, generator=gen, device=DEV) * a).half()
+    if layout == "packed" and lens_q == lens_k:
+        qkv, dqkv = rnd(tq, (heads + 2 * kv_heads) * dim), torch.full((tq, (heads + 2 * kv_heads) * dim), float("nan"), device=DEV).half()
+        cut = lambda t: (t[:, :heads * dim].view(tq, heads, dim), t[:, heads * dim:(heads + kv_heads) * dim].view(tq, kv_heads, dim),
+                         t[:, (heads + kv_heads) * dim:].view(tq, kv_heads, dim))
+        (q, k, v), (dq, dk, dv) = cut(qkv), cut(dqkv)
+    elif layout == "heads first":
+        q, k, v = rnd(heads, tq, dim).transpose(0, 1), rnd(kv_heads, tk, dim).transpose(0, 1), rnd(kv_heads, tk, dim).transpose(0, 1)
+        dq, dk, dv = (torch.full((t.shape[1], t.shape[0], dim), float("nan"), device=DEV).half().transpose(0, 1) for t in (q, k, v))
+    else:                                                    # rows further apart than they need to be
+        wide = lambda t, h: rnd(t, h, dim + 24)[:, :, 8:8 + dim]
+        q, k, v = wide(tq, heads), wide(tk, kv_heads), wide(tk, kv_heads)
+        dq, dk, dv = (torch.full((t.shape[0], t.shape[1], dim + 8), float("nan"), device=DEV).half()[:, :, :dim] for t in (q, k, v))
+    out, lse = torch.full((tq, heads, dim), float("nan"), device=DEV).half(), torch.full((heads, tq), float("nan"), device=DEV)
+    do = rnd(tq, heads, dim, a=dstd)
+    if fix:
+        fix(q, k, v, do)
+    scale = dim ** -0.5 if scale is None else scale
+    starts = lambda ns: torch.tensor(np.concatenate([[0], np.cumsum(ns)]), dtype=torch.int32, device=DEV)
+    args = dict(causal=causal, window=window, scale=scale)
+    if len(lens_q) > 1 or layout == "starts":
+        args.update(q_start=starts(lens_q), k_start=starts(lens_k), max_q=min(tq, max(lens_q) + slack))
+    samo.samo_attention(q, k, v, out, lse, **args)
+    if len(lens_q) > 1 or layout == "starts":
+        args.update(max_k=min(tk, max(lens_k) + slack))
+    samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv, **args)
+    q0 = k0 = 0
+    for n, m in zip(lens_q, lens_k):
+        seen = seen_of(n, m, causal, window)
+        grads = {}
+        for h in range(heads):
+            g = h * kv_heads // heads
+            r, b = reference(q[q0:q0 + n, h], k[k0:k0 + m, g], v[k0:k0 + m, g], do[q0:q0 + n, h], scale, seen)
+            got = dict(out=out[q0:q0 + n, h], dq=dq[q0:q0 + n, h])
+            for name, most in (("out", 1.25), ("dq", 3.0)):
+                d = (got[name].double() - r[name]).abs()
+                bound = most * U * b[name] + U * r[name].abs() + 2.0 ** -25
+                assert torch.all(d <= bound), (name, n, m, h, float((d - bound).max()))
+            z, want = lse[h, q0:q0 + n].double(), r["lse"]
+            empty = torch.isinf(want)
+            assert torch.equal(torch.isneginf(z), empty)
+            assert torch.all((z - want).abs()[~empty] <= (2.0 ** -23 * (dim + 8) * b["s"] + 2.0 ** -20 * (1 + want.abs()))[~empty])
+            assert torch.all(out[q0:q0 + n, h][empty] == 0) and torch.all(dq[q0:q0 + n, h][empty] == 0)
+            for name in ("dk", "dv"):
+                a, c = grads.get((name, g), (0, 0))
+                grads[name, g] = (a + r[name], c + b[name])
+        for (name, g), (want, size) in grads.items():
+            d = ((dk if name == "dk" else dv)[k0:k0 + m, g].double() - want).abs()
+            bound = 3.0 * U * size + U * want.abs() + 2.0 ** -25
+            assert torch.all(d <= bound), (name, n, m, g, float((d - bound).max()))
+        q0, k0 = q0 + n, k0 + m
+
+
+@pytest.mark.parametrize("dim", [8, 16, 24, 32, 40, 48, 56, 64, 72, 80, 88, 96, 104, 112, 120, 128])
+def test_every_head_dim(dim):
+    check([130, 67], [130, 67], 4, 2, dim, True, 0, seed=dim)
+    check([97], [97], 2, 2, dim, False, 0, seed=dim + 1, layout="wide")
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 640])
+def test_lengths_around_the_tiles(n):
+    check([n], [n], 2, 1, 64, True, 0, seed=n)
+    check([n], [n], 1, 1, 128, False, 0, seed=n)
+
+
+@pytest.mark.parametrize("layout", ["packed", "heads first", "wide", "starts"])
+def test_layouts(layout):
+    check([200], [200], 6, 2, 80, True, 0, layout=layout)
+
+
+def test_sequences_of_no_and_one_token_among_others():
+    check([0, 1, 200, 0, 3, 64, 1, 0], [0, 1, 200, 0, 3, 64, 1, 0], 4, 4, 64, True, 0, slack=77)
+    check([0, 5, 0], [7, 0, 0], 2, 1, 64, False, 0)          # queries without keys, keys without queries
+
+
+@pytest.mark.parametrize("window", [1, 2, 33, 64, 100, 5000])
+def test_windows(window):
+    check([300, 20], [300, 20], 2, 1, 96, True, window, seed=window)
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 50), (False, 0)])
+def test_fewer_and_more_queries_than_keys(causal, window):
+    check([70, 200], [333, 201], 4, 2, 128, causal, window)  # the last queries of longer contexts
+    check([333, 130], [70, 1], 4, 2, 64, causal, window)     # the first queries see nothing
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (8, 1), (6, 3), (16, 16)])
+def test_shared_heads(heads, kv):
+    check([150], [150], heads, kv, 64, True, 0)
+
+
+def test_large_scores_and_small_gradients():
+    """Scores of hundreds (one key takes all of a row), rows whose largest score comes last, gradients among fp16's small numbers."""
+    check([300], [300], 2, 2, 64, True, 0, std=6.0)
+    check([200], [200], 2, 2, 128, False, 0, dstd=2.0 ** -9)
+    check([150], [150], 1, 1, 64, False, 0, std=1.0, scale=3.0)
+
+    def rising(q, k, v, do):
+        k.mul_(torch.linspace(0, 4, k.shape[0], device=DEV)[:, None, None].half())
+        q.abs_()
+        k.abs_()
+    check([400], [400], 1, 1, 64, False, 0, fix=rising)
+
+
+def test_far_keys_that_are_not_finite_do_not_reach_a_query():
+    n, dim = 256, 64
+    q, k, v = (torch.randn(n, 1, dim, device=DEV).half() for _ in range(3))
+    out, lse, again, lse2 = torch.zeros_like(q), torch.zeros(1, n, device=DEV), torch.zeros_like(q), torch.zeros(1, n, device=DEV)
+    samo.samo_attention(q, k, v, out, lse)
+    k[192:] = float("nan")
+    v[192:] = float("inf")
+    samo.samo_attention(q, k, v, again, lse2)
+    assert torch.equal(out[:192], again[:192]) and torch.equal(lse[:, :192], lse2[:, :192])
+    assert torch.all(torch.isnan(again[192:]))
+    # another sequence's, in the same tile
+    k[:] = torch.randn(n, 1, dim, device=DEV).half()
+    v[:] = torch.randn(n, 1, dim, device=DEV).half()
+    starts = torch.tensor([0, 100, 256], dtype=torch.int32, device=DEV)
+    samo.samo_attention(q, k, v, out, lse, causal=False, q_start=starts, k_start=starts)
+    k[100:] = float("nan")
+    v[100:] = float("nan")
+    samo.samo_attention(q, k, v, again, lse2, causal=False, q_start=starts, k_start=starts)
+    assert torch.equal(out[:100], again[:100])
+
+
+def test_gradients_against_differences():
+    """The loss sum(out * do): its change along a random direction of q, k and v against the gradients, in steps that fp16 holds exactly.
+    The forward pass rounds to fp16 at 2^-11; over n * dim outputs those roundings add up as a random sum, 6 of whose deviations are granted."""
+    n, dim, eps = 96, 64, 2.0 ** -4
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(4)
+    grid = lambda: (torch.randn((n, 2, dim), generator=gen, device=DEV) * 16).round().div(16).half()
+    q, k, v, do = grid(), grid(), grid(), grid()
+    out, lse = torch.zeros_like(q), torch.zeros(2, n, device=DEV)
+    samo.samo_attention(q, k, v, out, lse)
+    grads = [torch.zeros_like(q) for _ in range(3)]
+    samo.samo_attention_backward(do, q, k, v, out, lse, *grads)
+    for which in range(3):
+        way = torch.randint(0, 2, q.shape, generator=gen, device=DEV).half() * 2 - 1
+        loss = []
+        for sign in (1, -1):
+            args = [q, k, v]
+            args[which] = args[which] + sign * eps * way
+            o = torch.zeros_like(q)
+            samo.samo_attention(*args, o, lse)
+            loss.append(float((o.double() * do.double()).sum()))
+        slope = (loss[0] - loss[1]) / (2 * eps)
+        want = float((grads[which].double() * way.double()).sum())
+        noise = 6 * U * math.sqrt(float((out.double() * do.double()).square().sum()) * 2) / (2 * eps)
+        third = 0.05 * float(grads[which].double().norm())           # the differences' own error, third order in eps
+        assert abs(slope - want) <= noise + third, (which, slope, want)
+
+
+def test_same_bits_again_other_stream_and_graph():
+    n, dim = 500, 80
+    q, k, v, do = (torch.randn(n, 4, dim, device=DEV).half() for _ in range(4))
+    bufs = lambda: [torch.zeros(n, 4, dim, device=DEV).half() for _ in range(4)] + [torch.zeros(4, n, device=DEV)]
+
+    def call(o, dq, dk, dv, lse, ws=None):
+        samo.samo_attention(q, k, v, o, lse)
+        samo.samo_attention_backward(do, q, k, v, o, lse, dq, dk, dv, workspace=ws)
+
+    first, second, third = bufs(), bufs(), bufs()
+    call(*first)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call(*second)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(*third)
+    for _ in range(3):
+        for t in third:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b, c in zip(first, second, third):
+            assert torch.equal(a, b) and torch.equal(a, c)
+        call(*bufs())
+
+
+def test_rows_past_two_gibibytes():
+    """A key/value slice whose rows are so far apart that the last ones begin past 2^31 bytes."""
+    n, dim, apart = 700, 64, 1 << 21
+    room = torch.zeros((n, apart), dtype=torch.float16, device=DEV)
+    k, v = room[:, :dim].unsqueeze(1), room[:, 64:64 + dim].unsqueeze(1)
+    kk, vv, q = (torch.randn(n, 1, dim, device=DEV).half() for _ in range(3))
+    k.copy_(kk)
+    v.copy_(vv)
+    a, b, lse = torch.zeros_like(q), torch.zeros_like(q), torch.zeros(1, n, device=DEV)
+    samo.samo_attention(q, k, v, a, lse)
+    samo.samo_attention(q, kk, vv, b, lse)
+    assert torch.equal(a, b)
