@@ -468,6 +468,24 @@ samo_status samo_attention(const samo_attention_desc *h_desc, void *stream);
 samo_status samo_attention_workspace_bytes(const samo_attention_desc *h_desc, size_t *bytes);
 samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------- gated feed-forward block
+ * The two up-projections of a gated block, its activation and the product in one kernel, and its backward pass:
+ *   G = X Wg^T,  U = X Wu^T,  h = act(G) U;      dG = dh U act'(G),  dU = dh act(G),  dX = dG Wg + dU Wu
+ * The weights' gradients are samo_wgrad_gather's with dY = dG or dU (one call for both: samo_wgrad_gather_batched).
+ * d_x: tokens x in, d_w_gate and d_w_up: ffn x in (the dense w of a layer, with explicit zeros), everything else tokens x ffn, dX tokens x in;
+ * row-major fp16, 16-byte aligned.  in and ffn are multiples of 8 below 2^20, tokens below 2^31; tokens 0 does nothing.
+ * Sums are fp32 in a fixed order.  samo_glu forms h from the sums, rounded once; d_gate and d_up, both or neither, receive G and U
+ * rounded once, for samo_glu_backward, which reads them.  d_dx may be NULL (no dX wanted).
+ * samo_glu_workspace_bytes: what samo_glu_backward can use on the current device for layers with few tiles of dX (fp32 sums of parts
+ * of the summation); with less, or NULL, it does without.  In use until the stream has passed the call. */
+enum { SAMO_ACT_SILU = 0, SAMO_ACT_GELU = 1, SAMO_ACT_GELU_TANH = 2, SAMO_ACT_RELU = 3 };
+samo_status samo_glu(const uint16_t *d_x, const uint16_t *d_w_gate, const uint16_t *d_w_up, int64_t tokens, int64_t in,
+                     int64_t ffn, int32_t act, uint16_t *d_h, uint16_t *d_gate, uint16_t *d_up, void *stream);
+samo_status samo_glu_workspace_bytes(int64_t tokens, int64_t in, int64_t ffn, size_t *bytes);
+samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, const uint16_t *d_up, const uint16_t *d_w_gate,
+                              const uint16_t *d_w_up, int64_t tokens, int64_t in, int64_t ffn, int32_t act, uint16_t *d_dgate,
+                              uint16_t *d_dup, uint16_t *d_dx, void *d_workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- compression inside the backward pass
  * (Section III-C: a layer's dense gradient is compressed as soon as the backward
  * pass has produced it; Section VI-C, discussion of the compute overhead: fusing
@@ -599,6 +617,10 @@ samo_status samo_mfma_rate_probe(int64_t iters, float *d_sink, int32_t workgroup
  *                        layer by itself does not count as a short launch while it is set; that of a plan may.
  *   SAMO_KNOB_STAGED_TILES  the most tiles (of the default weight) with which a fused step counts as a short launch
  *                        and takes the kernel made for those (default 10000); 0: never.
+ *   SAMO_KNOB_GLU_SHAPE  0 to 3: forces the tiles of samo_glu above 32 tokens (256 tokens x 128 features, 128 x 128, 128 x 64, 128 x 32) and,
+ *                        0 to 2, of dX in samo_glu_backward (256 x 256, 128 x 256, 128 x 128); default: by the tiles' number (their rounds
+ *                        of the compute units).
+ *   SAMO_KNOB_GLU_SPLIT  parts of the summation of dX (1 to 16), where they hold four stages of 32 each and the workspace is there.
  * Returns SAMO_ERR_ARG for an unknown knob. */
 enum {
     SAMO_KNOB_OCC_TILE_STEP = 0,
@@ -616,7 +638,9 @@ enum {
     SAMO_KNOB_WGRAD_SPLIT = 12,
     SAMO_KNOB_WGRAD_COLS = 13,
     SAMO_KNOB_STAGED_TILES = 14,
-    SAMO_KNOB_COUNT = 15
+    SAMO_KNOB_GLU_SHAPE = 15,
+    SAMO_KNOB_GLU_SPLIT = 16,
+    SAMO_KNOB_COUNT = 17
 };
 #define SAMO_KNOB_DEFAULT (-1)
 samo_status samo_debug_set(int32_t knob, int32_t value);

@@ -34,7 +34,8 @@ SAMO_OK = 0
 # samo_debug_set knobs
 (KNOB_OCC_TILE_STEP, KNOB_OCC_TILE_STEP32, KNOB_OCC_TILE_DECOMP, KNOB_OCC_TILE_C16, KNOB_OCC_FLAT_GATHER,
  KNOB_OCC_FLAT_STATS, KNOB_OCC_FLAT_STEP, KNOB_INDEX_SPIN_LIMIT, KNOB_WGRAD_TILE, KNOB_WGRAD_ROUND,
- KNOB_INDEX_PASSES, KNOB_TILE_COST, KNOB_WGRAD_SPLIT, KNOB_WGRAD_COLS, KNOB_STAGED_TILES) = range(15)
+ KNOB_INDEX_PASSES, KNOB_TILE_COST, KNOB_WGRAD_SPLIT, KNOB_WGRAD_COLS, KNOB_STAGED_TILES, KNOB_GLU_SHAPE,
+ KNOB_GLU_SPLIT) = range(17)
 KNOB_DEFAULT = -1
 
 
@@ -214,6 +215,15 @@ _SIGNATURES = {
     "samo_attention_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
     "samo_attention_backward": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_void_p, ctypes.c_size_t,
                                                  ctypes.c_void_p]),
+    "samo_glu": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+                                  ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                  ctypes.c_void_p]),
+    "samo_glu_workspace_bytes": (ctypes.c_int32, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                                  ctypes.POINTER(ctypes.c_size_t)]),
+    "samo_glu_backward": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_void_p]),
     "samo_memory_model": (ctypes.c_int32, [ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64),
                                            ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]),
     "samo_wgrad_gather": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
@@ -1138,6 +1148,68 @@ def samo_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor
     _check(lib().samo_attention_backward(ctypes.byref(d), _dev(workspace, torch.uint8, "workspace"),
                                          workspace.numel() if workspace is not None else 0, _stream()),
            "samo_attention_backward")
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+
+
+def _act(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError("act is one of %s, not %r" % (", ".join(ACTIVATIONS), act))
+    return ACTIVATIONS[act]
+
+
+def _dev_matrix_of(t: torch.Tensor, name: str, rows: int, columns: int) -> Optional[int]:
+    ptr, r, c = _dev_matrix(t, name)
+    if (r, c) != (rows, columns):
+        raise ValueError("%s is %d x %d, needs %d x %d" % (name, r, c, rows, columns))
+    return ptr
+
+
+def samo_glu(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, h: torch.Tensor, gate: Optional[torch.Tensor] = None,
+             up: Optional[torch.Tensor] = None, act: str = "silu") -> None:
+    """h = act(x w_gate^T) * (x w_up^T), the pre-activations kept in gate and up if they are given (for the backward pass).
+
+    x: (tokens, in), w_gate, w_up: (ffn, in), h, gate, up: (tokens, ffn), contiguous float16; act: a key of ACTIVATIONS."""
+    x_ptr, tokens, features = _dev_matrix(x, "x")
+    g_ptr, ffn, _ = _dev_matrix(w_gate, "w_gate")
+    if w_gate.shape[1] != features:
+        raise ValueError("x has %d features, w_gate %d" % (features, w_gate.shape[1]))
+    if (gate is None) != (up is None):
+        raise ValueError("gate and up are given together or not at all")
+    _check(lib().samo_glu(x_ptr, g_ptr, _dev_matrix_of(w_up, "w_up", ffn, features), tokens, features, ffn, _act(act),
+                          _dev_matrix_of(h, "h", tokens, ffn),
+                          None if gate is None else _dev_matrix_of(gate, "gate", tokens, ffn),
+                          None if up is None else _dev_matrix_of(up, "up", tokens, ffn), _stream()), "samo_glu")
+
+
+def samo_glu_workspace_bytes(tokens: int, features: int, ffn: int) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().samo_glu_workspace_bytes(int(tokens), int(features), int(ffn), ctypes.byref(out)), "samo_glu_workspace_bytes")
+    return out.value
+
+
+def samo_glu_backward(dh: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+                      dgate: torch.Tensor, dup: torch.Tensor, dx: Optional[torch.Tensor], act: str = "silu",
+                      workspace: Optional[torch.Tensor] = None) -> None:
+    """dgate, dup and (unless None) dx of samo_glu from dh and the gate and up it kept.  The weights' gradients are those of
+    samo_wgrad_gather_batched with dgate and dup as dy.
+
+    workspace (uint8, samo_glu_workspace_bytes of them; an empty one: none) is in use until the stream has passed the call.
+    Without one a call with few tiles of dx takes it from torch's allocator."""
+    dh_ptr, tokens, ffn = _dev_matrix(dh, "dh")
+    g_ptr, _, features = _dev_matrix(w_gate, "w_gate")
+    if w_gate.shape[0] != ffn:
+        raise ValueError("dh has %d features, w_gate %d" % (ffn, w_gate.shape[0]))
+    if workspace is None and dx is not None:
+        need = samo_glu_workspace_bytes(tokens, features, ffn)
+        workspace = _capture_scratch(need) if need else None
+    _check(lib().samo_glu_backward(dh_ptr, _dev_matrix_of(gate, "gate", tokens, ffn), _dev_matrix_of(up, "up", tokens, ffn),
+                                   g_ptr, _dev_matrix_of(w_up, "w_up", ffn, features), tokens, features, ffn, _act(act),
+                                   _dev_matrix_of(dgate, "dgate", tokens, ffn), _dev_matrix_of(dup, "dup", tokens, ffn),
+                                   None if dx is None else _dev_matrix_of(dx, "dx", tokens, features),
+                                   _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0,
+                                   _stream()), "samo_glu_backward")
 
 
 def samo_memory_model(n_total: int, nnz_total: int):

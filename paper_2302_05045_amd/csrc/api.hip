@@ -1295,6 +1295,89 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
     return hip_status(launch_attention_backward(a, as_stream(stream)));
 }
 
+}  // extern "C"
+
+// ---------------------------------------------------------------- gated feed-forward block
+namespace {
+
+samo_status check_glu(int64_t tokens, int64_t in, int64_t ffn, int32_t act)
+{
+    if (tokens < 0 || tokens > INT32_MAX || in < 8 || ffn < 8 || in % 8 || ffn % 8 || in >= 1 << 20 || ffn >= 1 << 20) return SAMO_ERR_SIZE;
+    // a launch's workgroups: the smallest tiles, the most parts
+    if (ceil_div(tokens, 128) * ceil_div(in > ffn ? in : ffn, 64) > INT32_MAX / (2 * kGluMaxSplits)) return SAMO_ERR_SIZE;
+    return act >= SAMO_ACT_SILU && act <= SAMO_ACT_RELU ? SAMO_OK : SAMO_ERR_ARG;
+}
+
+const _Float16 *halves(const uint16_t *p) { return reinterpret_cast<const _Float16 *>(p); }
+_Float16 *halves(uint16_t *p) { return reinterpret_cast<_Float16 *>(p); }
+
+size_t glu_workspace(int64_t tokens, int64_t in, const GluShape &shape)
+{
+    return shape.splits > 1 ? (size_t)shape.splits * (size_t)tokens * (size_t)in * sizeof(float) : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+samo_status samo_glu(const uint16_t *d_x, const uint16_t *d_w_gate, const uint16_t *d_w_up, int64_t tokens, int64_t in,
+                     int64_t ffn, int32_t act, uint16_t *d_h, uint16_t *d_gate, uint16_t *d_up, void *stream)
+{
+    if (samo_status s = check_glu(tokens, in, ffn, act)) return s;
+    if (tokens == 0) return SAMO_OK;
+    if (!d_x || !d_w_gate || !d_w_up || !d_h || !d_gate != !d_up) return SAMO_ERR_NULL;
+    if (misaligned(d_x) || misaligned(d_w_gate) || misaligned(d_w_up) || misaligned(d_h) || misaligned(d_gate) || misaligned(d_up)) return SAMO_ERR_ALIGN;
+    GluArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.x = halves(d_x);
+    a.w_gate = halves(d_w_gate);
+    a.w_up = halves(d_w_up);
+    a.h = halves(d_h);
+    a.gate = halves(d_gate);
+    a.up = halves(d_up);
+    a.tokens = tokens;
+    a.in = (int)in;
+    a.ffn = (int)ffn;
+    return hip_status(launch_glu(act, a, as_stream(stream)));
+}
+
+samo_status samo_glu_workspace_bytes(int64_t tokens, int64_t in, int64_t ffn, size_t *bytes)
+{
+    if (!bytes) return SAMO_ERR_NULL;
+    if (samo_status s = check_glu(tokens, in, ffn, SAMO_ACT_SILU)) return s;
+    *bytes = tokens ? glu_workspace(tokens, in, glu_dx_shape(tokens, ffn, in, kGluMaxSplits)) : 0;
+    return SAMO_OK;
+}
+
+samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, const uint16_t *d_up, const uint16_t *d_w_gate,
+                              const uint16_t *d_w_up, int64_t tokens, int64_t in, int64_t ffn, int32_t act, uint16_t *d_dgate,
+                              uint16_t *d_dup, uint16_t *d_dx, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    if (samo_status s = check_glu(tokens, in, ffn, act)) return s;
+    if (tokens == 0) return SAMO_OK;
+    if (!d_dh || !d_gate || !d_up || !d_dgate || !d_dup || (d_dx && (!d_w_gate || !d_w_up))) return SAMO_ERR_NULL;
+    if (misaligned(d_dh) || misaligned(d_gate) || misaligned(d_up) || misaligned(d_w_gate) || misaligned(d_w_up) || misaligned(d_dgate) ||
+        misaligned(d_dup) || misaligned(d_dx) || misaligned(d_workspace))
+        return SAMO_ERR_ALIGN;
+    GluArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.dh = halves(d_dh);
+    a.gate = const_cast<_Float16 *>(halves(d_gate));
+    a.up = const_cast<_Float16 *>(halves(d_up));
+    a.w_gate = halves(d_w_gate);
+    a.w_up = halves(d_w_up);
+    a.dgate = halves(d_dgate);
+    a.dup = halves(d_dup);
+    a.dx = halves(d_dx);
+    a.tokens = tokens;
+    a.in = (int)in;
+    a.ffn = (int)ffn;
+    GluShape shape = glu_dx_shape(tokens, ffn, in, kGluMaxSplits);
+    if (!d_workspace || workspace_bytes < glu_workspace(tokens, in, shape)) shape = glu_dx_shape(tokens, ffn, in, 1);
+    a.partial = static_cast<float *>(d_workspace);
+    return hip_status(launch_glu_backward(act, a, shape, as_stream(stream)));
+}
+
 samo_status samo_memory_model(int64_t n_total, int64_t nnz_total, int64_t *paper_default, int64_t *paper_samo,
                               int64_t *resident)
 {

@@ -257,6 +257,27 @@ struct AttnArgs {
 hipError_t launch_attention(const AttnArgs &a, hipStream_t s);
 hipError_t launch_attention_backward(const AttnArgs &a, hipStream_t s);
 
+// The gated feed-forward block (glu.hip).
+struct GluArgs {
+    const _Float16 *x, *w_gate, *w_up;      // tokens x in, ffn x in
+    _Float16 *h, *gate, *up;                // tokens x ffn; gate and up NULL: not kept; read in the backward pass
+    const _Float16 *dh;
+    _Float16 *dgate, *dup, *dx;             // dx NULL: not wanted
+    float *partial;                         // splits > 1: fp32 sums, splits x tokens x in
+    int64_t tokens;
+    int in, ffn;
+    int tiles_t, tiles_f, splits, part_stages;
+};
+constexpr int kGluSkinny = 32;             // tokens up to which the weights go past LDS
+constexpr int kGluMaxSplits = 16;
+struct GluShape {
+    int shape = 0, splits = 1, part_stages = 0;
+};
+// The tile shape of dX and the parts its summation is split into, at most max_splits.
+GluShape glu_dx_shape(int64_t tokens, int64_t ffn, int64_t in, int max_splits);
+hipError_t launch_glu(int act, const GluArgs &a, hipStream_t s);
+hipError_t launch_glu_backward(int act, GluArgs a, const GluShape &shape, hipStream_t s);
+
 hipError_t launch_copy(void *dst, const void *src, int64_t bytes, hipStream_t s);
 
 }  // namespace samo

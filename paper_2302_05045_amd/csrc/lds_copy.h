@@ -44,6 +44,14 @@ __device__ __forceinline__ half8 read_fragment(const unsigned char *p, int step)
     return __builtin_bit_cast(half8, q);
 }
 
+// A pointer all lanes of a wave agree on, told to the compiler.
+__device__ __forceinline__ const unsigned char *uniform(const unsigned char *p)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const unsigned char *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a) |
+                                                   (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) << 32);
+}
+
 // A bare workgroup barrier: what has to be complete before it is waited for explicitly.
 __device__ __forceinline__ void meet()
 {

@@ -726,14 +726,6 @@ constexpr int kResidentLds = kSmallTile * kResidentPitch * 2;
 static_assert(2 * kResidentStage <= kResidentLds, "the ring of two stages fits in the image's place");
 static_assert(4 * (kResidentLds + 1024) <= 160 * 1024, "four workgroups to a compute unit");
 
-// A pointer all lanes of a wave agree on, told to the compiler.
-__device__ __forceinline__ const unsigned char *uniform(const unsigned char *p)
-{
-    const uint64_t a = reinterpret_cast<uint64_t>(p);
-    return reinterpret_cast<const unsigned char *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a) |
-                                                   (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) << 32);
-}
-
 template <int OUT>
 __global__ void __launch_bounds__(kResidentThreads, 4) wgrad_resident_kernel(const WgradBatch B)
 {
