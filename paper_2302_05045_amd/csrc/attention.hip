@@ -49,21 +49,40 @@ struct Rows {
     int count, dim;
 };
 
-// The wave's share of a tile: rows first .. first + 63 to LDS; what is behind the rows or the dim is zero.
-template <int PITCH>
-__device__ __forceinline__ void copy_tile(const Rows &R, int first, unsigned lds_at)
-{
-    constexpr int kPieces = PITCH / 16, kRowsPer = 64 / kPieces, kCopies = kTileRows / kRowsPer / 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+// A wave's share of the tiles of one operand.
+template <int KS>
+struct Tiles {
+    static constexpr int PITCH = pitch_of(KS), kPieces = PITCH / 16, kRowsPer = 64 / kPieces, kCopies = kTileRows / kRowsPer / 4;
+    Rows R;
+    bool plain;                                              // whole tiles by a scalar address and these:
+    unsigned offset[kCopies];                                // of the lane's piece from the tile's first row
+    __device__ __forceinline__ static int copy_of(int i) { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kCopies + i; }
+    __device__ __forceinline__ static int row_of(int i) { return copy_of(i) * kRowsPer + (int)(threadIdx.x & 63) / kPieces; }
+    __device__ __forceinline__ static int piece_of(int i) { return (int)(threadIdx.x & 63) % kPieces ^ swizzle<PITCH>(row_of(i)); }
+    __device__ __forceinline__ explicit Tiles(const Rows &rows) : R(rows)
+    {
+        // A dim of whole steps reads no piece behind it into a product that counts; rows less than 2^24 elements apart keep the offsets in 32 bits.
+        plain = R.dim == 16 * KS && R.stride < 1 << 24;
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-        const int copy = wave * kCopies + i, row = copy * kRowsPer + lane / kPieces;
-        const int piece = (lane % kPieces) ^ swizzle<PITCH>(row);
-        const bool there = first + row < R.count && piece * 8 < R.dim;
-        const void *from = there ? static_cast<const void *>(R.base + (int64_t)(first + row) * R.stride + piece * 8) : zero_row;
-        dma16(from, lds_at + copy * 1024);
+        for (int i = 0; i < kCopies; ++i) offset[i] = (unsigned)row_of(i) * (unsigned)R.stride * 2 + (piece_of(i) * 8 < R.dim ? piece_of(i) * 16 : 0);
     }
-}
+    // rows first .. first + 63 to LDS; what is behind the rows is zero, and behind the dim where it counts
+    __device__ __forceinline__ void bring(int first, unsigned lds_at) const
+    {
+        if (plain && first + kTileRows <= R.count) {
+            const unsigned char *base = uniform(reinterpret_cast<const unsigned char *>(R.base + (int64_t)first * R.stride));
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) dma16_from(base, offset[i], lds_at + copy_of(i) * 1024);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int row = first + row_of(i), piece = piece_of(i);
+            const bool there = row < R.count && piece * 8 < R.dim;
+            dma16(there ? static_cast<const void *>(R.base + (int64_t)row * R.stride + piece * 8) : zero_row, lds_at + copy_of(i) * 1024);
+        }
+    }
+};
 
 // Operand with the tile's rows as its rows (32 of them from row 32 block) and 16 columns from 16 ks.
 template <int PITCH>
@@ -182,8 +201,8 @@ __device__ __forceinline__ bool pick_tile(int heads, int batch, int tiles, int &
     if ((int)(blockIdx.x >> 3) >= per_xcd || item >= items) return false;
     const int of_head = item / tiles;
     tile = tiles - 1 - (item - of_head * tiles);
-    b = of_head / heads;
-    head = of_head - b * heads;
+    head = of_head / batch;                                  // every XCD gets all sequences of a few heads: as much work as the others
+    b = of_head - head * batch;
     return true;
 }
 
@@ -246,15 +265,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     const int query = w_first + (lane & 31);
     const int kv = head / A.group;
     const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
-    const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
-    const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
+    const Tiles<KS> K(Rows{A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim});
+    const Tiles<KS> V(Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim});
     int k_first, k_end;
     key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
 
     if (k_first < k_end) {
-        copy_tile<PITCH>(K, k_first, lds_at);
-        copy_tile<PITCH>(V, k_first, lds_at + 2 * kTile);
+        K.bring(k_first, lds_at);
+        V.bring(k_first, lds_at + 2 * kTile);
     }
     half8 own[KS];
     load_own<KS>(Q, w_first, own);
@@ -268,8 +287,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         meet();                                              // the tile is there, and the other one has been read by every wave
         if (k0 + kTileRows < k_end) {
-            copy_tile<PITCH>(K, k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
-            copy_tile<PITCH>(V, k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
+            K.bring(k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
+            V.bring(k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
         }
         if (w_last < w_first || !M.any(w_first, w_last, k0, k0 + kTileRows - 1)) continue;
         const unsigned char *kt = lds + buffer * kTile, *vt = lds + (2 + buffer) * kTile;
@@ -340,16 +359,16 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
     const int query = w_first + (lane & 31);
     const int kv = head / A.group;
     const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
-    const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
-    const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
+    const Tiles<KS> K(Rows{A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim});
+    const Tiles<KS> V(Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim});
     const Rows DO = {A.dout + seq.q0 * A.dout_row + head * A.dout_head, A.dout_row, seq.q_len, A.dim};
     const Rows O = {A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, seq.q_len, A.dim};
     int k_first, k_end;
     key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
     if (k_first < k_end) {
-        copy_tile<PITCH>(K, k_first, lds_at);
-        copy_tile<PITCH>(V, k_first, lds_at + 2 * kTile);
+        K.bring(k_first, lds_at);
+        V.bring(k_first, lds_at + 2 * kTile);
     }
     half8 own[KS], down[KS];
     load_own<KS>(Q, w_first, own);
@@ -379,8 +398,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         meet();
         if (k0 + kTileRows < k_end) {
-            copy_tile<PITCH>(K, k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
-            copy_tile<PITCH>(V, k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
+            K.bring(k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
+            V.bring(k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
         }
         const unsigned char *kt = lds + buffer * kTile, *vt = lds + (2 + buffer) * kTile;
 #pragma unroll
@@ -442,6 +461,8 @@ __global__ void __launch_bounds__(kAttnThreads, KS <= 6 ? 2 : 1) attention_dkv_k
     const int key = w_first + (lane & 31);
     const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
     const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
+    Tiles<KS> Q(Rows{A.q + seq.q0 * A.q_row + kv * A.group * A.q_head, A.q_row, seq.q_len, A.dim});
+    Tiles<KS> DO(Rows{A.dout + seq.q0 * A.dout_row + kv * A.group * A.dout_head, A.dout_row, seq.q_len, A.dim});
     // the queries that see any of the workgroup's keys
     int q_first = 0, q_end = seq.q_len;
     if (M.causal) {
@@ -454,10 +475,10 @@ __global__ void __launch_bounds__(kAttnThreads, KS <= 6 ? 2 : 1) attention_dkv_k
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds, stats_at = (unsigned)(size_t)(LDS_AS unsigned char *)stats;
     auto bring = [&](int shared, int t, int buffer) {
         const int head = kv * A.group + shared, first = q_first + t * kTileRows;
-        const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
-        const Rows DO = {A.dout + seq.q0 * A.dout_row + head * A.dout_head, A.dout_row, seq.q_len, A.dim};
-        copy_tile<PITCH>(Q, first, lds_at + buffer * kTile);
-        copy_tile<PITCH>(DO, first, lds_at + (2 + buffer) * kTile);
+        Q.R.base = A.q + seq.q0 * A.q_row + head * A.q_head;
+        DO.R.base = A.dout + seq.q0 * A.dout_row + head * A.dout_head;
+        Q.bring(first, lds_at + buffer * kTile);
+        DO.bring(first, lds_at + (2 + buffer) * kTile);
         const int64_t stat = (int64_t)head * A.q_tokens + seq.q0;
         if (wave == 0) copy_stats(A.lse + stat, first, seq.q_len, infinite_lse, stats_at + buffer * 2 * kTileRows * 4);
         if (wave == 1) copy_stats(A.delta + stat, first, seq.q_len, reinterpret_cast<const float *>(zero_row), stats_at + (buffer * 2 + 1) * kTileRows * 4);
