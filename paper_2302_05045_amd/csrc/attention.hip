@@ -49,14 +49,14 @@ struct Rows {
     int count, dim;
 };
 
-// A wave's share of the tiles of one operand.
+// A wave's share, one of four, of the tiles of one operand.
 template <int KS>
 struct Tiles {
     static constexpr int PITCH = pitch_of(KS), kPieces = PITCH / 16, kRowsPer = 64 / kPieces, kCopies = kTileRows / kRowsPer / 4;
     Rows R;
     bool plain;                                              // whole tiles by a scalar address and these:
     unsigned offset[kCopies];                                // of the lane's piece from the tile's first row
-    __device__ __forceinline__ static int copy_of(int i) { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kCopies + i; }
+    __device__ __forceinline__ static int copy_of(int i) { return (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3) * kCopies + i; }
     __device__ __forceinline__ static int row_of(int i) { return copy_of(i) * kRowsPer + (int)(threadIdx.x & 63) / kPieces; }
     __device__ __forceinline__ static int piece_of(int i) { return (int)(threadIdx.x & 63) % kPieces ^ swizzle<PITCH>(row_of(i)); }
     __device__ __forceinline__ explicit Tiles(const Rows &rows) : R(rows)
@@ -193,15 +193,17 @@ __device__ __forceinline__ Sequence sequence_of(const AttnArgs &A, int b)
     return s;
 }
 
-// The workgroup's sequence, head and tile of own rows; tiles of a head run backwards (the last queries see the most keys).
+// The workgroup's sequence, head and tile of own rows.  Every XCD gets all sequences of a few heads, as much work as the others; the tiles of a head
+// run backwards, the last queries see the most keys.
 __device__ __forceinline__ bool pick_tile(int heads, int batch, int tiles, int &b, int &head, int &tile)
 {
-    const int items = batch * heads * tiles, per_xcd = (items + 7) / 8;
-    const int item = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per_xcd || item >= items) return false;
+    const int items = batch * heads * tiles, per_xcd = (items + 7) / 8, local = (int)(blockIdx.x >> 3);
+    if (local >= per_xcd) return false;
+    const int item = (int)(blockIdx.x & 7) * per_xcd + local;
+    if (item >= items) return false;
     const int of_head = item / tiles;
     tile = tiles - 1 - (item - of_head * tiles);
-    head = of_head / batch;                                  // every XCD gets all sequences of a few heads: as much work as the others
+    head = of_head / batch;
     b = of_head - head * batch;
     return true;
 }
@@ -442,12 +444,18 @@ __device__ __forceinline__ void copy_stats(const float *from, int first, int cou
 }
 __device__ const float infinite_lse[1] = {INFINITY};         // a probability of zero
 
-// dK and dV: a wave owns 32 keys, the queries of every head that shares them come by.
+// dK and dV: 128 keys to a workgroup of eight waves, 32 to a wave and the one four behind it, of which one takes the first 32 queries of every tile and the
+// other the last; their sums meet in LDS at the end.  The queries of every head that shares the keys come by.  Eight waves because a workgroup's
+// time counts as much as the device's: under a causal mask the first keys are seen by every query (8192 tokens, 32 heads of 128, 8 of keys:
+// with four waves the longest of 512 workgroups took 1.8 ms by itself).
+// Two waves to a SIMD have 256 registers each.  Heads of more than 96 fill half of them with their sums: there the rows of V stay in LDS, from where
+// they are read for every block.
 template <int KS>
-__global__ void __launch_bounds__(kAttnThreads, KS <= 6 ? 2 : 1) attention_dkv_kernel(const AttnArgs A)
+__global__ void __launch_bounds__(2 * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {
+    constexpr bool kWide = KS > 6;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // Q, dO; two tiles each
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide ? kOwnRows * PITCH : 0)];       // Q, dO; two tiles each; V
     __shared__ __attribute__((aligned(16))) float stats[2][2][kTileRows];         // lse, delta
     int b, kv, tile;
     if (!pick_tile(A.kv_heads, A.batch, A.tiles, b, kv, tile)) return;
@@ -455,14 +463,17 @@ __global__ void __launch_bounds__(kAttnThreads, KS <= 6 ? 2 : 1) attention_dkv_k
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.k_len) return;
     const Mask M = mask_of(A, seq);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, side = wave >> 2, qb = side;
     const int k_first = tile * kOwnRows, k_last = min(k_first + kOwnRows, seq.k_len) - 1;
-    const int w_first = k_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.k_len) - 1;
+    const int w_first = k_first + (wave & 3) * kWaveRows, w_last = min(w_first + kWaveRows, seq.k_len) - 1;
     const int key = w_first + (lane & 31);
     const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
     const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
-    Tiles<KS> Q(Rows{A.q + seq.q0 * A.q_row + kv * A.group * A.q_head, A.q_row, seq.q_len, A.dim});
-    Tiles<KS> DO(Rows{A.dout + seq.q0 * A.dout_row + kv * A.group * A.dout_head, A.dout_row, seq.q_len, A.dim});
+    // waves 0-3 bring Q and lse, 4-7 dO and delta
+    const _Float16 *coming = side ? A.dout + seq.q0 * A.dout_row : A.q + seq.q0 * A.q_row;
+    const int64_t apart = side ? A.dout_head : A.q_head;
+    Tiles<KS> queries(Rows{coming, side ? A.dout_row : A.q_row, seq.q_len, A.dim});
+    const float *coming_stats = (side ? A.delta : A.lse) + seq.q0, *behind = side ? reinterpret_cast<const float *>(zero_row) : infinite_lse;
     // the queries that see any of the workgroup's keys
     int q_first = 0, q_end = seq.q_len;
     if (M.causal) {
@@ -475,18 +486,16 @@ __global__ void __launch_bounds__(kAttnThreads, KS <= 6 ? 2 : 1) attention_dkv_k
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds, stats_at = (unsigned)(size_t)(LDS_AS unsigned char *)stats;
     auto bring = [&](int shared, int t, int buffer) {
         const int head = kv * A.group + shared, first = q_first + t * kTileRows;
-        Q.R.base = A.q + seq.q0 * A.q_row + head * A.q_head;
-        DO.R.base = A.dout + seq.q0 * A.dout_row + head * A.dout_head;
-        Q.bring(first, lds_at + buffer * kTile);
-        DO.bring(first, lds_at + (2 + buffer) * kTile);
-        const int64_t stat = (int64_t)head * A.q_tokens + seq.q0;
-        if (wave == 0) copy_stats(A.lse + stat, first, seq.q_len, infinite_lse, stats_at + buffer * 2 * kTileRows * 4);
-        if (wave == 1) copy_stats(A.delta + stat, first, seq.q_len, reinterpret_cast<const float *>(zero_row), stats_at + (buffer * 2 + 1) * kTileRows * 4);
+        queries.R.base = coming + head * apart;
+        queries.bring(first, lds_at + (2 * side + buffer) * kTile);
+        if ((wave & 3) == 0) copy_stats(coming_stats + (int64_t)head * A.q_tokens, first, seq.q_len, behind, stats_at + (buffer * 2 + side) * kTileRows * 4);
     };
+    if (kWide) Tiles<KS>(V).bring(k_first + side * kTileRows, lds_at + 4 * kTile + side * kTileRows * PITCH);
     if (tiles > 0) bring(0, 0, 0);
-    half8 own[KS], ownv[KS];
+    half8 own[KS], ownv[kWide ? 1 : KS];
     load_own<KS>(K, w_first, own);
-    load_own<KS>(V, w_first, ownv);
+    if constexpr (!kWide) load_own<KS>(V, w_first, ownv);
+    const unsigned char *v_rows = lds + 4 * kTile + (wave & 3) * kWaveRows * PITCH;
     const Span seen(M.first_query(key), M.end_query(key));
     f32x16 dk[DB], dv[DB];
     clear(dk);
@@ -500,52 +509,78 @@ __global__ void __launch_bounds__(kAttnThreads, KS <= 6 ? 2 : 1) attention_dkv_k
             if (t + 1 < tiles) bring(shared, t + 1, buffer ^ 1);
             else if (shared + 1 < A.group) bring(shared + 1, 0, buffer ^ 1);
             const unsigned char *qt = lds + buffer * kTile, *dot = lds + (2 + buffer) * kTile;
+            const int q1 = q_first + t * kTileRows + 32 * qb;
+            if (q1 >= seq.q_len || w_last < w_first || !M.any(q1, q1 + 31, w_first, w_last)) continue;
+            f32x16 s[1], dp[1];
+            clear(s);
+            clear(dp);
 #pragma unroll
-            for (int qb = 0; qb < 2; ++qb) {
-                const int q1 = q_first + t * kTileRows + 32 * qb;
-                if (q1 >= seq.q_len || w_last < w_first || !M.any(q1, q1 + 31, w_first, w_last)) continue;
-                f32x16 s[1], dp[1];
-                clear(s);
-                clear(dp);
+            for (int ks = 0; ks < KS; ++ks) {
+                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
+                const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
+                dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
+            }
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
-                    dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), ownv[ks], dp[0], 0, 0, 0);
+            for (int g = 0; g < 4; ++g) {
+                const int at = 32 * qb + 8 * g + 4 * (lane >> 5);
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][at]), delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][at]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 4 * g + e;
+                    s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
+                    dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
                 }
-                const int half = lane >> 5;
+            }
+            if (!M.all(q1, q1 + 31, w_first, w_last)) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][32 * qb + 8 * g + 4 * half]);
-                    const f32x4 delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][32 * qb + 8 * g + 4 * half]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * g + e;
-                        s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
-                        dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const bool on = seen.holds(q1 + acc_row(i));
+                    s[0][i] = on ? s[0][i] : 0.f;
+                    dp[0][i] = on ? dp[0][i] : 0.f;
                 }
-                if (!M.all(q1, q1 + 31, w_first, w_last)) {
+            }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool on = seen.holds(q1 + acc_row(i));
-                        s[0][i] = on ? s[0][i] : 0.f;
-                        dp[0][i] = on ? dp[0][i] : 0.f;
-                    }
-                }
+            for (int step = 0; step < 2; ++step) {
+                const half8 p = to_half8(s[0], 8 * step), ds = to_half8(dp[0], 8 * step);
 #pragma unroll
-                for (int step = 0; step < 2; ++step) {
-                    const half8 p = to_half8(s[0], 8 * step), ds = to_half8(dp[0], 8 * step);
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(dot, 2 * qb + step, db), p, dv[db], 0, 0, 0);
-                        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(qt, 2 * qb + step, db), ds, dk[db], 0, 0, 0);
-                    }
+                for (int db = 0; db < DB; ++db) {
+                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(dot, 2 * qb + step, db), p, dv[db], 0, 0, 0);
+                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(qt, 2 * qb + step, db), ds, dk[db], 0, 0, 0);
                 }
             }
         }
+    // a wave of the first four keeps dK and the one behind it dV: each gets the other's sums of it, kPart blocks of dims at a time
+    constexpr int kPart = 4 * kTile / (8 * 4096);
+    f32x4 *meeting = reinterpret_cast<f32x4 *>(lds) + lane;
+    auto give = [&](const f32x16 (&acc)[DB], int first) {
+#pragma unroll
+        for (int i = 0; i < kPart && first + i < DB; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                meeting[(((wave ^ 4) * kPart + i) * 4 + g) * 64] = f32x4{acc[first + i][4 * g], acc[first + i][4 * g + 1], acc[first + i][4 * g + 2], acc[first + i][4 * g + 3]};
+    };
+    auto take = [&](f32x16 (&acc)[DB], int first) {
+#pragma unroll
+        for (int i = 0; i < kPart && first + i < DB; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 other = meeting[((wave * kPart + i) * 4 + g) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[first + i][4 * g + e] += other[e];
+            }
+    };
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_own<DB>(A.dk + seq.k0 * A.dk_row + kv * A.dk_head, A.dk_row, key, seq.k_len, A.dim, dk, A.scale);
-    store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
+#pragma unroll
+    for (int first = 0; first < DB; first += kPart) {
+        __syncthreads();
+        if (side) give(dk, first);
+        else give(dv, first);
+        __syncthreads();
+        if (side) take(dv, first);
+        else take(dk, first);
+    }
+    if (side) store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
+    else store_own<DB>(A.dk + seq.k0 * A.dk_row + kv * A.dk_head, A.dk_row, key, seq.k_len, A.dim, dk, A.scale);
 }
 
 enum { kForward, kDq, kDkv };
@@ -555,7 +590,7 @@ hipError_t launch_dim(int which, const AttnArgs &a, dim3 grid, hipStream_t s)
 {
     if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
-    else hipLaunchKernelGGL((attention_dkv_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
+    else hipLaunchKernelGGL((attention_dkv_kernel<KS>), grid, dim3(2 * kAttnThreads), 0, s, a);
     return hipGetLastError();
 }
 
