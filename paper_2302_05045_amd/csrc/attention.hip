@@ -444,14 +444,14 @@ __device__ __forceinline__ void copy_stats(const float *from, int first, int cou
 }
 __device__ const float infinite_lse[1] = {INFINITY};         // a probability of zero
 
-// dK and dV: 128 keys to a workgroup of eight waves, 32 to a wave and the one four behind it, of which one takes the first 32 queries of every tile and the
-// other the last; their sums meet in LDS at the end.  The queries of every head that shares the keys come by.  Eight waves because a workgroup's
-// time counts as much as the device's: under a causal mask the first keys are seen by every query (8192 tokens, 32 heads of 128, 8 of keys:
-// with four waves the longest of 512 workgroups took 1.8 ms by itself).
+// dK and dV: 128 keys to a workgroup, 32 to a wave; the queries of every head that shares the keys come by.  With SIDES = 2 a wave and the one four behind it
+// have the same keys, one takes the first 32 queries of every tile and the other the last, and their sums meet in LDS at the end: a workgroup's time
+// counts as much as the device's, under a causal mask the first keys are seen by every query (8192 tokens, 32 heads of 128, 8 of keys: with
+// four waves the longest of 512 workgroups took 1.8 ms by itself; the whole backward pass 2414 -> 2090 us).
 // Two waves to a SIMD have 256 registers each.  Heads of more than 96 fill half of them with their sums: there the rows of V stay in LDS, from where
 // they are read for every block.
-template <int KS>
-__global__ void __launch_bounds__(2 * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
+template <int KS, int SIDES>
+__global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {
     constexpr bool kWide = KS > 6;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
@@ -463,17 +463,25 @@ __global__ void __launch_bounds__(2 * kAttnThreads, 2) attention_dkv_kernel(cons
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.k_len) return;
     const Mask M = mask_of(A, seq);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, side = wave >> 2, qb = side;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, side = wave >> 2;
     const int k_first = tile * kOwnRows, k_last = min(k_first + kOwnRows, seq.k_len) - 1;
     const int w_first = k_first + (wave & 3) * kWaveRows, w_last = min(w_first + kWaveRows, seq.k_len) - 1;
     const int key = w_first + (lane & 31);
     const Rows K = {A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim};
     const Rows V = {A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim};
-    // waves 0-3 bring Q and lse, 4-7 dO and delta
-    const _Float16 *coming = side ? A.dout + seq.q0 * A.dout_row : A.q + seq.q0 * A.q_row;
-    const int64_t apart = side ? A.dout_head : A.q_head;
-    Tiles<KS> queries(Rows{coming, side ? A.dout_row : A.q_row, seq.q_len, A.dim});
-    const float *coming_stats = (side ? A.delta : A.lse) + seq.q0, *behind = side ? reinterpret_cast<const float *>(zero_row) : infinite_lse;
+    // Q and lse come by waves 0-3, dO and delta by 4-7 where there are such
+    struct Coming {
+        Tiles<KS> tiles;
+        const _Float16 *base;
+        int64_t apart;
+        const float *stats, *behind;
+    };
+    auto coming_of = [&](int what) {
+        const _Float16 *base = what ? A.dout + seq.q0 * A.dout_row : A.q + seq.q0 * A.q_row;
+        return Coming{Tiles<KS>(Rows{base, what ? A.dout_row : A.q_row, seq.q_len, A.dim}), base, what ? A.dout_head : A.q_head,
+                      (what ? A.delta : A.lse) + seq.q0, what ? reinterpret_cast<const float *>(zero_row) : infinite_lse};
+    };
+    Coming first_operand = coming_of(side), second_operand = coming_of(1);
     // the queries that see any of the workgroup's keys
     int q_first = 0, q_end = seq.q_len;
     if (M.causal) {
@@ -484,13 +492,18 @@ __global__ void __launch_bounds__(2 * kAttnThreads, 2) attention_dkv_kernel(cons
     }
     const int tiles = q_end > q_first ? (q_end - q_first + kTileRows - 1) / kTileRows : 0;
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds, stats_at = (unsigned)(size_t)(LDS_AS unsigned char *)stats;
-    auto bring = [&](int shared, int t, int buffer) {
+    auto bring_one = [&](Coming &c, int what, int shared, int t, int buffer) {
         const int head = kv * A.group + shared, first = q_first + t * kTileRows;
-        queries.R.base = coming + head * apart;
-        queries.bring(first, lds_at + (2 * side + buffer) * kTile);
-        if ((wave & 3) == 0) copy_stats(coming_stats + (int64_t)head * A.q_tokens, first, seq.q_len, behind, stats_at + (buffer * 2 + side) * kTileRows * 4);
+        c.tiles.R.base = c.base + head * c.apart;
+        c.tiles.bring(first, lds_at + (2 * what + buffer) * kTile);
+        if ((wave & 3) == 0) copy_stats(c.stats + (int64_t)head * A.q_tokens, first, seq.q_len, c.behind, stats_at + (buffer * 2 + what) * kTileRows * 4);
     };
-    if (kWide) Tiles<KS>(V).bring(k_first + side * kTileRows, lds_at + 4 * kTile + side * kTileRows * PITCH);
+    auto bring = [&](int shared, int t, int buffer) {
+        bring_one(first_operand, side, shared, t, buffer);
+        if (SIDES == 1) bring_one(second_operand, 1, shared, t, buffer);
+    };
+    if (kWide)
+        for (int part = side; part < 2; part += SIDES) Tiles<KS>(V).bring(k_first + part * kTileRows, lds_at + 4 * kTile + part * kTileRows * PITCH);
     if (tiles > 0) bring(0, 0, 0);
     half8 own[KS], ownv[kWide ? 1 : KS];
     load_own<KS>(K, w_first, own);
@@ -509,88 +522,102 @@ __global__ void __launch_bounds__(2 * kAttnThreads, 2) attention_dkv_kernel(cons
             if (t + 1 < tiles) bring(shared, t + 1, buffer ^ 1);
             else if (shared + 1 < A.group) bring(shared + 1, 0, buffer ^ 1);
             const unsigned char *qt = lds + buffer * kTile, *dot = lds + (2 + buffer) * kTile;
-            const int q1 = q_first + t * kTileRows + 32 * qb;
-            if (q1 >= seq.q_len || w_last < w_first || !M.any(q1, q1 + 31, w_first, w_last)) continue;
-            f32x16 s[1], dp[1];
-            clear(s);
-            clear(dp);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
-                const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
-                dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
-            }
+            for (int part = 0; part < 2 / SIDES; ++part) {
+                const int qb = SIDES == 2 ? side : part;
+                const int q1 = q_first + t * kTileRows + 32 * qb;
+                if (q1 >= seq.q_len || w_last < w_first || !M.any(q1, q1 + 31, w_first, w_last)) continue;
+                f32x16 s[1], dp[1];
+                clear(s);
+                clear(dp);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at = 32 * qb + 8 * g + 4 * (lane >> 5);
-                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][at]), delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][at]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 4 * g + e;
-                    s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
-                    dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
+                for (int ks = 0; ks < KS; ++ks) {
+                    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
+                    const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
+                    dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
                 }
-            }
-            if (!M.all(q1, q1 + 31, w_first, w_last)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool on = seen.holds(q1 + acc_row(i));
-                    s[0][i] = on ? s[0][i] : 0.f;
-                    dp[0][i] = on ? dp[0][i] : 0.f;
+                for (int g = 0; g < 4; ++g) {
+                    const int at = 32 * qb + 8 * g + 4 * (lane >> 5);
+                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][at]), delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][at]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = 4 * g + e;
+                        s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
+                        dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
+                    }
                 }
-            }
+                if (!M.all(q1, q1 + 31, w_first, w_last)) {
 #pragma unroll
-            for (int step = 0; step < 2; ++step) {
-                const half8 p = to_half8(s[0], 8 * step), ds = to_half8(dp[0], 8 * step);
+                    for (int i = 0; i < 16; ++i) {
+                        const bool on = seen.holds(q1 + acc_row(i));
+                        s[0][i] = on ? s[0][i] : 0.f;
+                        dp[0][i] = on ? dp[0][i] : 0.f;
+                    }
+                }
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(dot, 2 * qb + step, db), p, dv[db], 0, 0, 0);
-                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(qt, 2 * qb + step, db), ds, dk[db], 0, 0, 0);
+                for (int step = 0; step < 2; ++step) {
+                    const half8 p = to_half8(s[0], 8 * step), ds = to_half8(dp[0], 8 * step);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(dot, 2 * qb + step, db), p, dv[db], 0, 0, 0);
+                        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(qt, 2 * qb + step, db), ds, dk[db], 0, 0, 0);
+                    }
                 }
             }
         }
-    // a wave of the first four keeps dK and the one behind it dV: each gets the other's sums of it, kPart blocks of dims at a time
-    constexpr int kPart = 4 * kTile / (8 * 4096);
-    f32x4 *meeting = reinterpret_cast<f32x4 *>(lds) + lane;
-    auto give = [&](const f32x16 (&acc)[DB], int first) {
+    if constexpr (SIDES == 2) {
+        // a wave of the first four keeps dK and the one behind it dV: each gets the other's sums of it, kPart blocks of dims at a time
+        constexpr int kPart = 4 * kTile / (8 * 4096);
+        f32x4 *meeting = reinterpret_cast<f32x4 *>(lds) + lane;
+        auto give = [&](const f32x16 (&acc)[DB], int first) {
 #pragma unroll
-        for (int i = 0; i < kPart && first + i < DB; ++i)
+            for (int i = 0; i < kPart && first + i < DB; ++i)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                meeting[(((wave ^ 4) * kPart + i) * 4 + g) * 64] = f32x4{acc[first + i][4 * g], acc[first + i][4 * g + 1], acc[first + i][4 * g + 2], acc[first + i][4 * g + 3]};
-    };
-    auto take = [&](f32x16 (&acc)[DB], int first) {
+                for (int g = 0; g < 4; ++g)
+                    meeting[(((wave ^ 4) * kPart + i) * 4 + g) * 64] = f32x4{acc[first + i][4 * g], acc[first + i][4 * g + 1], acc[first + i][4 * g + 2], acc[first + i][4 * g + 3]};
+        };
+        auto take = [&](f32x16 (&acc)[DB], int first) {
 #pragma unroll
-        for (int i = 0; i < kPart && first + i < DB; ++i)
+            for (int i = 0; i < kPart && first + i < DB; ++i)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 other = meeting[((wave * kPart + i) * 4 + g) * 64];
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 other = meeting[((wave * kPart + i) * 4 + g) * 64];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[first + i][4 * g + e] += other[e];
-            }
-    };
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    for (int e = 0; e < 4; ++e) acc[first + i][4 * g + e] += other[e];
+                }
+        };
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int first = 0; first < DB; first += kPart) {
-        __syncthreads();
-        if (side) give(dk, first);
-        else give(dv, first);
-        __syncthreads();
-        if (side) take(dv, first);
-        else take(dk, first);
+        for (int first = 0; first < DB; first += kPart) {
+            __syncthreads();
+            if (side) give(dk, first);
+            else give(dv, first);
+            __syncthreads();
+            if (side) take(dv, first);
+            else take(dk, first);
+        }
     }
-    if (side) store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
-    else store_own<DB>(A.dk + seq.k0 * A.dk_row + kv * A.dk_head, A.dk_row, key, seq.k_len, A.dim, dk, A.scale);
+    if (SIDES == 1 || side) store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
+    if (SIDES == 1 || !side) store_own<DB>(A.dk + seq.k0 * A.dk_row + kv * A.dk_head, A.dk_row, key, seq.k_len, A.dim, dk, A.scale);
 }
 
 enum { kForward, kDq, kDkv };
+
+// The workgroups of dK and dV from which a wave has its keys for itself; below, where the longest workgroup is what the call waits for, two share them.
+// Whole backward pass of heads of 64, one wave / two, us: 256 workgroups, 2048 tokens of 16 heads 98 / 85; 512, two times 2048 of 32 heads 77 / 84;
+// 512, 16384 of 16 heads on 4 2795 / 2795; 1024, 8192 in 16 sequences of 16 heads 90 / 104; 2048, 8192 of 32 heads 1185 / 1230.  Heads of 80 and 96
+// gain less from it (97 / 100, 121 / 134, 1580 / 1570; 512 long ones 3950 / 3400): two always, one would spill besides.
+constexpr int kOneSideFrom = 512;
 
 template <int KS>
 hipError_t launch_dim(int which, const AttnArgs &a, dim3 grid, hipStream_t s)
 {
     if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
-    else hipLaunchKernelGGL((attention_dkv_kernel<KS>), grid, dim3(2 * kAttnThreads), 0, s, a);
+    else if (KS <= 4 && (int64_t)a.batch * a.kv_heads * a.tiles >= kOneSideFrom)
+        hipLaunchKernelGGL((attention_dkv_kernel<KS, KS <= 4 ? 1 : 2>), grid, dim3(kAttnThreads), 0, s, a);
+    else hipLaunchKernelGGL((attention_dkv_kernel<KS, 2>), grid, dim3(2 * kAttnThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -144,6 +144,14 @@ def test_shared_heads(heads, kv):
     check([150], [150], heads, kv, 64, True, 0)
 
 
+@pytest.mark.parametrize("dim", [24, 64])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 40), (False, 0)])
+def test_many_workgroups(dim, causal, window):
+    """8 sequences, 16 heads, 4 tiles of keys: enough for the form in which a wave has its keys for itself."""
+    lens = [130, 0, 1, 64, 257, 200, 128, 65]
+    check(lens, [n + 3 * i for i, n in enumerate(lens)], 16, 16, dim, causal, window, slack=230, seed=dim)
+
+
 def test_large_scores_and_small_gradients():
     """Scores of hundreds (one key takes all of a row), rows whose largest score comes last, gradients among fp16's small numbers."""
     check([300], [300], 2, 2, 64, True, 0, std=6.0)
