@@ -449,7 +449,10 @@ samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
  * dim is a multiple of 8 up to 128; lengths from 0.  P = exp(S - lse) and dS = P (dP - delta) are rounded to fp16 where they enter a product
  * (as the tensors themselves are), sums and softmax are fp32; the order of the sums is fixed.  Masked scores are replaced, so a key
  * that is not finite does not reach a query that does not see its tile of 64 keys; within a tile a value that is not finite does (0 times it).
- * Backward: dq, dk, dv from dout and the forward pass's q, k, v, out, lse; d_workspace: samo_attention_workspace_bytes, 16-byte aligned. */
+ * Backward: dq, dk, dv from dout and the forward pass's q, k, v, out, lse; d_workspace: samo_attention_workspace_bytes, 16-byte aligned.
+ * Calls of few heads and rows (a few tokens behind a long context) split the keys, or for dk and dv the queries, over workgroups whose fp32 sums
+ * meet in d_sums; samo_attention_sums_bytes is what the forward or backward call can use of it on the current device (0: nothing),
+ * with less it does without.  Both workspaces are in use until the stream has passed the call. */
 typedef struct {
     void *d_data;
     int64_t row, head;
@@ -463,8 +466,11 @@ typedef struct {
     int32_t batch, heads, kv_heads, dim, max_q, max_k;
     float scale;
     int32_t causal, window;
+    void *d_sums;                                    /* samo_attention_sums_bytes, 16-byte aligned, or NULL */
+    size_t sums_bytes;
 } samo_attention_desc;
 samo_status samo_attention(const samo_attention_desc *h_desc, void *stream);
+samo_status samo_attention_sums_bytes(const samo_attention_desc *h_desc, int32_t backward, size_t *bytes);
 samo_status samo_attention_workspace_bytes(const samo_attention_desc *h_desc, size_t *bytes);
 samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_workspace, size_t workspace_bytes, void *stream);
 
@@ -621,6 +627,8 @@ samo_status samo_mfma_rate_probe(int64_t iters, float *d_sink, int32_t workgroup
  *                        0 to 2, of dX in samo_glu_backward (256 x 256, 128 x 256, 128 x 128); default: by the tiles' number (their rounds
  *                        of the compute units).
  *   SAMO_KNOB_GLU_SPLIT  parts of the summation of dX (1 to 16), where they hold four stages of 32 each and the workspace is there.
+ *   SAMO_KNOB_ATTENTION_SPLIT  parts (1 to 16) that attention splits the keys or queries into where the memory for their sums is there;
+ *                        default: by the number of workgroups and of tiles.  samo_attention_sums_bytes follows it.
  * Returns SAMO_ERR_ARG for an unknown knob. */
 enum {
     SAMO_KNOB_OCC_TILE_STEP = 0,
@@ -640,7 +648,8 @@ enum {
     SAMO_KNOB_STAGED_TILES = 14,
     SAMO_KNOB_GLU_SHAPE = 15,
     SAMO_KNOB_GLU_SPLIT = 16,
-    SAMO_KNOB_COUNT = 17
+    SAMO_KNOB_ATTENTION_SPLIT = 17,
+    SAMO_KNOB_COUNT = 18
 };
 #define SAMO_KNOB_DEFAULT (-1)
 samo_status samo_debug_set(int32_t knob, int32_t value);

@@ -35,7 +35,7 @@ SAMO_OK = 0
 (KNOB_OCC_TILE_STEP, KNOB_OCC_TILE_STEP32, KNOB_OCC_TILE_DECOMP, KNOB_OCC_TILE_C16, KNOB_OCC_FLAT_GATHER,
  KNOB_OCC_FLAT_STATS, KNOB_OCC_FLAT_STEP, KNOB_INDEX_SPIN_LIMIT, KNOB_WGRAD_TILE, KNOB_WGRAD_ROUND,
  KNOB_INDEX_PASSES, KNOB_TILE_COST, KNOB_WGRAD_SPLIT, KNOB_WGRAD_COLS, KNOB_STAGED_TILES, KNOB_GLU_SHAPE,
- KNOB_GLU_SPLIT) = range(17)
+ KNOB_GLU_SPLIT, KNOB_ATTENTION_SPLIT) = range(18)
 KNOB_DEFAULT = -1
 
 
@@ -111,7 +111,8 @@ class AttentionDesc(ctypes.Structure):
                 ("d_q_start", ctypes.c_void_p), ("d_k_start", ctypes.c_void_p), ("q_tokens", ctypes.c_int64),
                 ("k_tokens", ctypes.c_int64), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
                 ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
-                ("scale", ctypes.c_float), ("causal", ctypes.c_int32), ("window", ctypes.c_int32)]
+                ("scale", ctypes.c_float), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("d_sums", ctypes.c_void_p), ("sums_bytes", ctypes.c_size_t)]
 
 
 class StepGuard(ctypes.Structure):
@@ -212,6 +213,8 @@ _SIGNATURES = {
     "samo_state8_pack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
     "samo_state8_unpack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
     "samo_attention": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_void_p]),
+    "samo_attention_sums_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_int32,
+                                                   ctypes.POINTER(ctypes.c_size_t)]),
     "samo_attention_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
     "samo_attention_backward": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_void_p, ctypes.c_size_t,
                                                  ctypes.c_void_p]),
@@ -1117,16 +1120,34 @@ def _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, 
     return d
 
 
+def _attention_sums(d: AttentionDesc, backward: bool, workspace: Optional[torch.Tensor], used: int) -> Optional[torch.Tensor]:
+    """Gives d the sums' memory behind the first `used` bytes of the workspace, which is taken from torch's allocator if there is none."""
+    used = (used + 15) // 16 * 16
+    if workspace is None:
+        need = ctypes.c_size_t()
+        _check(lib().samo_attention_sums_bytes(ctypes.byref(d), backward, ctypes.byref(need)), "samo_attention_sums_bytes")
+        workspace = _capture_scratch(used + need.value) if used + need.value else None
+        if workspace is None and used:                    # without the sums the call does, without the rest it does not
+            workspace = _capture_scratch(used)
+    if workspace is not None and workspace.numel() > used:
+        d.d_sums, d.sums_bytes = _dev(workspace, torch.uint8, "workspace") + used, workspace.numel() - used
+    return workspace
+
+
 def samo_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
                    causal: bool = True, window: int = 0, scale: Optional[float] = None,
                    q_start: Optional[torch.Tensor] = None, k_start: Optional[torch.Tensor] = None,
-                   max_q: Optional[int] = None, max_k: Optional[int] = None) -> None:
+                   max_q: Optional[int] = None, max_k: Optional[int] = None,
+                   workspace: Optional[torch.Tensor] = None) -> None:
     """out = softmax(scale q k^T + mask) v and lse, its rows' log-sum-exp, over packed sequences.
 
     q, out: (tokens, heads, dim), k, v: (tokens, kv_heads, dim) fp16, strided as slices of a packed projection are; lse: float32
     (heads, tokens).  q_start, k_start: int32 (sequences + 1) on the GPU, the sequences' first tokens; none: one sequence.
-    max_q, max_k: the longest sequence's tokens (default: all tokens).  scale: default 1 / sqrt(dim)."""
+    max_q, max_k: the longest sequence's tokens (default: all tokens).  scale: default 1 / sqrt(dim).
+    Few heads and rows split the keys over workgroups, whose sums meet in the workspace (uint8; in use until the stream has passed the
+    call; too few bytes, or an empty one: not split).  Without one the call takes what it can use from torch's allocator."""
     d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)
+    workspace = _attention_sums(d, False, workspace, 0)
     _check(lib().samo_attention(ctypes.byref(d), _stream()), "samo_attention")
 
 
@@ -1137,14 +1158,12 @@ def samo_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor
                             max_k: Optional[int] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """dq, dk, dv of samo_attention with the same arguments, from dout and what the forward pass left in out and lse.
 
-    workspace (uint8, 4 * heads * tokens bytes) is in use until the stream has passed the call; without one the call takes
-    it from torch's allocator."""
+    workspace (uint8, 4 * heads * tokens bytes; more, from the next multiple of 16, for the sums of calls of few heads and rows) is in use until the
+    stream has passed the call; without one the call takes it from torch's allocator."""
     d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)
     d.dout, d.dq = _heads(dout, "dout", tuple(q.shape)), _heads(dq, "dq", tuple(q.shape))
     d.dk, d.dv = _heads(dk, "dk", tuple(k.shape)), _heads(dv, "dv", tuple(k.shape))
-    need = 4 * q.shape[0] * q.shape[1]
-    if workspace is None and need:
-        workspace = _capture_scratch(need)
+    workspace = _attention_sums(d, True, workspace, 4 * q.shape[0] * q.shape[1])
     _check(lib().samo_attention_backward(ctypes.byref(d), _dev(workspace, torch.uint8, "workspace"),
                                          workspace.numel() if workspace is not None else 0, _stream()),
            "samo_attention_backward")

@@ -1227,6 +1227,7 @@ samo_status check_attention(const samo_attention_desc *d, bool backward, AttnArg
         return SAMO_ERR_ALIGN;
     if (!(std::isfinite(d->scale) && d->scale > 0.f) || d->window < 0 || (d->window > 0 && !d->causal)) return SAMO_ERR_ARG;
     if (d->q_tokens > 0 && !d->d_lse) return SAMO_ERR_NULL;
+    if (misaligned(d->d_sums)) return SAMO_ERR_ALIGN;
     // a launch's workgroups, 128 rows of a head each, fit 31 bits
     if (ceil_div(d->max_q, 128) * d->batch * d->heads > INT32_MAX / 2 || ceil_div(d->max_k, 128) * d->batch * d->kv_heads > INT32_MAX / 2)
         return SAMO_ERR_SIZE;
@@ -1261,6 +1262,7 @@ samo_status check_attention(const samo_attention_desc *d, bool backward, AttnArg
     a->causal = d->causal != 0;
     a->window = d->window;
     a->scale = d->scale;
+    a->parts = static_cast<float *>(d->d_sums);
     return SAMO_OK;
 }
 
@@ -1272,7 +1274,16 @@ samo_status samo_attention(const samo_attention_desc *h_desc, void *stream)
 {
     AttnArgs a;
     if (samo_status s = check_attention(h_desc, false, &a)) return s;
-    return hip_status(launch_attention(a, as_stream(stream)));
+    return hip_status(launch_attention(a, h_desc->sums_bytes, as_stream(stream)));
+}
+
+samo_status samo_attention_sums_bytes(const samo_attention_desc *h_desc, int32_t backward, size_t *bytes)
+{
+    if (!bytes) return SAMO_ERR_NULL;
+    AttnArgs a;
+    if (samo_status s = check_attention(h_desc, backward != 0, &a)) return s;
+    *bytes = (size_t)attention_sums_bytes(a, backward != 0);
+    return SAMO_OK;
 }
 
 samo_status samo_attention_workspace_bytes(const samo_attention_desc *h_desc, size_t *bytes)
@@ -1292,7 +1303,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
     if (need > 0 && (!d_workspace || workspace_bytes < need)) return SAMO_ERR_WORKSPACE;
     if (misaligned(d_workspace)) return SAMO_ERR_ALIGN;
     a.delta = static_cast<float *>(d_workspace);
-    return hip_status(launch_attention_backward(a, as_stream(stream)));
+    return hip_status(launch_attention_backward(a, h_desc->sums_bytes, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -29,7 +29,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kAttnThreads = 256, kWaveRows = 32, kTileRows = 64;
 constexpr int kOwnRows = kAttnThreads / 64 * kWaveRows;           // 128
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // KS: steps of 16 that a head's dim takes; 32 x 32 blocks, bytes of an LDS row, 16-byte pieces of one, bytes of a tile.
 constexpr int blocks_of(int ks) { return (ks + 1) / 2; }
@@ -193,19 +193,53 @@ __device__ __forceinline__ Sequence sequence_of(const AttnArgs &A, int b)
     return s;
 }
 
-// The workgroup's sequence, head and tile of own rows.  Every XCD gets all sequences of a few heads, as much work as the others; the tiles of a head
-// run backwards, the last queries see the most keys.
-__device__ __forceinline__ bool pick_tile(int heads, int batch, int tiles, int &b, int &head, int &tile)
+// Of a launch's work: a sequence, a head, 128 of its own rows, and a part of what they are multiplied with.
+struct Place {
+    int b, head, tile, part;
+    int64_t slot;                            // of the part's sums
+};
+__device__ __forceinline__ Place place_of(int64_t item, int part, const AttnArgs &A)
 {
-    const int items = batch * heads * tiles, per_xcd = (items + 7) / 8, local = (int)(blockIdx.x >> 3);
+    Place p;
+    const int of_head = (int)(item / A.tiles);
+    p.tile = A.tiles - 1 - (int)(item - (int64_t)of_head * A.tiles);
+    p.head = of_head / A.batch;
+    p.b = of_head - p.head * A.batch;
+    p.part = part;
+    p.slot = item * A.splits + part;
+    return p;
+}
+// The workgroup's.  Every XCD gets all sequences of a few heads, as much work as the others; the tiles of a head run backwards, the last
+// queries see the most keys.
+__device__ __forceinline__ bool pick(const AttnArgs &A, int heads, Place &p)
+{
+    const int items = A.batch * heads * A.tiles * A.splits, per_xcd = (items + 7) / 8, local = (int)(blockIdx.x >> 3);
     if (local >= per_xcd) return false;
-    const int item = (int)(blockIdx.x & 7) * per_xcd + local;
-    if (item >= items) return false;
-    const int of_head = item / tiles;
-    tile = tiles - 1 - (item - of_head * tiles);
-    head = of_head / batch;
-    b = of_head - head * batch;
+    const int n = (int)(blockIdx.x & 7) * per_xcd + local;
+    if (n >= items) return false;
+    p = place_of(n / A.splits, n % A.splits, A);
     return true;
+}
+
+// Where a wave of a workgroup leaves the sums of its 32 rows, as they lie in its registers: part by part, and within a part wave by wave.
+template <int DB>
+__device__ __forceinline__ f32x4 *sums_of(float *parts, int64_t slot, int wave) { return reinterpret_cast<f32x4 *>(parts) + (slot * 4 + wave) * (DB * 256) + (threadIdx.x & 63); }
+template <int DB>
+__device__ __forceinline__ void leave(float *parts, int64_t slot, int wave, const f32x16 (&acc)[DB])
+{
+    f32x4 *to = sums_of<DB>(parts, slot, wave);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) to[(4 * db + g) * 64] = f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
+}
+
+// A part's share of the tiles first .. end: whole tiles of 64, in order.
+__device__ __forceinline__ void share_of(const AttnArgs &A, int part, int &first, int &end)
+{
+    const int tiles = end > first ? (end - first + kTileRows - 1) / kTileRows : 0, each = (tiles + A.splits - 1) / A.splits;
+    first += min(tiles, part * each) * kTileRows;
+    end = min(end, first + each * kTileRows);
 }
 
 // Which keys a query sees: first_key(query) .. end_key(query) - 1, all of them without `causal`; and which queries see a key.
@@ -256,8 +290,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
 {
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
-    int b, head, tile;
-    if (!pick_tile(A.heads, A.batch, A.tiles, b, head, tile)) return;
+    Place at;
+    if (!pick(A, A.heads, at)) return;
+    const int b = at.b, head = at.head, tile = at.tile;
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.q_len) return;
     const Mask M = mask_of(A, seq);
@@ -271,6 +306,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     const Tiles<KS> V(Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim});
     int k_first, k_end;
     key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
+    share_of(A, at.part, k_first, k_end);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
 
     if (k_first < k_end) {
@@ -339,6 +375,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     sum += other_half(sum);
+    if (A.splits > 1) {
+        leave<DB>(A.parts, at.slot, wave, out);
+        if (lane < 32) A.part_stats[(at.slot * 4 + wave) * 32 + lane] = f32x2{top * c, sum};
+        return;
+    }
     const float factor = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;      // a row that sees no key: zero; NaN stays
     store_own<DB>(A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, query, seq.q_len, A.dim, out, factor);
     if (lane < 32 && query < seq.q_len) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : top * A.scale + __logf(sum);
@@ -350,8 +391,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
 {
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];
-    int b, head, tile;
-    if (!pick_tile(A.heads, A.batch, A.tiles, b, head, tile)) return;
+    Place at;
+    if (!pick(A, A.heads, at)) return;
+    const int b = at.b, head = at.head, tile = at.tile;
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.q_len) return;
     const Mask M = mask_of(A, seq);
@@ -367,6 +409,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
     const Rows O = {A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, seq.q_len, A.dim};
     int k_first, k_end;
     key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
+    share_of(A, at.part, k_first, k_end);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
     if (k_first < k_end) {
         K.bring(k_first, lds_at);
@@ -390,7 +433,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
     float lse = 0.f;
     if (query < seq.q_len) {
         lse = A.lse[stat] * kLog2e;
-        if (lane < 32) A.delta[stat] = delta;
+        if (lane < 32 && at.part == 0) A.delta[stat] = delta;
     }
     const Span seen(M.first_key(query), M.end_key(query));
     f32x16 acc[DB];
@@ -432,7 +475,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    store_own<DB>(A.dq + seq.q0 * A.dq_row + head * A.dq_head, A.dq_row, query, seq.q_len, A.dim, acc, A.scale);
+    if (A.splits > 1) leave<DB>(A.parts, at.slot, wave, acc);
+    else store_own<DB>(A.dq + seq.q0 * A.dq_row + head * A.dq_head, A.dq_row, query, seq.q_len, A.dim, acc, A.scale);
 }
 
 // lse, or delta, of the 64 queries of a tile to LDS, by one wave; what is behind the rows as `behind`.
@@ -457,9 +501,9 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide ? kOwnRows * PITCH : 0)];       // Q, dO; two tiles each; V
     __shared__ __attribute__((aligned(16))) float stats[2][2][kTileRows];         // lse, delta
-    int b, kv, tile;
-    if (!pick_tile(A.kv_heads, A.batch, A.tiles, b, kv, tile)) return;
-    tile = A.tiles - 1 - tile;                               // the first keys are seen by the most queries
+    Place at;
+    if (!pick(A, A.kv_heads, at)) return;
+    const int b = at.b, kv = at.head, tile = A.tiles - 1 - at.tile;        // the first keys are seen by the most queries
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.k_len) return;
     const Mask M = mask_of(A, seq);
@@ -491,6 +535,9 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
         q_end = end < q_end ? (int)(end > 0 ? end : 0) : q_end;
     }
     const int tiles = q_end > q_first ? (q_end - q_first + kTileRows - 1) / kTileRows : 0;
+    // a part's share of the tiles of all heads
+    const int all = tiles * A.group, each = (all + A.splits - 1) / A.splits, from = min(all, at.part * each), count = min(all - from, each);
+    int shared = tiles ? from / tiles : 0, t = from - shared * tiles;
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds, stats_at = (unsigned)(size_t)(LDS_AS unsigned char *)stats;
     auto bring_one = [&](Coming &c, int what, int shared, int t, int buffer) {
         const int head = kv * A.group + shared, first = q_first + t * kTileRows;
@@ -504,7 +551,7 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
     };
     if (kWide)
         for (int part = side; part < 2; part += SIDES) Tiles<KS>(V).bring(k_first + part * kTileRows, lds_at + 4 * kTile + part * kTileRows * PITCH);
-    if (tiles > 0) bring(0, 0, 0);
+    if (count > 0) bring(shared, t, 0);
     half8 own[KS], ownv[kWide ? 1 : KS];
     load_own<KS>(K, w_first, own);
     if constexpr (!kWide) load_own<KS>(V, w_first, ownv);
@@ -515,57 +562,60 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
     clear(dv);
     const float c = A.scale * kLog2e;
     int buffer = 0;
-    for (int shared = 0; shared < A.group; ++shared)
-        for (int t = 0; t < tiles; ++t, buffer ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            meet();
-            if (t + 1 < tiles) bring(shared, t + 1, buffer ^ 1);
-            else if (shared + 1 < A.group) bring(shared + 1, 0, buffer ^ 1);
-            const unsigned char *qt = lds + buffer * kTile, *dot = lds + (2 + buffer) * kTile;
+    for (int n = 0; n < count; ++n, buffer ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        meet();
+        const int q0 = q_first + t * kTileRows;
+        if (++t == tiles) {
+            t = 0;
+            ++shared;
+        }
+        if (n + 1 < count) bring(shared, t, buffer ^ 1);
+        const unsigned char *qt = lds + buffer * kTile, *dot = lds + (2 + buffer) * kTile;
 #pragma unroll
-            for (int part = 0; part < 2 / SIDES; ++part) {
-                const int qb = SIDES == 2 ? side : part;
-                const int q1 = q_first + t * kTileRows + 32 * qb;
-                if (q1 >= seq.q_len || w_last < w_first || !M.any(q1, q1 + 31, w_first, w_last)) continue;
-                f32x16 s[1], dp[1];
-                clear(s);
-                clear(dp);
+        for (int part = 0; part < 2 / SIDES; ++part) {
+            const int qb = SIDES == 2 ? side : part;
+            const int q1 = q0 + 32 * qb;
+            if (q1 >= seq.q_len || w_last < w_first || !M.any(q1, q1 + 31, w_first, w_last)) continue;
+            f32x16 s[1], dp[1];
+            clear(s);
+            clear(dp);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
-                    const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
-                    dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
+            for (int ks = 0; ks < KS; ++ks) {
+                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
+                const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
+                dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int at = 32 * qb + 8 * g + 4 * (lane >> 5);
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][at]), delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][at]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 4 * g + e;
+                    s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
+                    dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
                 }
+            }
+            if (!M.all(q1, q1 + 31, w_first, w_last)) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int at = 32 * qb + 8 * g + 4 * (lane >> 5);
-                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][at]), delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][at]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * g + e;
-                        s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
-                        dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const bool on = seen.holds(q1 + acc_row(i));
+                    s[0][i] = on ? s[0][i] : 0.f;
+                    dp[0][i] = on ? dp[0][i] : 0.f;
                 }
-                if (!M.all(q1, q1 + 31, w_first, w_last)) {
+            }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool on = seen.holds(q1 + acc_row(i));
-                        s[0][i] = on ? s[0][i] : 0.f;
-                        dp[0][i] = on ? dp[0][i] : 0.f;
-                    }
-                }
+            for (int step = 0; step < 2; ++step) {
+                const half8 p = to_half8(s[0], 8 * step), ds = to_half8(dp[0], 8 * step);
 #pragma unroll
-                for (int step = 0; step < 2; ++step) {
-                    const half8 p = to_half8(s[0], 8 * step), ds = to_half8(dp[0], 8 * step);
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(dot, 2 * qb + step, db), p, dv[db], 0, 0, 0);
-                        dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(qt, 2 * qb + step, db), ds, dk[db], 0, 0, 0);
-                    }
+                for (int db = 0; db < DB; ++db) {
+                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(dot, 2 * qb + step, db), p, dv[db], 0, 0, 0);
+                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(qt, 2 * qb + step, db), ds, dk[db], 0, 0, 0);
                 }
             }
         }
+    }
     if constexpr (SIDES == 2) {
         // a wave of the first four keeps dK and the one behind it dV: each gets the other's sums of it, kPart blocks of dims at a time
         constexpr int kPart = 4 * kTile / (8 * 4096);
@@ -598,11 +648,72 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
             else take(dk, first);
         }
     }
+    if (A.splits > 1) {                                      // dK's sums, then dV's
+        if (SIDES == 1 || side) leave<DB>(A.parts, 2 * at.slot + 1, wave & 3, dv);
+        if (SIDES == 1 || !side) leave<DB>(A.parts, 2 * at.slot, wave & 3, dk);
+        return;
+    }
     if (SIDES == 1 || side) store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
     if (SIDES == 1 || !side) store_own<DB>(A.dk + seq.k0 * A.dk_row + kv * A.dk_head, A.dk_row, key, seq.k_len, A.dim, dk, A.scale);
 }
 
+// Whole rows from the sums of their parts, added in order: a wave has 32 rows, and 32 dims of them, as the kernel that left them had.
+// Parts of out are weighed by how far their exponents were taken down; one that has seen no key is not read.
 enum { kForward, kDq, kDkv };
+template <int DB, int WHICH>
+__global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs A)
+{
+    constexpr int kTensors = WHICH == kDkv ? 2 : 1;
+    const int rows = (int)(blockIdx.x & 3), db = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, tensor = (int)blockIdx.y;
+    const Place at = place_of(blockIdx.x >> 2, 0, A);
+    const Sequence seq = sequence_of(A, at.b);
+    const int count = WHICH == kDkv ? seq.k_len : seq.q_len, row = (WHICH == kDkv ? A.tiles - 1 - at.tile : at.tile) * kOwnRows + rows * kWaveRows + (lane & 31);
+    if (row >= count) return;
+    f32x16 acc[1];
+    clear(acc);
+    float top = -INFINITY, sum = 0.f;
+    if (WHICH == kForward)
+        for (int part = 0; part < A.splits; ++part) {
+            const f32x2 stat = A.part_stats[((at.slot + part) * 4 + rows) * 32 + (lane & 31)];
+            if (stat[1] != 0.f) top = fmaxf(top, stat[0]);
+        }
+    for (int part = 0; part < A.splits; ++part) {
+        float weight = 1.f;
+        if (WHICH == kForward) {
+            const f32x2 stat = A.part_stats[((at.slot + part) * 4 + rows) * 32 + (lane & 31)];
+            if (stat[1] == 0.f) continue;
+            weight = __builtin_amdgcn_exp2f(stat[0] - top);
+            sum = fmaf(stat[1], weight, sum);
+        }
+        const f32x4 *from = sums_of<DB>(A.parts, (at.slot + part) * kTensors + tensor, rows) + 4 * db * 64;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 x = from[g * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[0][4 * g + e] = fmaf(x[e], weight, acc[0][4 * g + e]);
+        }
+    }
+    _Float16 *to;
+    int64_t stride;
+    float factor = A.scale;
+    if (WHICH == kForward) {
+        to = A.out + seq.q0 * A.out_row + at.head * A.out_head;
+        stride = A.out_row;
+        factor = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+        if (db == 0 && lane < 32) A.lse[(int64_t)at.head * A.q_tokens + seq.q0 + row] = sum == 0.f ? -INFINITY : top * kLn2 + __logf(sum);
+    } else if (WHICH == kDq) {
+        to = A.dq + seq.q0 * A.dq_row + at.head * A.dq_head;
+        stride = A.dq_row;
+    } else if (tensor == 0) {
+        to = A.dk + seq.k0 * A.dk_row + at.head * A.dk_head;
+        stride = A.dk_row;
+    } else {
+        to = A.dv + seq.k0 * A.dv_row + at.head * A.dv_head;
+        stride = A.dv_row;
+        factor = 1.f;
+    }
+    store_own<1>(to + 32 * db, stride, row, count, A.dim - 32 * db, acc, factor);
+}
 
 // The workgroups of dK and dV from which a wave has its keys for itself; below, where the longest workgroup is what the call waits for, two share them.
 // Whole backward pass of heads of 64, one wave / two, us: 256 workgroups, 2048 tokens of 16 heads 98 / 85; 512, two times 2048 of 32 heads 77 / 84;
@@ -611,39 +722,84 @@ enum { kForward, kDq, kDkv };
 constexpr int kOneSideFrom = 512;
 
 template <int KS>
-hipError_t launch_dim(int which, const AttnArgs &a, dim3 grid, hipStream_t s)
+hipError_t launch_dim(int which, const AttnArgs &a, int64_t items, hipStream_t s)
 {
+    constexpr int DB = blocks_of(KS);
+    const dim3 grid((unsigned)(ceil_div(items * a.splits, 8) * 8)), joins((unsigned)(items * 4), which == kDkv ? 2 : 1);
     if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
-    else if (KS <= 4 && (int64_t)a.batch * a.kv_heads * a.tiles >= kOneSideFrom)
+    else if (KS <= 4 && items * a.splits >= kOneSideFrom)
         hipLaunchKernelGGL((attention_dkv_kernel<KS, KS <= 4 ? 1 : 2>), grid, dim3(kAttnThreads), 0, s, a);
     else hipLaunchKernelGGL((attention_dkv_kernel<KS, 2>), grid, dim3(2 * kAttnThreads), 0, s, a);
+    if (a.splits > 1) {
+        if (hipError_t e = hipGetLastError()) return e;
+        if (which == kForward) hipLaunchKernelGGL((attention_join_kernel<DB, kForward>), joins, dim3(DB * 64), 0, s, a);
+        else if (which == kDq) hipLaunchKernelGGL((attention_join_kernel<DB, kDq>), joins, dim3(DB * 64), 0, s, a);
+        else hipLaunchKernelGGL((attention_join_kernel<DB, kDkv>), joins, dim3(DB * 64), 0, s, a);
+    }
     return hipGetLastError();
 }
 
-hipError_t launch(int which, AttnArgs a, int64_t rows, int heads, hipStream_t s)
+int64_t items_of(int which, const AttnArgs &a)
 {
-    a.tiles = (int)ceil_div(rows, kOwnRows);
-    const int64_t items = (int64_t)a.batch * heads * a.tiles;
+    return (int64_t)a.batch * (which == kDkv ? a.kv_heads : a.heads) * ceil_div(which == kDkv ? a.max_k : a.max_q, kOwnRows);
+}
+
+// The parts that a launch of few workgroups splits its keys (or, for dK and dV, queries) into: two workgroups to a compute unit, at least
+// kLeast tiles to a part of an average sequence.
+int splits_of(int which, const AttnArgs &a)
+{
+    constexpr int kMost = 16, kLeast = 4;
+    const int64_t items = items_of(which, a), forced = knob(SAMO_KNOB_ATTENTION_SPLIT, -1);
+    if (items == 0) return 1;
+    if (forced > 0) return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, forced, INT32_MAX / 4 / items}));
+    int64_t others = ceil_div(which == kDkv ? a.q_tokens : a.k_tokens, a.batch);
+    if (a.window) others = std::min<int64_t>(others, a.window + kOwnRows);
+    const int64_t tiles = ceil_div(others, kTileRows) * (which == kDkv ? a.group : 1);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, 2 * compute_units() / items, tiles / kLeast}));
+}
+
+int blocks_of_dim(int dim) { return dim <= 32 ? 1 : dim <= 64 ? 2 : dim <= 96 ? 3 : 4; }
+
+// Bytes of the sums that a launch leaves: 128 rows of fp32 a part, and the softmax's two numbers a row.
+int64_t sums_bytes(int which, const AttnArgs &a, int splits)
+{
+    if (splits <= 1) return 0;
+    const int64_t slots = items_of(which, a) * splits;
+    return slots * kOwnRows * (which == kForward ? 32 * 4 * blocks_of_dim(a.dim) + 8 : (which == kDkv ? 2 : 1) * 32 * 4 * blocks_of_dim(a.dim));
+}
+
+hipError_t launch(int which, AttnArgs a, size_t bytes, hipStream_t s)
+{
+    a.tiles = (int)ceil_div(which == kDkv ? a.max_k : a.max_q, kOwnRows);
+    const int64_t items = items_of(which, a);
     if (items == 0) return hipSuccess;
-    const dim3 grid((unsigned)(ceil_div(items, 8) * 8));
+    a.splits = splits_of(which, a);
+    if (!a.parts || (size_t)sums_bytes(which, a, a.splits) > bytes) a.splits = 1;
+    a.part_stats = reinterpret_cast<f32x2 *>(a.parts + items * a.splits * kOwnRows * 32 * blocks_of_dim(a.dim));
     switch ((a.dim + 15) / 16) {                             // padded: a kernel for each of the sizes in use, and the next one up for the others
-    case 1: case 2: return launch_dim<2>(which, a, grid, s);
-    case 3: case 4: return launch_dim<4>(which, a, grid, s);
-    case 5: return launch_dim<5>(which, a, grid, s);
-    case 6: return launch_dim<6>(which, a, grid, s);
-    default: return launch_dim<8>(which, a, grid, s);
+    case 1: case 2: return launch_dim<2>(which, a, items, s);
+    case 3: case 4: return launch_dim<4>(which, a, items, s);
+    case 5: return launch_dim<5>(which, a, items, s);
+    case 6: return launch_dim<6>(which, a, items, s);
+    default: return launch_dim<8>(which, a, items, s);
     }
 }
 
 }  // namespace
 
-hipError_t launch_attention(const AttnArgs &a, hipStream_t s) { return launch(kForward, a, a.max_q, a.heads, s); }
-
-hipError_t launch_attention_backward(const AttnArgs &a, hipStream_t s)
+int64_t attention_sums_bytes(const AttnArgs &a, bool backward)
 {
-    if (hipError_t e = launch(kDq, a, a.max_q, a.heads, s)) return e;       // delta first: the other kernel reads it
-    return launch(kDkv, a, a.max_k, a.kv_heads, s);
+    if (!backward) return sums_bytes(kForward, a, splits_of(kForward, a));
+    return std::max(sums_bytes(kDq, a, splits_of(kDq, a)), sums_bytes(kDkv, a, splits_of(kDkv, a)));
+}
+
+hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s) { return launch(kForward, a, bytes, s); }
+
+hipError_t launch_attention_backward(const AttnArgs &a, size_t bytes, hipStream_t s)
+{
+    if (hipError_t e = launch(kDq, a, bytes, s)) return e;   // delta first: the other kernel reads it
+    return launch(kDkv, a, bytes, s);
 }
 
 }  // namespace samo

@@ -243,6 +243,7 @@ hipError_t launch_step8(const Step8Launch &ls, bool dense, const Step8Args &a, h
 hipError_t launch_state8(const Step8Launch &ls, bool pack, hipStream_t s);
 
 // Attention (attention.hip): tensors of tokens x heads x dim, a row's elements adjacent, strides in elements.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 struct AttnArgs {
     const _Float16 *q, *k, *v, *dout;
     _Float16 *out, *dq, *dk, *dv;
@@ -251,11 +252,15 @@ struct AttnArgs {
     const int32_t *q_start, *k_start;       // batch + 1 each, NULL: one sequence of all tokens
     int64_t q_tokens, k_tokens;
     int batch, heads, kv_heads, group, dim, max_q, max_k, causal, window;
-    int tiles;                              // of own rows a head, set by the launch
+    int tiles, splits;                      // of own rows a head, and parts of what they are multiplied with; set by the launch
     float scale;
+    float *parts;                           // NULL: a launch is not split
+    f32x2 *part_stats;
 };
-hipError_t launch_attention(const AttnArgs &a, hipStream_t s);
-hipError_t launch_attention_backward(const AttnArgs &a, hipStream_t s);
+// Bytes that a call can use at `parts`; with less a launch that would need them is not split.
+int64_t attention_sums_bytes(const AttnArgs &a, bool backward);
+hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s);
+hipError_t launch_attention_backward(const AttnArgs &a, size_t bytes, hipStream_t s);
 
 // The gated feed-forward block (glu.hip).
 struct GluArgs {

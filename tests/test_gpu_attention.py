@@ -152,6 +152,58 @@ def test_many_workgroups(dim, causal, window):
     check(lens, [n + 3 * i for i, n in enumerate(lens)], 16, 16, dim, causal, window, slack=230, seed=dim)
 
 
+@pytest.fixture
+def parts(request):
+    samo.samo_debug_set(samo.KNOB_ATTENTION_SPLIT, request.param)
+    yield request.param
+    samo.samo_debug_set(samo.KNOB_ATTENTION_SPLIT)
+
+
+@pytest.mark.parametrize("parts", [1, 2, 3, 7, 16], indirect=True)
+@pytest.mark.parametrize("dim", [32, 64, 72, 96, 128])
+def test_keys_and_queries_in_parts(parts, dim):
+    """Parts of one tile and of many, parts that hold nothing, sequences without any; the sums are fp32 whatever their order: the same bounds."""
+    check([0, 1, 130, 300, 64], [7, 400, 131, 290, 0], 4, 2, dim, True, 0, seed=dim, slack=60)
+    check([200, 70], [90, 515], 3, 1, dim, False, 0, seed=dim + 1)
+    check([450, 20], [450, 20], 2, 2, dim, True, 70, seed=dim + 2)
+
+
+@pytest.mark.parametrize("parts", [4], indirect=True)
+def test_parts_of_large_scores(parts):
+    """A part's exponents are taken against its own largest score: parts hundreds apart, either way round."""
+    check([300], [300], 2, 2, 64, True, 0, std=6.0)
+
+    def steps(sign):
+        def fix(q, k, v, do):
+            k.mul_((1 + sign * torch.arange(k.shape[0], device=DEV)[:, None, None].div(128).floor()).half())
+        return fix
+    check([64], [512], 1, 1, 64, False, 0, fix=steps(1.0))
+    check([64], [512], 1, 1, 64, False, 0, fix=steps(-0.25))
+
+
+@pytest.mark.parametrize("context", [1, 63, 1000, 9001])
+def test_one_token_behind_a_context(context):
+    """The form of generation: one query a sequence, split as the sizes make it."""
+    check([1, 1, 1], [context, 5, max(1, context // 2)], 8, 2, 64, True, 0, seed=context)
+    check([1], [context], 4, 4, 128, True, 300, seed=context)
+
+
+def test_parts_where_there_is_no_memory_for_them():
+    """An empty workspace: the forward pass by single workgroups; one of delta alone: the backward pass."""
+    q, k, v, do = (torch.randn(2000, 2, 64, device=DEV).half() for _ in range(4))
+    res = []
+    for room in (None, 0, 4 * 2 * 2000):
+        o, dq, dk, dv = (torch.full_like(q, float("nan")) for _ in range(4))
+        lse = torch.zeros(2, 2000, device=DEV)
+        ws = None if room is None else torch.empty(room, dtype=torch.uint8, device=DEV)
+        samo.samo_attention(q, k, v, o, lse, workspace=ws)
+        samo.samo_attention_backward(do, q, k, v, o, lse, dq, dk, dv, workspace=ws if room else None)
+        res.append((o, dq, dk, dv))
+    assert all(torch.equal(a, b) for a, b in zip(res[1][:1], res[2][:1]))
+    for a, b in zip(res[0], res[2]):
+        assert float((a.float() - b.float()).norm() / b.float().norm()) < 1e-2
+
+
 def test_large_scores_and_small_gradients():
     """Scores of hundreds (one key takes all of a row), rows whose largest score comes last, gradients among fp16's small numbers."""
     check([300], [300], 2, 2, 64, True, 0, std=6.0)
