@@ -225,8 +225,9 @@ __device__ __forceinline__ bool pick(const AttnArgs &A, int heads, Place &p)
 template <int DB>
 __device__ __forceinline__ f32x4 *sums_of(float *parts, int64_t slot, int wave) { return reinterpret_cast<f32x4 *>(parts) + (slot * 4 + wave) * (DB * 256) + (threadIdx.x & 63); }
 template <int DB>
-__device__ __forceinline__ void leave(float *parts, int64_t slot, int wave, const f32x16 (&acc)[DB])
+__device__ __forceinline__ void leave(float *parts, int64_t slot, int wave, int row, int count, const f32x16 (&acc)[DB])
 {
+    if (row >= count) return;
     f32x4 *to = sums_of<DB>(parts, slot, wave);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -376,7 +377,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     sum += other_half(sum);
     if (A.splits > 1) {
-        leave<DB>(A.parts, at.slot, wave, out);
+        leave<DB>(A.parts, at.slot, wave, query, seq.q_len, out);
         if (lane < 32) A.part_stats[(at.slot * 4 + wave) * 32 + lane] = f32x2{top * c, sum};
         return;
     }
@@ -475,7 +476,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (A.splits > 1) leave<DB>(A.parts, at.slot, wave, acc);
+    if (A.splits > 1) leave<DB>(A.parts, at.slot, wave, query, seq.q_len, acc);
     else store_own<DB>(A.dq + seq.q0 * A.dq_row + head * A.dq_head, A.dq_row, query, seq.q_len, A.dim, acc, A.scale);
 }
 
@@ -649,8 +650,8 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
         }
     }
     if (A.splits > 1) {                                      // dK's sums, then dV's
-        if (SIDES == 1 || side) leave<DB>(A.parts, 2 * at.slot + 1, wave & 3, dv);
-        if (SIDES == 1 || !side) leave<DB>(A.parts, 2 * at.slot, wave & 3, dk);
+        if (SIDES == 1 || side) leave<DB>(A.parts, 2 * at.slot + 1, wave & 3, key, seq.k_len, dv);
+        if (SIDES == 1 || !side) leave<DB>(A.parts, 2 * at.slot, wave & 3, key, seq.k_len, dk);
         return;
     }
     if (SIDES == 1 || side) store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
@@ -745,20 +746,6 @@ int64_t items_of(int which, const AttnArgs &a)
     return (int64_t)a.batch * (which == kDkv ? a.kv_heads : a.heads) * ceil_div(which == kDkv ? a.max_k : a.max_q, kOwnRows);
 }
 
-// The parts that a launch of few workgroups splits its keys (or, for dK and dV, queries) into: two workgroups to a compute unit, at least
-// kLeast tiles to a part of an average sequence.
-int splits_of(int which, const AttnArgs &a)
-{
-    constexpr int kMost = 16, kLeast = 4;
-    const int64_t items = items_of(which, a), forced = knob(SAMO_KNOB_ATTENTION_SPLIT, -1);
-    if (items == 0) return 1;
-    if (forced > 0) return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, forced, INT32_MAX / 4 / items}));
-    int64_t others = ceil_div(which == kDkv ? a.q_tokens : a.k_tokens, a.batch);
-    if (a.window) others = std::min<int64_t>(others, a.window + kOwnRows);
-    const int64_t tiles = ceil_div(others, kTileRows) * (which == kDkv ? a.group : 1);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, 2 * compute_units() / items, tiles / kLeast}));
-}
-
 int blocks_of_dim(int dim) { return dim <= 32 ? 1 : dim <= 64 ? 2 : dim <= 96 ? 3 : 4; }
 
 // Bytes of the sums that a launch leaves: 128 rows of fp32 a part, and the softmax's two numbers a row.
@@ -767,6 +754,51 @@ int64_t sums_bytes(int which, const AttnArgs &a, int splits)
     if (splits <= 1) return 0;
     const int64_t slots = items_of(which, a) * splits;
     return slots * kOwnRows * (which == kForward ? 32 * 4 * blocks_of_dim(a.dim) + 8 : (which == kDkv ? 2 : 1) * 32 * 4 * blocks_of_dim(a.dim));
+}
+
+// What a launch costs with its keys (for dK and dV: queries) in so many parts, us.  A workgroup works through tiles of 64; the device's share of all of them,
+// and as the launch ends half the longest workgroup besides; the longest one by itself; and for parts a second kernel and the sums, written and read.
+// A tile by itself takes 1.25 us with heads of 64 and 1.5 with 128, 1.4 and 2.3 where two workgroups share a compute unit; the backward pass's
+// a quarter more.  Measured against the parts taken, whole calls, us: one token behind 8192, 32 heads of 128, 180 with one part, 39 with 8; 2000 tokens
+// in 3 sequences behind 3000 each, 16 heads of 64, 80 and 60 with three; 4096 tokens, 8 heads of 128, 87 and 60 with three; 1024 tokens of
+// 16 heads of 96 24 and 26 with two; 2048 in 4 sequences, 16 heads of 64, 13 and 24 with two.
+double launch_us(int which, const AttnArgs &a, int64_t items, int splits)
+{
+    const bool dkv = which == kDkv, one_side = dkv && a.dim <= 64 && items * splits >= kOneSideFrom;
+    const double q = (double)a.q_tokens / a.batch, k = (double)a.k_tokens / a.batch;
+    double longest = dkv ? q : k, mean = 1.0;
+    if (a.window) longest = std::min(longest, (double)a.window + kOwnRows);
+    else if (a.causal) mean = 1.0 - 0.5 * std::min(1.0, q / std::max(k, 1.0));
+    longest = std::ceil(longest / kTileRows) * (dkv ? a.group : 1);
+    const double own = std::min((double)items, (double)(dkv ? a.kv_heads : a.heads) * ((double)(dkv ? a.k_tokens : a.q_tokens) / kOwnRows + a.batch));
+    const double alone = (1.0 + 0.004 * a.dim) * (which == kForward ? 1.0 : 1.25), shared = (0.57 + 0.0133 * a.dim) * (which == kForward ? 1.0 : 1.25);
+    const double all = own * longest * mean / compute_units() * (dkv && !one_side ? alone : shared / 2);
+    const double part = alone * std::ceil(longest / splits);
+    const double us = std::max(part, all + part / 2);
+    return splits > 1 ? us + 5.0 + (double)sums_bytes(which, a, splits) * 2 / 5e6 : us;
+}
+
+// The parts a launch is split into.
+int splits_of(int which, const AttnArgs &a)
+{
+    constexpr int kMost = 16, kSlots = 2048;
+    const int64_t items = items_of(which, a), forced = knob(SAMO_KNOB_ATTENTION_SPLIT, -1);
+    if (items == 0) return 1;
+    if (forced > 0) return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, forced, INT32_MAX / 4 / items}));
+    // Two rounds of the device are even enough: the longest workgroups come first (8192 tokens, 32 heads of 128, 8 of keys: dK and dV 1350 us as they are, 1550
+    // in two parts; forward 597 and 674).
+    if (items >= (which == kDkv && a.dim > 64 ? 2 : 4) * compute_units()) return 1;
+    int best = 1;
+    double least = launch_us(which, a, items, 1);
+    if (least < 12.0) return 1;                              // two parts take six of them, and five for the second kernel
+    for (int splits = 2; splits <= kMost && items * splits <= kSlots; ++splits) {
+        const double us = launch_us(which, a, items, splits);
+        if (us < least) {
+            least = us;
+            best = splits;
+        }
+    }
+    return best;
 }
 
 hipError_t launch(int which, AttnArgs a, size_t bytes, hipStream_t s)
