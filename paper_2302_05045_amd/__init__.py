@@ -1092,14 +1092,25 @@ def _heads(t: torch.Tensor, name: str, shape: Optional[tuple] = None) -> Heads:
     return Heads(t.data_ptr() if t.numel() else None, row if t.shape[0] > 1 else 0, head if t.shape[1] > 1 else 0)
 
 
+_HEADS_AT = {name: getattr(AttentionDesc, name).offset for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")}
+
+
+def _set_heads(d: AttentionDesc, name: str, t: torch.Tensor, tokens: int = -1, heads: int = -1, dim: int = -1) -> None:
+    """Field `name` of d from a tensor of that name and shape (any, if tokens is -1), in native code where it is built."""
+    if _marshal is None or not _marshal.heads(ctypes.addressof(d) + _HEADS_AT[name], t, tokens, heads, dim):
+        setattr(d, name, _heads(t, name, None if tokens < 0 else (tokens, heads, dim)))
+
+
 def _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k) -> AttentionDesc:
     d = AttentionDesc()
-    d.q, d.k = _heads(q, "q"), _heads(k, "k")
+    _set_heads(d, "q", q)
+    _set_heads(d, "k", k)
     q_tokens, heads, dim = q.shape
     k_tokens, kv_heads, k_dim = k.shape
     if k_dim != dim:
         raise ValueError("q has heads of %d, k of %d" % (dim, k_dim))
-    d.v, d.out = _heads(v, "v", tuple(k.shape)), _heads(out, "out", tuple(q.shape))
+    _set_heads(d, "v", v, k_tokens, kv_heads, dim)
+    _set_heads(d, "out", out, q_tokens, heads, dim)
     if not isinstance(lse, torch.Tensor) or not lse.is_cuda or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise TypeError("lse must be a contiguous float32 tensor on the GPU")
     if tuple(lse.shape) != (heads, q_tokens):
@@ -1161,9 +1172,12 @@ def samo_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor
     workspace (uint8, 4 * heads * tokens bytes; more, from the next multiple of 16, for the sums of calls of few heads and rows) is in use until the
     stream has passed the call; without one the call takes it from torch's allocator."""
     d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)
-    d.dout, d.dq = _heads(dout, "dout", tuple(q.shape)), _heads(dq, "dq", tuple(q.shape))
-    d.dk, d.dv = _heads(dk, "dk", tuple(k.shape)), _heads(dv, "dv", tuple(k.shape))
-    workspace = _attention_sums(d, True, workspace, 4 * q.shape[0] * q.shape[1])
+    like_q, like_k = (d.q_tokens, d.heads, d.dim), (d.k_tokens, d.kv_heads, d.dim)
+    _set_heads(d, "dout", dout, *like_q)
+    _set_heads(d, "dq", dq, *like_q)
+    _set_heads(d, "dk", dk, *like_k)
+    _set_heads(d, "dv", dv, *like_k)
+    workspace = _attention_sums(d, True, workspace, 4 * d.q_tokens * d.heads)
     _check(lib().samo_attention_backward(ctypes.byref(d), _dev(workspace, torch.uint8, "workspace"),
                                          workspace.numel() if workspace is not None else 0, _stream()),
            "samo_attention_backward")

@@ -1,7 +1,7 @@
 // Argument marshalling of the Python binding in native code: a tensor argument's checks and its device
 // pointer in one call.  In Python the same checks are eight attribute reads, about 1 us per tensor, and an
 // entry point takes up to seven tensors: more host time than the kernel of a small layer runs.
-// Nothing but reads of tensor metadata happens in vector() and matrix().  Whatever is not a plain torch.Tensor or Parameter
+// Nothing but reads of tensor metadata happens in vector(), matrix() and heads().  Whatever is not a plain torch.Tensor or Parameter
 // (subclasses may override attributes, other objects have to be refused) goes to the Python function that makes the
 // same checks, given once by use().
 //
@@ -76,6 +76,30 @@ PyObject *matrix(PyObject *, PyObject *const *args, Py_ssize_t count)
     PyObject *pointer = pointer_or_none(t);
     if (!pointer) return nullptr;
     return Py_BuildValue("NLL", pointer, (long long)t.size(0), (long long)t.size(1));
+    END_HANDLE_TH_ERRORS
+}
+
+// heads(address, tensor, tokens, heads, dim): writes the samo_heads of a (tokens, heads, dim) float16 GPU tensor whose last dimension is
+// contiguous to the address (a field of a descriptor that the caller holds) and returns True; tokens -1: of any shape.  False, and nothing
+// written, for everything else: the Python function that makes the same checks says what is wrong with it.
+PyObject *heads(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    HANDLE_TH_ERRORS
+    if (count != 5) {
+        PyErr_SetString(PyExc_TypeError, "heads(address, tensor, tokens, heads, dim)");
+        return nullptr;
+    }
+    if (!THPVariable_CheckExact(args[1])) Py_RETURN_FALSE;
+    samo_heads *to = static_cast<samo_heads *>(PyLong_AsVoidPtr(args[0]));
+    const long long want[3] = {PyLong_AsLongLong(args[2]), PyLong_AsLongLong(args[3]), PyLong_AsLongLong(args[4])};
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(args[1]);
+    if (!to || !t.is_cuda() || t.scalar_type() != at::kHalf || t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1)) Py_RETURN_FALSE;
+    if (want[0] >= 0 && (t.size(0) != want[0] || t.size(1) != want[1] || t.size(2) != want[2])) Py_RETURN_FALSE;
+    to->d_data = t.numel() ? t.data_ptr() : nullptr;
+    to->row = t.size(0) > 1 ? t.stride(0) : 0;
+    to->head = t.size(1) > 1 ? t.stride(1) : 0;
+    Py_RETURN_TRUE;
     END_HANDLE_TH_ERRORS
 }
 
@@ -261,6 +285,7 @@ PyObject *use(PyObject *, PyObject *const *args, Py_ssize_t count)
 PyMethodDef methods[] = {
     {"vector", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(vector)), METH_FASTCALL, nullptr},
     {"matrix", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(matrix)), METH_FASTCALL, nullptr},
+    {"heads", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(heads)), METH_FASTCALL, nullptr},
     {"build_indices", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(build_indices)), METH_FASTCALL, nullptr},
     {"use", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(use)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

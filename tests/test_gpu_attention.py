@@ -307,3 +307,25 @@ def test_rows_past_two_gibibytes():
     samo.samo_attention(q, k, v, a, lse)
     samo.samo_attention(q, kk, vv, b, lse)
     assert torch.equal(a, b)
+
+
+def test_native_and_python_descriptors_agree():
+    """The descriptor's fields of a tensor, written by native code and in Python, and the refusals of both."""
+    import ctypes
+    whole = torch.zeros(6, 5, 16, device=DEV).half()
+    kinds = [whole, whole[:, :, :8], whole[:, 1:3], whole.transpose(0, 1), whole[:1], whole[:, :1], whole[:0], torch.nn.Parameter(whole), whole.float(),
+             whole[0], whole[:, :, ::2], whole.cpu(), None, [1]]
+    for t in kinds:
+        for shape in ((-1, -1, -1), (6, 5, 16), (1, 5, 16)):
+            made = samo.AttentionDesc()
+            made.q.row = 77
+            done = samo._marshal.heads(ctypes.addressof(made) + samo._HEADS_AT["q"], t, *shape)
+            try:
+                want = samo._heads(t, "q", None if shape[0] < 0 else shape)
+            except (TypeError, ValueError):
+                assert not done and made.q.row == 77
+                continue
+            if done:
+                assert (made.q.d_data, made.q.row, made.q.head) == (want.d_data, want.row, want.head)
+            samo._set_heads(made, "q", t, *shape)
+            assert (made.q.d_data, made.q.row, made.q.head) == (want.d_data, want.row, want.head)
