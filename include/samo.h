@@ -46,7 +46,8 @@
  *   - Sizes: 0 <= N <= 2^31 - 1 per layer (the index is 32-bit, Section III-B);
  *     0 <= nnz <= N.  N = 0 and nnz = 0 are valid and do nothing / zero-fill;
  *     pointers to arrays of nnz elements may be NULL when nnz == 0.
- *   - Alignment: every array pointer must be 16-byte aligned (SAMO_ERR_ALIGN).
+ *   - Alignment: every array pointer must be 16-byte aligned (SAMO_ERR_ALIGN); s8 2-byte, attention's lse and
+ *     starts 4-byte.
  *   - Preconditions NOT checked on the hot path (results undefined if violated;
  *     samo_validate_index checks them): idx strictly ascending, 0 <= idx[i] < N,
  *     seg_ptr consistent with idx.  Strictly ascending indices make scatter
