@@ -15,7 +15,7 @@
 //    So P and dS go from one product to the next without leaving the registers.
 //  - A tile's LDS rows are 128 or 256 bytes; 16-byte piece c of row r lies at c ^ swizzle(r), which spreads both kinds of read, 16
 //    rows by one piece and 4 rows by 64 bytes, over all banks.
-//  - Workgroups are dealt to the 8 XCDs in contiguous runs, a head's workgroups together: they share its other side in one L2.
+//  - Workgroups of a head go to one of the 8 XCDs, where they share its other side in the L2 (pick()).
 // P and dS are rounded to fp16 for the products they enter, as Q, K, V and dO are: 2^-11 of themselves; statistics and all sums are fp32.
 // dQ and dK, dV are formed by two kernels, each of which forms S and dP: 7 products for the 5 that one kernel would need, but every
 // sum has one owner and one order, so the same call gives the same bits (with additions to dQ in memory it would not).
@@ -198,26 +198,23 @@ struct Place {
     int b, head, tile, part;
     int64_t slot;                            // of the part's sums
 };
-__device__ __forceinline__ Place place_of(int64_t item, int part, const AttnArgs &A)
+__device__ __forceinline__ Place place_of(int of_head, int tile, int part, const AttnArgs &A)
 {
-    Place p;
-    const int of_head = (int)(item / A.tiles);
-    p.tile = A.tiles - 1 - (int)(item - (int64_t)of_head * A.tiles);
-    p.head = of_head / A.batch;
-    p.b = of_head - p.head * A.batch;
-    p.part = part;
-    p.slot = item * A.splits + part;
-    return p;
+    const int head = of_head / A.batch;
+    return {of_head - head * A.batch, head, tile, part, ((int64_t)of_head * A.tiles + tile) * A.splits + part};
 }
-// The workgroup's.  Every XCD gets all sequences of a few heads, as much work as the others; the tiles of a head run backwards, the last
-// queries see the most keys.
+// The workgroup's place.  The tiles that see the most go first, of all heads and sequences, so that a launch ends with short workgroups.  An XCD gets
+// the same heads of every tile, whose other side stays in its L2, or, where few heads and sequences do not divide evenly among
+// the XCDs, what comes next.  All tiles of a head together / this, us, forward and backward: 8192 causal tokens in 4
+// sequences, 32 heads of 64, 117 and 378 / 91 and 303; of 80 184 and 555 / 151 and 493; in one sequence, 32 heads of 128 on 8, 600 and 2035 / 576 and 1934.
+__device__ __host__ inline int heads_an_xcd(int all) { return all % 8 == 0 || all >= 64 ? (all + 7) / 8 : 0; }       // 0: what comes next
 __device__ __forceinline__ bool pick(const AttnArgs &A, int heads, Place &p)
 {
-    const int items = A.batch * heads * A.tiles * A.splits, per_xcd = (items + 7) / 8, local = (int)(blockIdx.x >> 3);
-    if (local >= per_xcd) return false;
-    const int n = (int)(blockIdx.x & 7) * per_xcd + local;
-    if (n >= items) return false;
-    p = place_of(n / A.splits, n % A.splits, A);
+    const int all = A.batch * heads, share = heads_an_xcd(all), xcd = (int)(blockIdx.x & 7), local = (int)(blockIdx.x >> 3) / A.splits;
+    const int n = share ? 0 : local * 8 + xcd, turn = share ? local / share : n / all;
+    const int of_head = share ? xcd * share + local - turn * share : n - turn * all;
+    if (turn >= A.tiles || of_head >= all) return false;
+    p = place_of(of_head, A.tiles - 1 - turn, (int)(blockIdx.x >> 3) % A.splits, A);
     return true;
 }
 
@@ -670,7 +667,8 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
 {
     constexpr int kTensors = WHICH == kDkv ? 2 : 1;
     const int rows = (int)(blockIdx.x & 3), db = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, tensor = (int)blockIdx.y;
-    const Place at = place_of(blockIdx.x >> 2, 0, A);
+    const int item = (int)(blockIdx.x >> 2);
+    const Place at = place_of(item / A.tiles, item % A.tiles, 0, A);
     const Sequence seq = sequence_of(A, at.b);
     const int count = WHICH == kDkv ? seq.k_len : seq.q_len, row = (WHICH == kDkv ? A.tiles - 1 - at.tile : at.tile) * kOwnRows + rows * kWaveRows + (lane & 31);
     if (row >= count) return;
@@ -730,7 +728,10 @@ template <int KS>
 hipError_t launch_dim(int which, const AttnArgs &a, int64_t items, hipStream_t s)
 {
     constexpr int DB = blocks_of(KS);
-    const dim3 grid((unsigned)(ceil_div(items * a.splits, 8) * 8)), joins((unsigned)(items * 4), which == kDkv ? 2 : 1);
+    // as pick() deals them
+    const int share = heads_an_xcd((int)(items / a.tiles));
+    const int64_t places = share ? (int64_t)share * a.tiles : ceil_div(items, 8);
+    const dim3 grid((unsigned)(places * a.splits * 8)), joins((unsigned)(items * 4), which == kDkv ? 2 : 1);
     if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (KS <= 4 && items * a.splits >= kOneSideFrom)
@@ -763,9 +764,11 @@ int64_t sums_bytes(int which, const AttnArgs &a, int splits)
 // What a launch costs with its keys (for dK and dV: queries) in so many parts, us.  A workgroup works through tiles of 64; the device's share of all of them,
 // and as the launch ends half the longest workgroup besides; the longest one by itself; and for parts a second kernel and the sums, written and read.
 // A tile by itself takes 1.25 us with heads of 64 and 1.5 with 128, 1.4 and 2.3 where two workgroups share a compute unit; the backward pass's
-// a quarter more.  Measured against the parts taken, whole calls, us: one token behind 8192, 32 heads of 128, 180 with one part, 39 with 8; 2000 tokens
-// in 3 sequences behind 3000 each, 16 heads of 64, 80 and 60 with three; 4096 tokens, 8 heads of 128, 87 and 60 with three; 1024 tokens of
-// 16 heads of 96 24 and 26 with two; 2048 in 4 sequences, 16 heads of 64, 13 and 24 with two.
+// a quarter more.  Measured against the parts taken, whole calls, us: one token behind 8192, 32 heads of 128, 180 with one part, 38 with 8, 34 with 16; 2000 tokens
+// in 3 sequences behind 3000 each, 16 heads of 64, 71 and 57 with three; 4096 tokens, 8 heads of 128, 89 and 60 with three; 1024 tokens of
+// 16 heads of 96 24 and 26 with two; 2048 in 4 sequences, 16 heads of 64, 13 and 24 with two; one token each behind 8 contexts of 2048, 32 heads of
+// 128, 54 and 36 with two.
+// Where every workgroup has as much to do, the rounds that they take count whole.
 double launch_us(int which, const AttnArgs &a, int64_t items, int splits)
 {
     const bool dkv = which == kDkv, one_side = dkv && a.dim <= 64 && items * splits >= kOneSideFrom;
@@ -776,10 +779,13 @@ double launch_us(int which, const AttnArgs &a, int64_t items, int splits)
     longest = std::ceil(longest / kTileRows) * (dkv ? a.group : 1);
     const double own = std::min((double)items, (double)(dkv ? a.kv_heads : a.heads) * ((double)(dkv ? a.k_tokens : a.q_tokens) / kOwnRows + a.batch));
     const double alone = (1.0 + 0.004 * a.dim) * (which == kForward ? 1.0 : 1.25), shared = (0.57 + 0.0133 * a.dim) * (which == kForward ? 1.0 : 1.25);
+    const double rows = std::min(1.0, (double)(dkv ? a.max_k : a.max_q) / kOwnRows);
     const double all = own * longest * mean / compute_units() * (dkv && !one_side ? alone : shared / 2);
-    const double part = alone * std::ceil(longest / splits);
-    const double us = std::max(part, all + part / 2);
-    return splits > 1 ? us + 5.0 + (double)sums_bytes(which, a, splits) * 2 / 5e6 : us;
+    const double part = std::ceil(longest / splits), slots = compute_units() * (dkv && !one_side ? 1.0 : 2.0);
+    double us = std::max(alone * part, all + alone * part / 2);
+    if (mean > 0.95)                                         // workgroups alike: whole rounds of them
+        us = std::ceil(own * splits / slots) * part * ((dkv && !one_side) || own * splits <= compute_units() ? alone : shared);
+    return splits > 1 ? us + 4.5 + 0.5 * splits + (double)sums_bytes(which, a, splits) * rows * 2 / 5e6 : us;
 }
 
 // The parts a launch is split into.
@@ -789,7 +795,7 @@ int splits_of(int which, const AttnArgs &a)
     const int64_t items = items_of(which, a), forced = knob(SAMO_KNOB_ATTENTION_SPLIT, -1);
     if (items == 0) return 1;
     if (forced > 0) return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, forced, INT32_MAX / 4 / items}));
-    // Two rounds of the device are even enough: the longest workgroups come first (8192 tokens, 32 heads of 128, 8 of keys: dK and dV 1350 us as they are, 1550
+    // Two rounds of the device are even enough: the longest workgroups come first (8192 tokens, 32 heads of 128, 8 of keys: dK and dV 1350 us as they are, 1500
     // in two parts; forward 597 and 674).
     if (items >= (which == kDkv && a.dim > 64 ? 2 : 4) * compute_units()) return 1;
     int best = 1;
