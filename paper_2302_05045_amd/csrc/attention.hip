@@ -283,9 +283,9 @@ __device__ __forceinline__ void key_range(const Mask &M, int q0, int q1, int k_l
 }
 
 // The forward pass.  Four waves of 32 queries: with two tiles of keys and values in LDS two workgroups fit a compute unit up to heads of 128, which is
-// what covers the copies' latency and the softmax of one by the products of the other.  8192 causal tokens, 32 heads of 128 on 8: 597 us,
-// 920 TFLOP/s, bound by the chip's power (zeros: 1240); two sequences of 4096, not causal, 940; 4 x 2048 causal, 32 heads of 80:
-// 185 us, 455 (a sixth of the products is padding to 96, a quarter lies behind the diagonal).
+// what covers the copies' latency and the softmax of one by the products of the other.  8192 causal tokens, 32 heads of 128 on 8: 590 us,
+// 930 TFLOP/s, bound by the chip's power (zeros: 1240); two sequences of 4096, not causal, 950; 4 x 2048 causal, 32 heads of 80:
+// 159 us, 540 (80 is padded to 96 in the second product; 17 tiles a workgroup pay for its start and for what lies behind the diagonal in two).
 template <int KS>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnArgs A)
 {
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     if (lane < 32 && query < seq.q_len) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : top * A.scale + __logf(sum);
 }
 
-// dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 850 us, 970 TFLOP/s; 4 x 2048, 32 heads of 80: 230 us.
+// dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 840 us, 980 TFLOP/s; 4 x 2048, 32 heads of 80: 200 us.
 template <int KS>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const AttnArgs A)
 {
@@ -493,7 +493,7 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 // have the same keys, one takes the first 32 queries of every tile and the other the last, and their sums meet in LDS at the end: a workgroup's time
 // counts as much as the device's, under a causal mask the first keys are seen by every query (8192 tokens, 32 heads of 128, 8 of keys: with
 // four waves the longest of 512 workgroups took 1.8 ms by itself; the whole backward pass 2414 -> 2090 us).
-// Four products a tile: 1300 us for those 8192 tokens, 845 TFLOP/s; 4 x 2048, 32 heads of 80: 340 us.
+// Four products a tile: 1300 us for those 8192 tokens, 845 TFLOP/s; 4 x 2048, 32 heads of 80: 330 us.
 // Two waves to a SIMD have 256 registers each.  Heads of more than 96 fill half of them with their sums: there the rows of V stay in LDS, from where
 // they are read for every block.
 template <int KS, int SIDES>
