@@ -171,3 +171,26 @@ def test_m0_is_touched_only_by_the_copies_into_lds(tmp_path, source):
         assert re.fullmatch(r"s_mov_b32 m0, s\d+", code[i]), code[i]
         assert code[i + 1] == "s_nop 0" and re.match(r"global_load_lds_dword(x4)? ", code[i + 2]), code[i:i + 3]
     assert sum(ln.startswith("global_load_lds_") for ln in code) == len(uses)
+
+
+def test_attention_memory_for_sums():
+    """What calls can use beside their workspace: a query of NULL or of a refused descriptor, the sizes by the number of parts, misaligned memory."""
+    L = samo.lib()
+    need = ctypes.c_size_t(7)
+    ask = lambda d, backward: L.samo_attention_sums_bytes(ctypes.byref(d), backward, ctypes.byref(need))
+    assert L.samo_attention_sums_bytes(None, 0, ctypes.byref(need)) == NULL
+    assert L.samo_attention_sums_bytes(ctypes.byref(attention()), 0, None) == NULL
+    assert ask(attention(dim=12), 0) == SIZE and ask(attention(dq=samo.Heads(None, 256, 64)), 1) == NULL
+    assert L.samo_attention(ctypes.byref(attention(d_sums=FAKE + 8, sums_bytes=1 << 20)), None) == ALIGN
+    assert L.samo_attention_backward(ctypes.byref(attention(d_sums=FAKE + 4)), FAKE, 1 << 20, None) == ALIGN
+    try:
+        for parts in (1, 2, 16, 40):
+            samo.samo_debug_set(samo.KNOB_ATTENTION_SPLIT, parts)
+            slots = 0 if parts == 1 else min(parts, 16)       # of 128 rows, one tile of a head; more than 16 parts are 16
+            assert ask(attention(), 0) == OK and need.value == 4 * slots * 128 * (4 * 64 + 8)
+            assert ask(attention(), 1) == OK and need.value == slots * max(4 * 128 * 4 * 64, 2 * 2 * 128 * 4 * 64)
+            assert ask(attention(dim=72), 0) == OK and need.value == 4 * slots * 128 * (4 * 96 + 8)
+    finally:
+        samo.samo_debug_set(samo.KNOB_ATTENTION_SPLIT)
+    # a short call of this size has no use for any
+    assert ask(attention(), 0) == OK and need.value == 0
