@@ -719,9 +719,10 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
 }
 
 // The workgroups of dK and dV from which a wave has its keys for itself; below, where the longest workgroup is what the call waits for, two share them.
-// Whole backward pass of heads of 64, one wave / two, us: 256 workgroups, 2048 tokens of 16 heads 98 / 85; 512, two times 2048 of 32 heads 77 / 84;
-// 512, 16384 of 16 heads on 4 2795 / 2795; 1024, 8192 in 16 sequences of 16 heads 90 / 104; 2048, 8192 of 32 heads 1185 / 1230.  Heads of 80 and 96
-// gain less from it (97 / 100, 121 / 134, 1580 / 1570; 512 long ones 3950 / 3400): two always, one would spill besides.
+// Whole backward pass of heads of 64, one wave / two, us: 32 workgroups, 512 tokens of 8 heads 33 / 30; 256, 2048 of 16 heads 80 / 78; 512,
+// two times 2048 of 32 heads 68 / 68; 512, 16384 of 16 heads on 4 2118 / 2240; 1024, 8192 in 16 sequences of 16 heads 77 / 90; 2048, 8192 of 32
+// heads 1078 / 1150.  Heads of 80 and 96 gain less from it (97 / 100, 121 / 134, 1580 / 1570 before the order of pick(); 512 long ones 3950 / 3400): two
+// always, one would spill besides.
 constexpr int kOneSideFrom = 512;
 
 template <int KS>
