@@ -721,9 +721,9 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
 // The workgroups of dK and dV from which a wave has its keys for itself; below, where the longest workgroup is what the call waits for, two share them.
 // Whole backward pass of heads of 64, one wave / two, us: 32 workgroups, 512 tokens of 8 heads 33 / 30; 256, 2048 of 16 heads 80 / 78; 512,
 // two times 2048 of 32 heads 68 / 68; 512, 16384 of 16 heads on 4 2118 / 2240; 1024, 8192 in 16 sequences of 16 heads 77 / 90; 2048, 8192 of 32
-// heads 1078 / 1150.  Heads of 80 and 96 gain less from it (97 / 100, 121 / 134, 1580 / 1570 before the order of pick(); 512 long ones 3950 / 3400): two
-// always, one would spill besides.
-constexpr int kOneSideFrom = 512;
+// heads 1078 / 1150.  Of 80: 1024 workgroups 100 / 120, 2048 1479 / 1581, but 512 long ones 3910 / 3105; of 96 108 / 126, 1588 / 1665, 4150 / 3350.
+// Heads of more than 96 always share: V's rows in LDS leave room for one workgroup.
+constexpr int one_side_from(int dim) { return dim <= 64 ? 512 : dim <= 96 ? 1024 : INT32_MAX; }
 
 template <int KS>
 hipError_t launch_dim(int which, const AttnArgs &a, int64_t items, hipStream_t s)
@@ -735,8 +735,8 @@ hipError_t launch_dim(int which, const AttnArgs &a, int64_t items, hipStream_t s
     const dim3 grid((unsigned)(places * a.splits * 8)), joins((unsigned)(items * 4), which == kDkv ? 2 : 1);
     if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
-    else if (KS <= 4 && items * a.splits >= kOneSideFrom)
-        hipLaunchKernelGGL((attention_dkv_kernel<KS, KS <= 4 ? 1 : 2>), grid, dim3(kAttnThreads), 0, s, a);
+    else if (KS <= 6 && items * a.splits >= one_side_from(a.dim))
+        hipLaunchKernelGGL((attention_dkv_kernel<KS, KS <= 6 ? 1 : 2>), grid, dim3(kAttnThreads), 0, s, a);
     else hipLaunchKernelGGL((attention_dkv_kernel<KS, 2>), grid, dim3(2 * kAttnThreads), 0, s, a);
     if (a.splits > 1) {
         if (hipError_t e = hipGetLastError()) return e;
@@ -772,7 +772,7 @@ int64_t sums_bytes(int which, const AttnArgs &a, int splits)
 // Where every workgroup has as much to do, the rounds that they take count whole.
 double launch_us(int which, const AttnArgs &a, int64_t items, int splits)
 {
-    const bool dkv = which == kDkv, one_side = dkv && a.dim <= 64 && items * splits >= kOneSideFrom;
+    const bool dkv = which == kDkv, one_side = dkv && items * splits >= one_side_from(a.dim);
     const double q = (double)a.q_tokens / a.batch, k = (double)a.k_tokens / a.batch;
     double longest = dkv ? q : k, mean = 1.0;
     if (a.window) longest = std::min(longest, (double)a.window + kOwnRows);

@@ -152,6 +152,13 @@ def test_many_workgroups(dim, causal, window):
     check(lens, [n + 3 * i for i, n in enumerate(lens)], 16, 16, dim, causal, window, slack=230, seed=dim)
 
 
+@pytest.mark.parametrize("dim", [80, 96, 104])
+def test_more_workgroups(dim):
+    """1024 workgroups of keys: the same form for the larger heads that have it."""
+    lens = [130, 0, 1, 64, 257, 200, 128, 65]
+    check(lens, [n + 3 * i for i, n in enumerate(lens)], 16, 16, dim, True, 0, slack=700, seed=dim)
+
+
 @pytest.fixture
 def parts(request):
     samo.samo_debug_set(samo.KNOB_ATTENTION_SPLIT, request.param)
