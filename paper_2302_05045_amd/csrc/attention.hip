@@ -493,7 +493,7 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 // have the same keys, one takes the first 32 queries of every tile and the other the last, and their sums meet in LDS at the end: a workgroup's time
 // counts as much as the device's, under a causal mask the first keys are seen by every query (8192 tokens, 32 heads of 128, 8 of keys: with
 // four waves the longest of 512 workgroups took 1.8 ms by itself; the whole backward pass 2414 -> 2090 us).
-// Four products a tile: 1300 us for those 8192 tokens, 845 TFLOP/s; 4 x 2048, 32 heads of 80: 330 us.
+// Four products a tile: 1300 us for those 8192 tokens, 845 TFLOP/s; 4 x 2048, 32 heads of 80 (one wave to its keys): 270 us.
 // Two waves to a SIMD have 256 registers each.  Heads of more than 96 fill half of them with their sums: there the rows of V stay in LDS, from where
 // they are read for every block.
 template <int KS, int SIDES>
