@@ -482,7 +482,9 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * d_x: tokens x in, d_w_gate and d_w_up: ffn x in (the dense w of a layer, with explicit zeros), everything else tokens x ffn, dX tokens x in;
  * row-major fp16, 16-byte aligned.  in and ffn are multiples of 8 below 2^20, tokens below 2^31; tokens 0 does nothing.
  * Sums are fp32 in a fixed order.  samo_glu forms h from the sums, rounded once; d_gate and d_up, both or neither, receive G and U
- * rounded once, for samo_glu_backward, which reads them.  d_dx may be NULL (no dX wanted).
+ * rounded once, for samo_glu_backward, which reads them.  d_dx may be NULL (no dX wanted).  With relu a positive G is kept as 2^-24, fp16's smallest
+ * number, where it would round to zero: the slope is that of the sum which h was formed from.  (That sum is the fp32 one: where the exact sum
+ * is nearer to zero than its roundings it may be on the other side.)
  * samo_glu_workspace_bytes: what samo_glu_backward can use on the current device for layers with few tiles of dX (fp32 sums of parts
  * of the summation); with less, or NULL, it does without.  In use until the stream has passed the call. */
 enum { SAMO_ACT_SILU = 0, SAMO_ACT_GELU = 1, SAMO_ACT_GELU_TANH = 2, SAMO_ACT_RELU = 3 };

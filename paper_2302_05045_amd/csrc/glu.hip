@@ -92,6 +92,14 @@ __device__ __forceinline__ float activation(float z, float &slope)
     return z > 0.f ? z : (z <= 0.f ? 0.f : z);               // NaN stays
 }
 
+// G as it is kept for the backward pass, which has relu's slope from its sign: a positive sum that rounds to zero stays the smallest positive number, so
+// that both passes are on the same side of zero.
+template <int ACT>
+__device__ __forceinline__ _Float16 kept_gate(float g)
+{
+    return (_Float16)(ACT == SAMO_ACT_RELU && g > 0.f ? fmaxf(g, 0x1p-24f) : g);
+}
+
 // Waits until at most `younger` stages' copies of this wave, PER each, are outstanding, and every LDS read has returned.
 template <int PER, int MOST>
 __device__ __forceinline__ void wait_copies(int younger)
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(kGluThreads, 2) glu_kernel(const GluArgs A)
                 float slope;
                 const float g = acc[b][a][r], u = acc[b][a + AB / 2][r];
                 h[r] = (_Float16)(activation<ACT>(g, slope) * u);
-                gate[r] = (_Float16)g;
+                gate[r] = kept_gate<ACT>(g);
                 up[r] = (_Float16)u;
             }
             const int64_t at = t * A.ffn + f;
@@ -421,7 +429,7 @@ __global__ void __launch_bounds__(64 * kSkinnyWaves, 2) glu_skinny_kernel(const 
             float slope;
             const float g = acc[0][b][r], u = acc[1][b][r];
             h[r] = (_Float16)(activation<ACT>(g, slope) * u);
-            gate[r] = (_Float16)g;
+            gate[r] = kept_gate<ACT>(g);
             up[r] = (_Float16)u;
         }
         const int64_t at = t * A.ffn + f;

@@ -222,3 +222,44 @@ def test_same_bits_again_other_stream_and_graph():
         for a, b, c in zip(first, second, third):
             assert torch.equal(a, b) and torch.equal(a, c)
         call(*bufs())
+
+
+def exact_sums(tokens, features, ffn, seed):
+    """Inputs whose sums are multiples of 2^-9 below 2^10, exact in fp32 in every order, and features whose gate is 2^-26, -2^-26 and 0 exactly."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    whole = lambda *s: torch.randint(-32, 33, s, generator=gen, device=DEV).float()
+    x = whole(tokens, features) / 8
+    wg, wu = (whole(ffn, features) / 64 * (torch.rand((ffn, features), generator=gen, device=DEV) < 0.1) for _ in range(2))
+    x[:, -1], wg[:, -1], wu[:, -1] = 2.0 ** -13, 0.0, 0.0
+    for first, small in ((1, 2.0 ** -13), (2, -2.0 ** -13), (3, 0.0)):
+        wg[first::4] = 0.0
+        wg[first::4, -1] = small
+    return gen, x.half(), wg.half(), wu.half()
+
+
+@pytest.mark.parametrize("tokens,shape", [(5, None), (20, None), (40, None), (300, 0), (300, 1), (300, 2), (300, 3)])
+def test_relu_gradients_from_the_inputs(tokens, shape):
+    """relu's slope jumps at zero: the gradients against those of X, Wg, Wu and dh in 64 bits, with gates as small as 2^-26.  up is rounded once, dgate
+    once more: 2.01 u of the result.  A gate is kept within 2^-24, fp16's smallest number, which dup sees times dh."""
+    features, ffn = 264, 520
+    gen, x, wg, wu = exact_sums(tokens, features, ffn, tokens)
+    dh = rnd(gen, tokens, ffn)
+    h, gate, up, dgate, dup, dx = (nan16(tokens, n) for n in (ffn, ffn, ffn, ffn, ffn, features))
+    if shape is not None:
+        samo.samo_debug_set(samo.KNOB_GLU_SHAPE, shape)
+    try:
+        samo.samo_glu(x, wg, wu, h, gate, up, "relu")
+        samo.samo_glu_backward(dh, gate, up, wg, wu, dgate, dup, dx, "relu")
+    finally:
+        samo.samo_debug_set(samo.KNOB_GLU_SHAPE)
+    check_forward(x, wg, wu, h, gate, up, "relu")
+    z, v, d = x.double() @ wg.double().T, x.double() @ wu.double().T, dh.double()
+    assert torch.all(z[:, 1::4] == 2.0 ** -26) and torch.all(z[:, 2::4] == -2.0 ** -26) and torch.all(z[:, 3::4] == 0)
+    dz, dv = d * v * (z > 0), d * torch.relu(z)
+    within(dgate, dz, 2.01 * U * dz.abs(), "dgate")
+    within(dup, dv, 2.01 * U * dv.abs() + TINY * d.abs(), "dup")
+    want = dz @ wg.double() + dv @ wu.double()
+    terms = dz.abs() @ wg.double().abs() + dv.abs() @ wu.double().abs()
+    least = TINY * (wg.double().abs().sum(0) + (1 + d.abs()) @ wu.double().abs())
+    within(dx, want, (2.01 * U + (2 * ffn + 2) * 2.0 ** -24) * terms + least + U * want.abs(), "dx")
