@@ -485,6 +485,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * rounded once, for samo_glu_backward, which reads them.  d_dx may be NULL (no dX wanted).  With relu a positive G is kept as 2^-24, fp16's smallest
  * number, where it would round to zero: the slope is that of the sum which h was formed from.  (That sum is the fp32 one: where the exact sum
  * is nearer to zero than its roundings it may be on the other side.)
+ * A G beyond fp16's range is kept as an infinity, at which the backward pass takes the limits of act' (0 and 1) and of act (0 and infinity).
  * samo_glu_workspace_bytes: what samo_glu_backward can use on the current device for layers with few tiles of dX (fp32 sums of parts
  * of the summation); with less, or NULL, it does without.  In use until the stream has passed the call. */
 enum { SAMO_ACT_SILU = 0, SAMO_ACT_GELU = 1, SAMO_ACT_GELU_TANH = 2, SAMO_ACT_RELU = 3 };

@@ -357,8 +357,11 @@ __global__ void __launch_bounds__(256) glu_pointwise_kernel(const _Float16 *dh, 
     half8 dg, du;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        float slope;
-        const float a = activation<ACT>((float)g[e], slope), back = (float)d[e];
+        // A G beyond fp16's range was kept as an infinity, where the formulas are zero times infinity: act' there is what it is at fp16's largest number
+        // (0 or 1), act(-inf) is 0, and act(inf) stays infinite.
+        const float kept = (float)g[e], z = fabsf(kept) == INFINITY ? copysignf(65504.f, kept) : kept, back = (float)d[e];
+        float slope, a = activation<ACT>(z, slope);
+        if (kept == INFINITY) a = kept;
         dg[e] = (_Float16)(back * (float)u[e] * slope);
         du[e] = (_Float16)(back * a);
     }

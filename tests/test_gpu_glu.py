@@ -263,3 +263,41 @@ def test_relu_gradients_from_the_inputs(tokens, shape):
     terms = dz.abs() @ wg.double().abs() + dv.abs() @ wu.double().abs()
     least = TINY * (wg.double().abs().sum(0) + (1 + d.abs()) @ wu.double().abs())
     within(dx, want, (2.01 * U + (2 * ffn + 2) * 2.0 ** -24) * terms + least + U * want.abs(), "dx")
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+def test_gates_beyond_fp16_have_the_limits_of_the_slope(act):
+    """Sums of 70000 and -70000 are kept as infinities.  The slope there is 1 and 0, act(-70000) is 0: a gradient is finite wherever it does not contain act(70000)."""
+    tokens, features, ffn = 40, 64, 128
+    gen, x, wg, wu = make(tokens, features, ffn, 12)
+    x[:, :3] = 0
+    wg[:, :3], wu[:, :3] = 0, 0
+    wg[0::2, 0], wg[1::2, 0], wu[:, 1], wg[:, 2] = 200.0, -200.0, torch.linspace(-0.75, 0.75, ffn, device=DEV).half(), -200.0
+    x[1], x[2] = 0, 0
+    x[1, 0], x[1, 1] = 350.0, 1.0                            # both signs in turn
+    x[2, 2], x[2, 1] = 350.0, 1.0                            # -70000 everywhere
+    dh = rnd(gen, tokens, ffn)
+    dh[dh == 0] = 1
+    h, gate, up, dgate, dup, dx = (nan16(tokens, n) for n in (ffn, ffn, ffn, ffn, ffn, features))
+    samo.samo_glu(x, wg, wu, h, gate, up, act)
+    check_forward(x, wg, wu, h, None, None, act)
+    assert torch.all(torch.isposinf(gate[1, 0::2])) and torch.all(torch.isneginf(gate[1, 1::2])) and torch.all(torch.isneginf(gate[2]))
+    samo.samo_glu_backward(dh, gate, up, wg, wu, dgate, dup, dx, act)
+    want = dh[1].double() * up[1].double()
+    want[1::2] = 0
+    within(dgate[1], want, 1.01 * U * want.abs(), "dgate")
+    assert torch.equal(dup[1, 0::2], torch.copysign(torch.full_like(dh[1, 0::2], math.inf), dh[1, 0::2])) and torch.all(dup[1, 1::2] == 0)
+    assert torch.all(dgate[2] == 0) and torch.all(dup[2] == 0) and torch.all(dx[2] == 0)
+    rest = [0] + list(range(3, tokens))
+    check_backward(dh[rest], gate[rest], up[rest], wg, wu, dgate[rest], dup[rest], dx[rest], act)
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+def test_a_gate_that_is_no_number_stays_one(act):
+    gen, x, wg, wu = make(40, 64, 128, 13)
+    gate, up, dh = (rnd(gen, 40, 128) for _ in range(3))
+    gate[3, 5] = float("nan")
+    dgate, dup = nan16(40, 128), nan16(40, 128)
+    samo.samo_glu_backward(dh, gate, up, wg, wu, dgate, dup, None, act)
+    hit = torch.isnan(gate)
+    assert torch.equal(torch.isnan(dup), hit) and torch.all(torch.isfinite(dgate[~hit])) and (act == "relu" or torch.isnan(dgate[3, 5]))
