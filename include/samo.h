@@ -444,6 +444,8 @@ samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
  * Sequences lie end to end: sequence s of `batch` holds the tokens start[s] .. start[s + 1] - 1 of q_start and k_start (device,
  * int32[batch + 1], ascending from 0 up; read when the kernels run; tokens behind the last start are not touched).  Both NULL: batch is 1
  * and the sequence is all tokens.  max_q and max_k: at least the longest sequence's tokens (rows behind them are not computed).
+ * Every 128 of them are a workgroup for each sequence and head, and a launch holds fewer than 2^24 (dk and dv with a dim above 96: 2^23): where
+ * ceil(max_q / 128) batch heads or, backward, ceil(max_k / 128) batch kv_heads reaches that, SAMO_ERR_SIZE.
  *   S = scale q k^T;  out = softmax(S) v;  lse = log sum exp S, float[heads * q_tokens], head by head (natural logarithm)
  * causal != 0: the last query of a sequence sees all of its keys, query i key j if j <= i + k_len - q_len and, with window > 0, only
  * the last `window` of those.  A query that sees no key has out = 0, lse = -infinity and no gradient.  scale > 0.

@@ -1156,7 +1156,8 @@ def samo_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
 
     q, out: (tokens, heads, dim), k, v: (tokens, kv_heads, dim) fp16, strided as slices of a packed projection are; lse: float32
     (heads, tokens).  q_start, k_start: int32 (sequences + 1) on the GPU, the sequences' first tokens; none: one sequence.
-    max_q, max_k: the longest sequence's tokens (default: all tokens).  scale: default 1 / sqrt(dim).
+    max_q, max_k: the longest sequence's tokens (default: all tokens, for which a call of many sequences has as many more workgroups,
+    idle ones, and is refused from 2^23 or 2^24 on).  scale: default 1 / sqrt(dim).
     Few heads and rows split the keys over workgroups, whose sums meet in the workspace (uint8; in use until the stream has passed the
     call; too few bytes, or an empty one: not split).  Without one the call takes what it can use from torch's allocator."""
     d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)

@@ -1228,9 +1228,7 @@ samo_status check_attention(const samo_attention_desc *d, bool backward, AttnArg
     if (!(std::isfinite(d->scale) && d->scale > 0.f) || d->window < 0 || (d->window > 0 && !d->causal)) return SAMO_ERR_ARG;
     if (d->q_tokens > 0 && !d->d_lse) return SAMO_ERR_NULL;
     if (misaligned(d->d_sums)) return SAMO_ERR_ALIGN;
-    // a launch's workgroups, 128 rows of a head each, fit 31 bits
-    if (ceil_div(d->max_q, 128) * d->batch * d->heads > INT32_MAX / 2 || ceil_div(d->max_k, 128) * d->batch * d->kv_heads > INT32_MAX / 2)
-        return SAMO_ERR_SIZE;
+    if (!attention_fits(*d, backward)) return SAMO_ERR_SIZE;
     const samo_heads *of_q[] = {&d->q, &d->out, &d->dout, &d->dq}, *of_k[] = {&d->k, &d->v, &d->dk, &d->dv};
     for (int i = 0; i < (backward ? 4 : 2); ++i) {
         if (samo_status s = check_heads(*of_q[i], d->q_tokens)) return s;

@@ -725,14 +725,18 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
 // Heads of more than 96 always share: V's rows in LDS leave room for one workgroup.
 constexpr int one_side_from(int dim) { return dim <= 64 ? 512 : dim <= 96 ? 1024 : INT32_MAX; }
 
+// An XCD's workgroups, as pick() deals them; heads and sequences are fewer than 2^31 together.
+int64_t places_of(int64_t all, int64_t tiles)
+{
+    const int share = heads_an_xcd((int)all);
+    return share ? share * tiles : ceil_div(all * tiles, 8);
+}
+
 template <int KS>
 hipError_t launch_dim(int which, const AttnArgs &a, int64_t items, hipStream_t s)
 {
     constexpr int DB = blocks_of(KS);
-    // as pick() deals them
-    const int share = heads_an_xcd((int)(items / a.tiles));
-    const int64_t places = share ? (int64_t)share * a.tiles : ceil_div(items, 8);
-    const dim3 grid((unsigned)(places * a.splits * 8)), joins((unsigned)(items * 4), which == kDkv ? 2 : 1);
+    const dim3 grid((unsigned)(places_of(items / a.tiles, a.tiles) * a.splits * 8)), joins((unsigned)(items * 4), which == kDkv ? 2 : 1);
     if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
     else if (KS <= 6 && items * a.splits >= one_side_from(a.dim))
@@ -795,7 +799,7 @@ int splits_of(int which, const AttnArgs &a)
     constexpr int kMost = 16, kSlots = 2048;
     const int64_t items = items_of(which, a), forced = knob(SAMO_KNOB_ATTENTION_SPLIT, -1);
     if (items == 0) return 1;
-    if (forced > 0) return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, forced, INT32_MAX / 4 / items}));
+    if (forced > 0) return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, forced, (1 << 21) / items}));       // a launch holds 2^23 workgroups and more
     // Two rounds of the device are even enough: the longest workgroups come first (8192 tokens, 32 heads of 128, 8 of keys: dK and dV 1350 us as they are, 1500
     // in two parts; forward 597 and 674).
     if (items >= (which == kDkv && a.dim > 64 ? 2 : 4) * compute_units()) return 1;
@@ -830,6 +834,18 @@ hipError_t launch(int which, AttnArgs a, size_t bytes, hipStream_t s)
 }
 
 }  // namespace
+
+// The runtime counts a launch's threads in 32 bits: fewer than 2^24 workgroups, of dK and dV where two waves share the keys of so many 2^23.  (Launches in
+// parts are far smaller.)
+bool attention_fits(const samo_attention_desc &d, bool backward)
+{
+    for (int which = backward ? kDq : kForward; which <= (backward ? kDkv : kForward); ++which) {
+        const int64_t all = (int64_t)d.batch * (which == kDkv ? d.kv_heads : d.heads), tiles = ceil_div(which == kDkv ? d.max_k : d.max_q, kOwnRows);
+        const int64_t most = UINT32_MAX / (kAttnThreads * (which == kDkv && one_side_from(d.dim) == INT32_MAX ? 2 : 1));
+        if (tiles > 0 && (all > most || places_of(all, tiles) > most / 8)) return false;
+    }
+    return true;
+}
 
 int64_t attention_sums_bytes(const AttnArgs &a, bool backward)
 {

@@ -257,6 +257,8 @@ struct AttnArgs {
     float *parts;                           // NULL: a launch is not split
     f32x2 *part_stats;
 };
+// Whether the call's launches can be made.
+bool attention_fits(const samo_attention_desc &d, bool backward);
 // Bytes that a call can use at `parts`; with less a launch that would need them is not split.
 int64_t attention_sums_bytes(const AttnArgs &a, bool backward);
 hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s);

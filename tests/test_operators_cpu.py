@@ -194,3 +194,35 @@ def test_attention_memory_for_sums():
         samo.samo_debug_set(samo.KNOB_ATTENTION_SPLIT)
     # a short call of this size has no use for any
     assert ask(attention(), 0) == OK and need.value == 0
+
+
+def views_of(dim):
+    return {name: samo.Heads(FAKE, 32 * dim, dim) for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")}
+
+
+@pytest.mark.parametrize("kw,dkv_only", [
+    (dict(batch=2 ** 19, heads=32, kv_heads=32, max_q=1), False),                              # 2^24 workgroups of 256 threads
+    (dict(batch=512, heads=32, kv_heads=32, q_tokens=2 ** 18, k_tokens=2 ** 18, max_q=2 ** 18, max_k=2 ** 18), False),
+    (dict(batch=2 ** 31 - 1, heads=2 ** 31 - 1, kv_heads=1, max_q=10), False),
+    (dict(batch=2 ** 18, heads=32, kv_heads=32, dim=128, max_q=1, max_k=1), True),             # 2^23 of 512
+    (dict(batch=2 ** 19, heads=32, kv_heads=32, max_q=0, max_k=1), True),
+])
+def test_attention_refuses_more_threads_than_a_launch_holds(kw, dkv_only):
+    """A launch's threads are counted in 32 bits: refused before the first of the call's launches."""
+    L = samo.lib()
+    d = attention(d_q_start=FAKE, d_k_start=FAKE, **kw, **views_of(kw.get("dim", 64)))
+    need = ctypes.c_size_t()
+    room = 4 * d.heads * d.q_tokens
+    assert L.samo_attention_backward(ctypes.byref(d), FAKE, room, None) == SIZE
+    assert L.samo_attention_sums_bytes(ctypes.byref(d), 1, ctypes.byref(need)) == SIZE
+    assert L.samo_attention_sums_bytes(ctypes.byref(d), 0, ctypes.byref(need)) == (OK if dkv_only else SIZE)
+    if not dkv_only:
+        assert L.samo_attention(ctypes.byref(d), None) == SIZE
+
+
+@pytest.mark.parametrize("kw", [dict(batch=2 ** 19 - 1, heads=32, kv_heads=32, max_q=1, max_k=0), dict(batch=2 ** 19 - 1, heads=32, kv_heads=32, max_q=1, max_k=1),
+                                dict(batch=2 ** 18 - 1, heads=32, kv_heads=32, dim=128, max_q=1, max_k=1)])
+def test_attention_takes_what_a_launch_holds(kw):
+    need = ctypes.c_size_t()
+    for backward in (0, 1):
+        assert samo.lib().samo_attention_sums_bytes(ctypes.byref(attention(d_q_start=FAKE, d_k_start=FAKE, **kw, **views_of(kw.get("dim", 64)))), backward, ctypes.byref(need)) == OK
