@@ -449,7 +449,7 @@ samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
  *   S = scale q k^T;  out = softmax(S) v;  lse = log sum exp S, float[heads * q_tokens], head by head (natural logarithm)
  * causal != 0: the last query of a sequence sees all of its keys, query i key j if j <= i + k_len - q_len and, with window > 0, only
  * the last `window` of those.  A query that sees no key has out = 0, lse = -infinity and no gradient.  scale > 0.
- * dim is a multiple of 8 up to 128; lengths from 0.  P = exp(S - lse) and dS = P (dP - delta) are rounded to fp16 where they enter a product
+ * dim is a multiple of 8 up to 128; lengths from 0, q_tokens and k_tokens up to 2^30 - 128.  P = exp(S - lse) and dS = P (dP - delta) are rounded to fp16 where they enter a product
  * (as the tensors themselves are), sums and softmax are fp32; the order of the sums is fixed.  Masked scores are replaced, so a key
  * that is not finite does not reach a query that does not see its tile of 64 keys; within a tile a value that is not finite does (0 times it).
  * Backward: dq, dk, dv from dout and the forward pass's q, k, v, out, lse; d_workspace: samo_attention_workspace_bytes, 16-byte aligned.

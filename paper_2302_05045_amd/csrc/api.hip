@@ -1205,6 +1205,7 @@ samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream) { r
 namespace {
 
 constexpr int kMaxHeadDim = 128;
+constexpr int64_t kMaxTokens = (1 << 30) - 128;              // the masks are sums of two lengths and a window, 2^30 where there is none, in 32 bits
 
 samo_status check_heads(const samo_heads &t, int64_t tokens)
 {
@@ -1218,7 +1219,7 @@ samo_status check_heads(const samo_heads &t, int64_t tokens)
 samo_status check_attention(const samo_attention_desc *d, bool backward, AttnArgs *a)
 {
     if (!d) return SAMO_ERR_NULL;
-    if (d->q_tokens < 0 || d->q_tokens > INT32_MAX || d->k_tokens < 0 || d->k_tokens > INT32_MAX) return SAMO_ERR_SIZE;
+    if (d->q_tokens < 0 || d->q_tokens > kMaxTokens || d->k_tokens < 0 || d->k_tokens > kMaxTokens) return SAMO_ERR_SIZE;
     if (d->batch < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->dim < 8 || d->dim > kMaxHeadDim || d->dim % 8)
         return SAMO_ERR_SIZE;
     if (d->max_q < 0 || d->max_k < 0 || d->max_q > d->q_tokens || d->max_k > d->k_tokens) return SAMO_ERR_SIZE;
@@ -1287,7 +1288,7 @@ samo_status samo_attention_sums_bytes(const samo_attention_desc *h_desc, int32_t
 samo_status samo_attention_workspace_bytes(const samo_attention_desc *h_desc, size_t *bytes)
 {
     if (!h_desc || !bytes) return SAMO_ERR_NULL;
-    if (h_desc->heads < 1 || h_desc->q_tokens < 0 || h_desc->q_tokens > INT32_MAX) return SAMO_ERR_SIZE;
+    if (h_desc->heads < 1 || h_desc->q_tokens < 0 || h_desc->q_tokens > kMaxTokens) return SAMO_ERR_SIZE;
     *bytes = (size_t)h_desc->heads * (size_t)h_desc->q_tokens * sizeof(float);
     return SAMO_OK;
 }

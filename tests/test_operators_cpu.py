@@ -226,3 +226,15 @@ def test_attention_takes_what_a_launch_holds(kw):
     need = ctypes.c_size_t()
     for backward in (0, 1):
         assert samo.lib().samo_attention_sums_bytes(ctypes.byref(attention(d_q_start=FAKE, d_k_start=FAKE, **kw, **views_of(kw.get("dim", 64)))), backward, ctypes.byref(need)) == OK
+
+
+@pytest.mark.parametrize("name", ["q_tokens", "k_tokens"])
+def test_attention_refuses_tokens_whose_bounds_pass_32_bits(name):
+    """Windows and masks are sums of two lengths and a window, which is 2^30 where there is none."""
+    L = samo.lib()
+    need = ctypes.c_size_t()
+    for tokens, want in ((2 ** 30 - 127, SIZE), (2 ** 30, SIZE), (2 ** 31 - 1, SIZE), (2 ** 30 - 128, OK)):
+        d = attention(**{name: tokens})
+        assert L.samo_attention_sums_bytes(ctypes.byref(d), 0, ctypes.byref(need)) == want, tokens
+        if want == SIZE:
+            assert L.samo_attention(ctypes.byref(d), None) == SIZE and L.samo_attention_backward(ctypes.byref(d), FAKE, 1 << 40, None) == SIZE
