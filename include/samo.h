@@ -449,9 +449,12 @@ samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
  *   S = scale q k^T;  out = softmax(S) v;  lse = log sum exp S, float[heads * q_tokens], head by head (natural logarithm)
  * causal != 0: the last query of a sequence sees all of its keys, query i key j if j <= i + k_len - q_len and, with window > 0, only
  * the last `window` of those.  A query that sees no key has out = 0, lse = -infinity and no gradient.  scale > 0.
- * dim is a multiple of 8 up to 128; lengths from 0, q_tokens and k_tokens up to 2^30 - 128.  P = exp(S - lse) and dS = P (dP - delta) are rounded to fp16 where they enter a product
- * (as the tensors themselves are), sums and softmax are fp32; the order of the sums is fixed.  Masked scores are replaced, so a key
- * that is not finite does not reach a query that does not see its tile of 64 keys; within a tile a value that is not finite does (0 times it).
+ * dim is a multiple of 8 up to 128; lengths from 0, q_tokens and k_tokens up to 2^30 - 128.  P = exp(S - lse) and dS = P (dP - delta) are rounded to
+ * fp16 where they enter a product (as the tensors themselves are), sums and softmax are fp32; the order of the sums is fixed.
+ * Masked scores are replaced, and products are formed by blocks of 32 queries and 64 keys (the gradients': 32), counted from a sequence's first token;
+ * a pair of blocks that the mask hides entirely is left out.  So a key or value that is not finite changes no lse of a query that does not see it, but
+ * reaches, as 0 times it, the out and from there the gradients of every query whose block sees any key of its block; likewise a query or dout the dk
+ * and dv of every key of a block that its own sees.
  * Backward: dq, dk, dv from dout and the forward pass's q, k, v, out, lse; d_workspace: samo_attention_workspace_bytes, 16-byte aligned.
  * Calls of few heads and rows (a few tokens behind a long context) split the keys, or for dk and dv the queries, over workgroups whose fp32 sums
  * meet in d_sums; samo_attention_sums_bytes is what the forward or backward call can use of it on the current device (0: nothing),

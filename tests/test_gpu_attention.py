@@ -336,3 +336,63 @@ def test_native_and_python_descriptors_agree():
                 assert (made.q.d_data, made.q.row, made.q.head) == (want.d_data, want.row, want.head)
             samo._set_heads(made, "q", t, *shape)
             assert (made.q.d_data, made.q.row, made.q.head) == (want.d_data, want.row, want.head)
+
+
+def reached(seen, bad_q, bad_k, block_k):
+    """Which queries and keys share a block (32 queries, block_k keys) that holds a seen pair with one of the bad ones."""
+    n, m = seen.shape
+    qs, ks = -(-n // 32), -(-m // block_k)
+    whole = torch.zeros((qs * 32, ks * block_k), dtype=torch.bool, device=DEV)
+    whole[:n, :m] = seen
+    meet = whole.view(qs, 32, ks, block_k).any(3).any(1)
+    spread = lambda bad, count, size: torch.nn.functional.pad(bad, (0, count * size - bad.numel())).view(count, size).any(1)
+    of_q = (meet & spread(bad_k, ks, block_k)[None]).any(1).repeat_interleave(32)[:n]
+    of_k = (meet & spread(bad_q, qs, 32)[:, None]).any(0).repeat_interleave(block_k)[:m]
+    return of_q, of_k
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,prefix,window,bad", [(200, 0, 0, 70), (200, 10, 0, 70), (200, 10, 16, 70), (200, 33, 100, 130), (160, 300, 20, 5), (300, 1, 0, 255)])
+def test_what_is_not_finite_reaches_no_further_than_its_blocks(n, prefix, window, bad, dim):
+    """A key, value, query or gradient that is not finite reaches the rows whose block of 32 queries and 64 keys (gradients: 32) holds a pair that the mask
+    leaves, and no other; where a query does not see the key, lse is as it was."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(n + prefix)
+    m = n + prefix
+    rnd = lambda t: torch.randn((t, 1, dim), generator=gen, device=DEV).half()
+    q, k, v, do = rnd(n), rnd(m), rnd(m), rnd(n)
+    seen = seen_of(n, m, True, window)
+
+    def run(q, k, v, do):
+        out, lse, dq, dk, dv = torch.zeros_like(q), torch.zeros(1, n, device=DEV), torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+        samo.samo_attention(q, k, v, out, lse, window=window)
+        samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv, window=window)
+        return out, lse[0], dq, dk, dv
+
+    clean = run(q, k, v, do)
+    assert all(torch.all(torch.isfinite(t)) for t in clean)
+    bad_k = torch.zeros(m, dtype=torch.bool, device=DEV)
+    bad_k[bad] = True
+    k2, v2 = k.clone(), v.clone()
+    k2[bad], v2[bad] = float("nan"), float("inf")
+    for keys, values in ((k2, v2), (k, v2), (k2, v)):
+        got = run(q, keys, values, do)
+        bad_q, _ = reached(seen, torch.zeros(n, dtype=torch.bool, device=DEV), bad_k, 64)
+        hidden = ~seen[:, bad]
+        assert torch.equal(got[0][~bad_q], clean[0][~bad_q]) and torch.equal(got[2][~bad_q], clean[2][~bad_q])
+        assert torch.all((got[1] - clean[1])[hidden].abs() <= 2.0 ** -19 * (1 + clean[1][hidden].abs()))
+        assert not torch.isfinite(got[0][~hidden]).all(2).any()
+        _, keys_hit = reached(seen, bad_q, bad_k, 32)
+        for i in (3, 4):
+            assert torch.equal(got[i][~keys_hit & ~bad_k], clean[i][~keys_hit & ~bad_k])
+    hit = n // 2
+    one = torch.zeros(n, dtype=torch.bool, device=DEV)
+    one[hit] = True
+    _, keys_hit = reached(seen, one, torch.zeros(m, dtype=torch.bool, device=DEV), 32)
+    q2, do2 = q.clone(), do.clone()
+    q2[hit], do2[hit] = float("nan"), float("inf")
+    for queries, grads in ((q2, do), (q, do2)):
+        got = run(queries, k, v, grads)
+        assert torch.equal(got[0][~one], clean[0][~one]) or queries is q2
+        for i in (3, 4):
+            assert torch.equal(got[i][~keys_hit], clean[i][~keys_hit])
