@@ -396,3 +396,16 @@ def test_what_is_not_finite_reaches_no_further_than_its_blocks(n, prefix, window
         assert torch.equal(got[0][~one], clean[0][~one]) or queries is q2
         for i in (3, 4):
             assert torch.equal(got[i][~keys_hit], clean[i][~keys_hit])
+
+
+@pytest.mark.parametrize("dim", [64, 80, 128])
+def test_gradients_of_large_losses(dim):
+    """dP - delta of tens of thousands; from 65504 on dS, as any fp16 gradient, is infinite, and what is formed from it is no finite number."""
+    check([2] * 12, [2] * 12, 8, 4, dim, False, 0, dstd=1500.0)
+    q, k, v, do = (torch.zeros(2, 1, dim, device=DEV).half() for _ in range(4))
+    k[0], k[1], v[0], v[1], do[:] = 0.5, -0.5, 60.0, -60.0, 60.0
+    out, lse, dq, dk, dv = torch.zeros_like(q), torch.zeros(1, 2, device=DEV), torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(q)
+    samo.samo_attention(q, k, v, out, lse, causal=False)
+    samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv, causal=False)
+    assert torch.all(out == 0) and torch.all(dv == 60.0)      # P is 1/2 everywhere, |dS| = 1800 dim
+    assert not torch.isfinite(dq).any() and not torch.isfinite(dk).any()
