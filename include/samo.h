@@ -439,7 +439,8 @@ samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
  * What lies between the QKV projection and the output projection (Section V trains GPT models), forward and backward; the
  * gradients it leaves in the QKV projection's output gradient are the dY of samo_wgrad_gather.
  * A samo_heads is a tokens x heads x dim fp16 tensor: element (t, h, d) at d_data[t * row + h * head + d].  row and head are
- * multiples of 8 and not negative, d_data is 16-byte aligned: a slice of a packed projection will do.
+ * multiples of 8 and not negative, d_data is 16-byte aligned: a slice of a packed projection will do.  Of what is only read rows or heads may be the same
+ * memory; those of a result are at least dim apart (SAMO_ERR_SIZE).
  * q, out, dout and dq have `heads` heads, k, v, dk and dv kv_heads, a divisor of it: query head h reads head h / (heads / kv_heads).
  * Sequences lie end to end: sequence s of `batch` holds the tokens start[s] .. start[s + 1] - 1 of q_start and k_start (device,
  * int32[batch + 1], ascending from 0 up; read when the kernels run; tokens behind the last start are not touched).  Both NULL: batch is 1

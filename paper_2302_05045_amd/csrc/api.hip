@@ -1216,6 +1216,9 @@ samo_status check_heads(const samo_heads &t, int64_t tokens)
     return SAMO_OK;
 }
 
+// Whether rows or heads of a result surely overlap.
+bool overlaps(const samo_heads &t, int64_t tokens, int32_t heads, int32_t dim) { return (tokens > 1 && t.row < dim) || (heads > 1 && t.head < dim && tokens > 0); }
+
 samo_status check_attention(const samo_attention_desc *d, bool backward, AttnArgs *a)
 {
     if (!d) return SAMO_ERR_NULL;
@@ -1273,6 +1276,7 @@ samo_status samo_attention(const samo_attention_desc *h_desc, void *stream)
 {
     AttnArgs a;
     if (samo_status s = check_attention(h_desc, false, &a)) return s;
+    if (overlaps(h_desc->out, a.q_tokens, a.heads, a.dim)) return SAMO_ERR_SIZE;
     return hip_status(launch_attention(a, h_desc->sums_bytes, as_stream(stream)));
 }
 
@@ -1298,6 +1302,8 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
     AttnArgs a;
     size_t need = 0;
     if (samo_status s = check_attention(h_desc, true, &a)) return s;
+    if (overlaps(h_desc->dq, a.q_tokens, a.heads, a.dim) || overlaps(h_desc->dk, a.k_tokens, a.kv_heads, a.dim) || overlaps(h_desc->dv, a.k_tokens, a.kv_heads, a.dim))
+        return SAMO_ERR_SIZE;
     if (samo_status s = samo_attention_workspace_bytes(h_desc, &need)) return s;
     if (need > 0 && (!d_workspace || workspace_bytes < need)) return SAMO_ERR_WORKSPACE;
     if (misaligned(d_workspace)) return SAMO_ERR_ALIGN;

@@ -238,3 +238,20 @@ def test_attention_refuses_tokens_whose_bounds_pass_32_bits(name):
         assert L.samo_attention_sums_bytes(ctypes.byref(d), 0, ctypes.byref(need)) == want, tokens
         if want == SIZE:
             assert L.samo_attention(ctypes.byref(d), None) == SIZE and L.samo_attention_backward(ctypes.byref(d), FAKE, 1 << 40, None) == SIZE
+
+
+@pytest.mark.parametrize("view", [samo.Heads(FAKE, 0, 64), samo.Heads(FAKE, 256, 0), samo.Heads(FAKE, 56, 640), samo.Heads(FAKE, 256, 56)])
+def test_attention_refuses_results_that_overlap(view):
+    """Rows or heads of a result less than dim apart are written by several workgroups; of what is only read they may be one and the same.  (max_q and
+    max_k of 0: nothing is launched.)"""
+    L = samo.lib()
+    forward = lambda **kw: L.samo_attention(ctypes.byref(attention(**{**dict(max_q=0, max_k=0), **kw})), None)
+    back = lambda **kw: L.samo_attention_backward(ctypes.byref(attention(**{**dict(max_q=0, max_k=0), **kw})), FAKE, 1 << 20, None)
+    assert forward(out=view) == SIZE and all(back(**{name: view}) == SIZE for name in ("dq", "dk", "dv"))
+    for name in ("q", "k", "v", "dq", "dk", "dv"):
+        assert forward(**{name: view}) == OK, name
+    for name in ("q", "k", "v", "dout", "out"):              # the backward pass reads out
+        assert back(**{name: view}) == OK, name
+    # strides of a dimension of one element are not looked at
+    assert forward(out=samo.Heads(FAKE, 0, 64), q_tokens=1) == OK and forward(out=samo.Heads(FAKE, 64, 0), heads=1, kv_heads=1) == OK
+    assert back(dk=samo.Heads(FAKE, 64, 0), kv_heads=1) == OK and back(dk=samo.Heads(FAKE, 0, 64), k_tokens=1) == OK
