@@ -1103,6 +1103,14 @@ def _set_heads(d: AttentionDesc, name: str, t: torch.Tensor, tokens: int = -1, h
         setattr(d, name, _heads(t, name, None if tokens < 0 else (tokens, heads, dim)))
 
 
+def _int32(x: int, name: str) -> int:
+    """A number for a 32-bit field, which would take the low bits of any."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError("%s = %d does not fit 32 bits" % (name, x))
+    return x
+
+
 def _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k) -> AttentionDesc:
     d = AttentionDesc()
     _set_heads(d, "q", q)
@@ -1126,10 +1134,10 @@ def _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, 
         d.d_q_start = _dev(q_start, torch.int32, "q_start", 2)
         d.d_k_start = _dev(k_start, torch.int32, "k_start", d.batch + 1)
     d.q_tokens, d.k_tokens, d.heads, d.kv_heads, d.dim = q_tokens, k_tokens, heads, kv_heads, dim
-    d.max_q = q_tokens if max_q is None else int(max_q)
-    d.max_k = k_tokens if max_k is None else int(max_k)
+    d.max_q = _int32(q_tokens if max_q is None else max_q, "max_q")
+    d.max_k = _int32(k_tokens if max_k is None else max_k, "max_k")
     d.scale = float(scale) if scale is not None else dim ** -0.5
-    d.causal, d.window = int(bool(causal)), int(window)
+    d.causal, d.window = int(bool(causal)), _int32(window, "window")
     return d
 
 

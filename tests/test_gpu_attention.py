@@ -409,3 +409,16 @@ def test_gradients_of_large_losses(dim):
     samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv, causal=False)
     assert torch.all(out == 0) and torch.all(dv == 60.0)      # P is 1/2 everywhere, |dS| = 1800 dim
     assert not torch.isfinite(dq).any() and not torch.isfinite(dk).any()
+
+
+@pytest.mark.parametrize("name", ["window", "max_q", "max_k"])
+def test_numbers_that_do_not_fit_the_descriptor_are_refused(name):
+    """2^32 and more would become small numbers in a 32-bit field: another window, rows that are not computed."""
+    q = torch.zeros(6, 2, 16, device=DEV).half()
+    out, lse = torch.full_like(q, 7.0), torch.zeros(2, 6, device=DEV)
+    for value in (2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 32):
+        with pytest.raises(ValueError):
+            samo.samo_attention(q, q, q, out, lse, **{name: value})
+        with pytest.raises(ValueError):
+            samo.samo_attention_backward(q, q, q, q, out, lse, out, out, out, **{name: value})
+    assert torch.all(out == 7.0)
