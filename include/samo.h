@@ -488,7 +488,8 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  *   G = X Wg^T,  U = X Wu^T,  h = act(G) U;      dG = dh U act'(G),  dU = dh act(G),  dX = dG Wg + dU Wu
  * The weights' gradients are samo_wgrad_gather's with dY = dG or dU (one call for both: samo_wgrad_gather_batched).
  * d_x: tokens x in, d_w_gate and d_w_up: ffn x in (the dense w of a layer, with explicit zeros), everything else tokens x ffn, dX tokens x in;
- * row-major fp16, 16-byte aligned.  in and ffn are multiples of 8 below 2^20, tokens below 2^31; tokens 0 does nothing.
+ * row-major fp16, 16-byte aligned.  in and ffn are multiples of 8 below 2^20, tokens below 2^31 (fewer, SAMO_ERR_SIZE, where a launch would
+ * hold 2^32 threads: a result of 2^35 elements does); tokens 0 does nothing.
  * Sums are fp32 in a fixed order.  samo_glu forms h from the sums, rounded once; d_gate and d_up, both or neither, receive G and U
  * rounded once, for samo_glu_backward, which reads them.  d_dx may be NULL (no dX wanted).  With relu a positive G is kept as 2^-24, fp16's smallest
  * number, where it would round to zero: the slope is that of the sum which h was formed from.  (That sum is the fp32 one: where the exact sum

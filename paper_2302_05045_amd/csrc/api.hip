@@ -1319,8 +1319,6 @@ namespace {
 samo_status check_glu(int64_t tokens, int64_t in, int64_t ffn, int32_t act)
 {
     if (tokens < 0 || tokens > INT32_MAX || in < 8 || ffn < 8 || in % 8 || ffn % 8 || in >= 1 << 20 || ffn >= 1 << 20) return SAMO_ERR_SIZE;
-    // a launch's workgroups: the smallest tiles, the most parts
-    if (ceil_div(tokens, 128) * ceil_div(in > ffn ? in : ffn, 64) > INT32_MAX / (2 * kGluMaxSplits)) return SAMO_ERR_SIZE;
     return act >= SAMO_ACT_SILU && act <= SAMO_ACT_RELU ? SAMO_OK : SAMO_ERR_ARG;
 }
 
@@ -1341,6 +1339,7 @@ samo_status samo_glu(const uint16_t *d_x, const uint16_t *d_w_gate, const uint16
 {
     if (samo_status s = check_glu(tokens, in, ffn, act)) return s;
     if (tokens == 0) return SAMO_OK;
+    if (!glu_fits(tokens, in, ffn)) return SAMO_ERR_SIZE;
     if (!d_x || !d_w_gate || !d_w_up || !d_h || !d_gate != !d_up) return SAMO_ERR_NULL;
     if (misaligned(d_x) || misaligned(d_w_gate) || misaligned(d_w_up) || misaligned(d_h) || misaligned(d_gate) || misaligned(d_up)) return SAMO_ERR_ALIGN;
     GluArgs a;
@@ -1361,7 +1360,11 @@ samo_status samo_glu_workspace_bytes(int64_t tokens, int64_t in, int64_t ffn, si
 {
     if (!bytes) return SAMO_ERR_NULL;
     if (samo_status s = check_glu(tokens, in, ffn, SAMO_ACT_SILU)) return s;
-    *bytes = tokens ? glu_workspace(tokens, in, glu_dx_shape(tokens, ffn, in, kGluMaxSplits)) : 0;
+    *bytes = 0;
+    if (tokens == 0) return SAMO_OK;
+    const GluShape shape = glu_dx_shape(tokens, ffn, in, kGluMaxSplits);
+    if (!glu_backward_fits(tokens, in, ffn, shape)) return SAMO_ERR_SIZE;
+    *bytes = glu_workspace(tokens, in, shape);
     return SAMO_OK;
 }
 
@@ -1390,6 +1393,7 @@ samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, cons
     a.ffn = (int)ffn;
     GluShape shape = glu_dx_shape(tokens, ffn, in, kGluMaxSplits);
     if (!d_workspace || workspace_bytes < glu_workspace(tokens, in, shape)) shape = glu_dx_shape(tokens, ffn, in, 1);
+    if (!glu_backward_fits(tokens, in, ffn, shape)) return SAMO_ERR_SIZE;
     a.partial = static_cast<float *>(d_workspace);
     return hip_status(launch_glu_backward(act, a, shape, as_stream(stream)));
 }

@@ -282,6 +282,9 @@ struct GluShape {
 };
 // The tile shape of dX and the parts its summation is split into, at most max_splits.
 GluShape glu_dx_shape(int64_t tokens, int64_t ffn, int64_t in, int max_splits);
+// Whether the launches of a call, its sizes otherwise in order, can be made.
+bool glu_fits(int64_t tokens, int64_t in, int64_t ffn);
+bool glu_backward_fits(int64_t tokens, int64_t in, int64_t ffn, const GluShape &shape);
 hipError_t launch_glu(int act, const GluArgs &a, hipStream_t s);
 hipError_t launch_glu_backward(int act, GluArgs a, const GluShape &shape, hipStream_t s);
 

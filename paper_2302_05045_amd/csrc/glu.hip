@@ -530,6 +530,23 @@ GluShape glu_dx_shape(int64_t tokens, int64_t ffn, int64_t in, int max_splits)
     return best;
 }
 
+// Whether the launches of a call can be made: the runtime counts a launch's threads in 32 bits.
+bool glu_fits(int64_t tokens, int64_t in, int64_t ffn)
+{
+    if (tokens <= kGluSkinny) return true;
+    const TileShape &t = kShapes[glu_shape(tokens, ffn, in)];
+    return ceil_div(tokens, t.tokens) * ceil_div(ffn, t.side / 2) <= (int64_t)(UINT32_MAX / kGluThreads - 8);
+}
+
+bool glu_backward_fits(int64_t tokens, int64_t in, int64_t ffn, const GluShape &shape)
+{
+    const TileShape &t = kShapes[shape.shape];
+    // eight elements to a thread in glu_pointwise_kernel, and in glu_sum_kernel
+    const int64_t most = (int64_t)(UINT32_MAX - 256) * 8;
+    return tokens * ffn <= most && tokens * in <= most &&
+           ceil_div(tokens, t.tokens) * ceil_div(in, t.side) * shape.splits <= (int64_t)(UINT32_MAX / kGluThreads - 8);
+}
+
 hipError_t launch_glu(int act, const GluArgs &a, hipStream_t s)
 {
     switch (act) {

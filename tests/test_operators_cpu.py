@@ -255,3 +255,19 @@ def test_attention_refuses_results_that_overlap(view):
     # strides of a dimension of one element are not looked at
     assert forward(out=samo.Heads(FAKE, 0, 64), q_tokens=1) == OK and forward(out=samo.Heads(FAKE, 64, 0), heads=1, kv_heads=1) == OK
     assert back(dk=samo.Heads(FAKE, 64, 0), kv_heads=1) == OK and back(dk=samo.Heads(FAKE, 0, 64), k_tokens=1) == OK
+
+
+def test_glu_refuses_more_threads_than_a_launch_holds():
+    L = samo.lib()
+    forward = lambda tokens, fin, ffn: L.samo_glu(FAKE, FAKE, FAKE, tokens, fin, ffn, 0, FAKE, None, None, None)
+    back = lambda tokens, fin, ffn: L.samo_glu_backward(FAKE, FAKE, FAKE, FAKE, FAKE, tokens, fin, ffn, 0, FAKE, FAKE, FAKE, None, 0, None)
+    need = ctypes.c_size_t()
+    assert forward(2 ** 27, 8, 2048) == SIZE                   # 2^19 by 16 tiles of 512 threads
+    assert back(2 ** 24, 8, 2048) == SIZE                      # 2^35 elements, eight to a thread
+    assert back(2 ** 27, 4096, 8) == SIZE and L.samo_glu_workspace_bytes(2 ** 27, 4096, 8, ctypes.byref(need)) == SIZE     # of dX: 2^19 by 16
+    samo.samo_debug_set(samo.KNOB_GLU_SHAPE, 3)
+    try:
+        assert forward(2 ** 24, 8, 2048) == SIZE               # 2^17 by 64 tiles of 128 tokens x 32 features
+    finally:
+        samo.samo_debug_set(samo.KNOB_GLU_SHAPE)
+    assert L.samo_glu_workspace_bytes(2 ** 24, 8, 2040, ctypes.byref(need)) == OK
