@@ -1086,7 +1086,8 @@ samo_status plan8_sizes(const samo_layer8 *h_layers, int32_t num_layers, Plan8Si
     }
     z->rounds = step8_rounds(segments);
     for (int32_t l = 0; l < num_layers; ++l) (h_layers[l].seg_ptr ? z->pruned : z->dense) += recs_of(h_layers[l], z->rounds);
-    if (z->pruned > INT32_MAX || z->dense > INT32_MAX) return SAMO_ERR_SIZE;      // a launch's workgroups
+    constexpr int64_t most = UINT32_MAX / kStep8Threads;         // a launch's threads are counted in 32 bits
+    if (z->pruned > most || z->dense > most) return SAMO_ERR_SIZE;
     z->layers_bytes = (size_t)ceil_div((int64_t)num_layers * (int64_t)sizeof(samo_layer8), 256) * 256;
     z->bytes = z->layers_bytes + (size_t)(z->pruned + z->dense) * sizeof(uint64_t);
     return SAMO_OK;

@@ -271,3 +271,14 @@ def test_glu_refuses_more_threads_than_a_launch_holds():
     finally:
         samo.samo_debug_set(samo.KNOB_GLU_SHAPE)
     assert L.samo_glu_workspace_bytes(2 ** 24, 8, 2040, ctypes.byref(need)) == OK
+
+
+def test_plan8_refuses_more_threads_than_a_launch_holds():
+    """Unpruned layers have a workgroup of 256 threads for every four segments: 32 of the largest are 2^24."""
+    L = samo.lib()
+    need, plan = ctypes.c_size_t(), samo.Plan8Desc()
+    n = 2 ** 31 - 1
+    layers = (samo.Layer8Desc * 32)(*[layer8(n=n, nnz=n, idx=None, seg_ptr=None) for _ in range(32)])
+    assert L.samo_plan8_workspace_bytes(layers, 31, ctypes.byref(need)) == OK
+    assert L.samo_plan8_workspace_bytes(layers, 32, ctypes.byref(need)) == SIZE
+    assert L.samo_plan8_init(layers, 32, FAKE, 1 << 40, None, ctypes.byref(plan)) == SIZE
