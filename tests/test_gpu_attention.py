@@ -422,3 +422,55 @@ def test_numbers_that_do_not_fit_the_descriptor_are_refused(name):
         with pytest.raises(ValueError):
             samo.samo_attention_backward(q, q, q, q, out, lse, out, out, out, **{name: value})
     assert torch.all(out == 7.0)
+
+
+@pytest.mark.parametrize("parts", [1, 3], indirect=True)
+@pytest.mark.parametrize("heads,kv,lens", [(25, 25, [130, 40, 257]), (50, 25, [129, 1, 200]), (67, 67, [300])])
+def test_heads_that_do_not_divide_among_the_xcds(heads, kv, lens, parts):
+    """More than 64 heads and sequences, not a multiple of 8: the last XCD has fewer, and some of a launch's workgroups none."""
+    check(lens, [n + 7 for n in lens], heads, kv, 64, True, 0, seed=heads)
+    check(lens, lens, heads, kv, 128, False, 0, seed=heads + 1)
+
+
+def within_bounds(q, k, v, do, scale, seen, out=None, dq=None, dk=None, dv=None):
+    """One head's results element by element, as in check()."""
+    r, b = reference(q, k, v, do, scale, seen)
+    for name, got, most in (("out", out, 1.25), ("dq", dq, 3.0), ("dk", dk, 3.0), ("dv", dv, 3.0)):
+        if got is not None:
+            d = (got.double() - r[name]).abs()
+            bound = most * U * b[name] + U * r[name].abs() + 2.0 ** -25
+            assert torch.all(d <= bound), (name, float((d - bound).max()))
+
+
+@pytest.mark.parametrize("room", [None, 0, 4 * 2 * 2000])
+def test_parts_and_no_memory_for_them_element_by_element(room):
+    """With the memory for parts and without it: every element of out and of the gradients."""
+    q, k, v, do = (torch.randn(2000, 2, 64, device=DEV).half() for _ in range(4))
+    out, dq, dk, dv = (torch.full_like(q, float("nan")) for _ in range(4))
+    lse = torch.zeros(2, 2000, device=DEV)
+    ws = None if room is None else torch.empty(room, dtype=torch.uint8, device=DEV)
+    samo.samo_attention(q, k, v, out, lse, workspace=ws)
+    samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv, workspace=ws if room else None)
+    for h in range(2):
+        within_bounds(*(t[:, h] for t in (q, k, v, do)), 0.125, seen_of(2000, 2000, True, 0), out[:, h], dq[:, h], dk[:, h], dv[:, h])
+
+
+@pytest.mark.parametrize("n,apart", [(700, 1 << 21), (200, 1 << 24)])
+def test_rows_past_two_gibibytes_backward(n, apart):
+    """Every tensor a slice whose rows lie so far apart that the last ones begin past 2^31 bytes, read and written."""
+    dim = 64
+    room = torch.full((n, apart), float("nan"), dtype=torch.float16, device=DEV)
+    q, k, v, do, out, dq, dk, dv = (room[:, 64 * i:64 * i + dim].unsqueeze(1) for i in range(8))
+    near = [torch.randn(n, 1, dim, device=DEV).half() for _ in range(4)]
+    for far, t in zip((q, k, v, do), near):
+        far.copy_(t)
+    lse = torch.zeros(1, n, device=DEV)
+    samo.samo_attention(q, k, v, out, lse)
+    samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv)
+    a, b, c, d, lse2 = *(torch.zeros_like(t) for t in near), torch.zeros(1, n, device=DEV)
+    samo.samo_attention(*near[:3], a, lse2)
+    samo.samo_attention_backward(near[3], *near[:3], a, lse2, b, c, d)
+    assert torch.equal(lse, lse2)
+    for far, t in zip((out, dq, dk, dv), (a, b, c, d)):
+        assert torch.equal(far, t)
+    assert torch.isnan(room[:, 512:520]).all()

@@ -301,3 +301,48 @@ def test_training_with_8_bit_states_follows_32_bits():
                 samo.samo_fused_step(g, w, None, None, p, m, v, 1 / 64, cfg)
         losses.append(float(((p - target) ** 2).mean()))
     assert losses[1] <= max(1e-3, 4 * losses[0]), losses
+
+
+def test_every_code_is_stored_as_it_was_read():
+    """All codes of both states that a block can hold (the largest in the range of its scale), in blocks of ordinary and of extreme scales: unpack, pack, compare."""
+    code_m = np.concatenate([np.arange(0, 120), np.arange(128, 248)])               # below 2^8 units, both signs and zeros
+    code_v = np.concatenate([np.arange(0, 248), np.full(8, 247)])                   # below 1
+    scales = np.array([[1, 32], [7, 60], [100, 100], [127, 127], [200, 200], [246, 253]], np.uint8)
+    n = 1024 * len(scales)
+    rng = np.random.default_rng(5)
+    q8 = np.empty((n, 2), np.uint8)
+    for s in range(len(scales)):
+        q8[1024 * s:1024 * (s + 1), 0] = rng.permutation(np.resize(code_m, 1024))
+        q8[1024 * s:1024 * (s + 1), 1] = rng.permutation(np.resize(code_v, 1024))
+    d = Dev(n, np.arange(n), np.zeros(n, np.float32))
+    d.q8.copy_(torch.from_numpy(q8.reshape(-1)))
+    d.s8.copy_(torch.from_numpy(scales.reshape(-1)))
+    samo.samo_state8_unpack(d.layer())
+    rm, rv = ref.decode(q8.reshape(-1), scales.reshape(-1), np.arange(n))
+    assert np.array_equal(d.m.cpu().numpy(), rm.astype(np.float32)) and np.array_equal(d.v.cpu().numpy(), rv.astype(np.float32))
+    d.q8.fill_(9), d.s8.fill_(9)
+    samo.samo_state8_pack(d.layer())
+    assert np.array_equal(d.s8.cpu().numpy().reshape(-1, 2), scales)
+    assert np.array_equal(d.q8.cpu().numpy().reshape(-1, 2), q8)
+
+
+@pytest.mark.parametrize("which,least", [(0, 2.0 ** -16), (1, 2.0 ** -32)])
+def test_stochastic_rounding_of_each_state(which, least):
+    """m and v by themselves: the mean over K seeds is within 5 standard errors, a code's gap being 2^-3 of the value or the step of the block's smallest numbers
+    (m: 2^-9 of units of which the largest has 2^7 and more, v: 2^-33 of units of which it has 1/2), and 16 random bits resolve 2^-16 of a gap."""
+    n, K = 1024, 400
+    idx, g, p = make(n, 1.0, 18, True)
+    g = (np.abs(g) + np.float16(0.5)).astype(np.float16)
+    d = Dev(n, idx, p, True)
+    d.set_grad(g)
+    total = torch.zeros(n, dtype=torch.float64, device=DEV)
+    for seed in range(K):
+        d.q8.zero_(), d.s8.zero_()
+        samo.samo_step8(d.layer(), INV, samo.adam_cfg(1, **CFG), 1000 + seed)
+        samo.samo_state8_unpack(d.layer())
+        total += (d.v if which else d.m).double()
+    got = (total / K).cpu().numpy()
+    g32 = g.astype(np.float32) * np.float32(INV)
+    want = ((g32 * np.float32(1 - float(np.float32(0.999)))) * g32 if which else g32 * np.float32(1 - float(np.float32(0.9)))).astype(np.float64)
+    gap = np.maximum(want * 2.0 ** -3, want.max() * least)
+    assert np.all(np.abs(got - want) <= 5 * gap / 2 / np.sqrt(K) + gap * 2.0 ** -16 + want * 2.0 ** -22)
