@@ -491,9 +491,9 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * row-major fp16, 16-byte aligned.  in and ffn are multiples of 8 below 2^20, tokens below 2^31 (fewer, SAMO_ERR_SIZE, where a launch would
  * hold 2^32 threads: a result of 2^35 elements does); tokens 0 does nothing.
  * Sums are fp32 in a fixed order.  samo_glu forms h from the sums, rounded once; d_gate and d_up, both or neither, receive G and U
- * rounded once, for samo_glu_backward, which reads them.  d_dx may be NULL (no dX wanted).  With relu a positive G is kept as 2^-24, fp16's smallest
- * number, where it would round to zero: the slope is that of the sum which h was formed from.  (That sum is the fp32 one: where the exact sum
- * is nearer to zero than its roundings it may be on the other side.)
+ * rounded once, for samo_glu_backward, which reads them; dX is formed from dG and dU as they are stored, rounded.  d_dx may be NULL (no dX wanted).
+ * relu: a positive G that would round to zero is kept as 2^-24, fp16's smallest number, so that the slope is that of the sum which h was formed
+ * from.  (That sum is fp32: where the exact one is nearer to zero than its roundings it may be on the other side.)
  * A G beyond fp16's range is kept as an infinity, at which the backward pass takes the limits of act' (0 and 1) and of act (0 and infinity).
  * samo_glu_workspace_bytes: what samo_glu_backward can use on the current device for layers with few tiles of dX (fp32 sums of parts
  * of the summation); with less, or NULL, it does without.  In use until the stream has passed the call. */

@@ -208,8 +208,8 @@ __device__ __forceinline__ Place place_of(int of_head, int tile, int part, const
 }
 // The workgroup's place.  The tiles that see the most go first, of all heads and sequences, so that a launch ends with short workgroups.  An XCD gets
 // the same heads of every tile, whose other side stays in its L2, or, where few heads and sequences do not divide evenly among
-// the XCDs, what comes next.  All tiles of a head together / this, us, forward and backward: 8192 causal tokens in 4
-// sequences, 32 heads of 64, 117 and 378 / 91 and 303; of 80 184 and 555 / 151 and 493; in one sequence, 32 heads of 128 on 8, 600 and 2035 / 576 and 1934.
+// the XCDs, what comes next.  All tiles of a head together / this, us on one card, forward and backward: 8192 causal tokens in 4
+// sequences, 32 heads of 64, 122 and 378 / 100 and 317; of 80 163 and 509 / 140 and 481; in one sequence, 32 heads of 128 on 8, 608 and 2094 / 598 and 2052.
 __device__ __host__ inline int heads_an_xcd(int all) { return all % 8 == 0 || all >= 64 ? (all + 7) / 8 : 0; }       // 0: what comes next
 __device__ __forceinline__ bool pick(const AttnArgs &A, int heads, Place &p)
 {
@@ -286,9 +286,9 @@ __device__ __forceinline__ void key_range(const Mask &M, int q0, int q1, int k_l
 }
 
 // The forward pass.  Four waves of 32 queries: with two tiles of keys and values in LDS two workgroups fit a compute unit up to heads of 128, which is
-// what covers the copies' latency and the softmax of one by the products of the other.  8192 causal tokens, 32 heads of 128 on 8: 590 us,
-// 930 TFLOP/s, bound by the chip's power (zeros: 1240); two sequences of 4096, not causal, 950; 4 x 2048 causal, 32 heads of 80:
-// 159 us, 540 (80 is padded to 96 in the second product; 17 tiles a workgroup pay for its start and for what lies behind the diagonal in two).
+// what covers the copies' latency and the softmax of one by the products of the other.  8192 causal tokens, 32 heads of 128 on 8: 595 us,
+// 920 TFLOP/s, bound by the chip's power (zeros: 1230); two sequences of 4096, not causal, 935; 4 x 2048 causal, 32 heads of 80:
+// 140 to 153 us by card, 600 (80 is padded to 96 in the second product; 17 tiles a workgroup pay for its start and for what lies behind the diagonal in two).
 template <int KS>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnArgs A)
 {
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     if (lane < 32 && query < seq.q_len) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : top * A.scale + __logf(sum);
 }
 
-// dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 840 us, 980 TFLOP/s; 4 x 2048, 32 heads of 80: 200 us.
+// dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 825 us, 1000 TFLOP/s; 4 x 2048, 32 heads of 80: 180 us.
 template <int KS>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const AttnArgs A)
 {
@@ -496,7 +496,7 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 // have the same keys, one takes the first 32 queries of every tile and the other the last, and their sums meet in LDS at the end: a workgroup's time
 // counts as much as the device's, under a causal mask the first keys are seen by every query (8192 tokens, 32 heads of 128, 8 of keys: with
 // four waves the longest of 512 workgroups took 1.8 ms by itself; the whole backward pass 2414 -> 2090 us).
-// Four products a tile: 1300 us for those 8192 tokens, 845 TFLOP/s; 4 x 2048, 32 heads of 80 (one wave to its keys): 270 us.
+// Four products a tile: 1220 us for those 8192 tokens, 900 TFLOP/s; 4 x 2048, 32 heads of 80 (one wave to its keys): 240 us.
 // Two waves to a SIMD have 256 registers each.  Heads of more than 96 fill half of them with their sums: there the rows of V stay in LDS, from where
 // they are read for every block.
 template <int KS, int SIDES>
@@ -722,9 +722,9 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
 }
 
 // The workgroups of dK and dV from which a wave has its keys for itself; below, where the longest workgroup is what the call waits for, two share them.
-// Whole backward pass of heads of 64, one wave / two, us: 32 workgroups, 512 tokens of 8 heads 33 / 30; 256, 2048 of 16 heads 80 / 78; 512,
-// two times 2048 of 32 heads 68 / 68; 512, 16384 of 16 heads on 4 2118 / 2240; 1024, 8192 in 16 sequences of 16 heads 77 / 90; 2048, 8192 of 32
-// heads 1078 / 1150.  Of 80: 1024 workgroups 100 / 120, 2048 1479 / 1581, but 512 long ones 3910 / 3105; of 96 108 / 126, 1588 / 1665, 4150 / 3350.
+// Whole backward pass of heads of 64, one wave / two, us: 32 workgroups, 512 tokens of 8 heads 31 / 29; 256, 2048 of 16 heads 76 / 75; 512,
+// two times 2048 of 16 heads 111 / 103; 512, 16384 of 16 heads on 4 2108 / 2204; 1024, 8192 in 16 sequences of 16 heads 73 / 86; 2048, 8192 of 32
+// heads 1064 / 1132.  Of 80: 1024 workgroups 94 / 113, 2048 1395 / 1495, but 512 long ones 3651 / 2935; of 96 101 / 120, 1506 / 1584, 3947 / 3105.
 // Heads of more than 96 always share: V's rows in LDS leave room for one workgroup.
 constexpr int one_side_from(int dim) { return dim <= 64 ? 512 : dim <= 96 ? 1024 : INT32_MAX; }
 
@@ -772,10 +772,10 @@ int64_t sums_bytes(int which, const AttnArgs &a, int splits)
 // What a launch costs with its keys (for dK and dV: queries) in so many parts, us.  A workgroup works through tiles of 64; the device's share of all of them,
 // and as the launch ends half the longest workgroup besides; the longest one by itself; and for parts a second kernel and the sums, written and read.
 // A tile by itself takes 1.25 us with heads of 64 and 1.5 with 128, 1.4 and 2.3 where two workgroups share a compute unit; the backward pass's
-// a quarter more.  Measured against the parts taken, whole calls, us: one token behind 8192, 32 heads of 128, 180 with one part, 38 with 8, 34 with 16; 2000 tokens
-// in 3 sequences behind 3000 each, 16 heads of 64, 71 and 57 with three; 4096 tokens, 8 heads of 128, 89 and 60 with three; 1024 tokens of
-// 16 heads of 96 24 and 26 with two; 2048 in 4 sequences, 16 heads of 64, 13 and 24 with two; one token each behind 8 contexts of 2048, 32 heads of
-// 128, 54 and 36 with two.
+// a quarter more.  Measured against the parts taken, whole calls, us: one token behind 8191, 32 heads of 128 on 8, 181 with one part, 36 with 8, 33 with 16;
+// 2000 tokens in 3 sequences behind 3000 each, 16 heads of 64, 72 and 57 with three; 4096 tokens, 8 heads of 128, 89 and 59 with three; 1024 tokens of
+// 16 heads of 96 23 and 25 with two, which it takes; 2048 in 4 sequences, 16 heads of 64, 13 and 23 with two; one token each behind 8 contexts of 2048, 32 heads of
+// 128, 62, 50 with two and 57 with four.
 // Where every workgroup has as much to do, the rounds that they take count whole.
 double launch_us(int which, const AttnArgs &a, int64_t items, int splits)
 {
@@ -803,8 +803,8 @@ int splits_of(int which, const AttnArgs &a)
     const int64_t items = items_of(which, a), forced = knob(SAMO_KNOB_ATTENTION_SPLIT, -1);
     if (items == 0) return 1;
     if (forced > 0) return (int)std::max<int64_t>(1, std::min<int64_t>({kMost, forced, (1 << 21) / items}));       // a launch holds 2^23 workgroups and more
-    // Two rounds of the device are even enough: the longest workgroups come first (8192 tokens, 32 heads of 128, 8 of keys: dK and dV 1350 us as they are, 1500
-    // in two parts; forward 597 and 674).
+    // Two rounds of the device are even enough: the longest workgroups come first (8192 tokens, 32 heads of 128, 8 of keys: forward 574 us as they are and 660
+    // in two parts, backward 1983 and 2107).
     if (items >= (which == kDkv && a.dim > 64 ? 2 : 4) * compute_units()) return 1;
     int best = 1;
     double least = launch_us(which, a, items, 1);

@@ -2,7 +2,8 @@
 // and two weight matrices of ffn x in, dense fp16 with explicit zeros as the expansion leaves them (Section III-C):
 //   G = X Wg^T,  U = X Wu^T,  h = act(G) U
 //   dG = dh U act'(G),  dU = dh act(G),  dX = dG Wg + dU Wu          (dWg = dG^T X and dWu = dU^T X are samo_wgrad_gather's)
-// Products of fp16 with fp32 sums; G and U are rounded once to fp16 where they are kept for the backward pass, h is formed from the sums.
+// Products of fp16 with fp32 sums; G and U are rounded once to fp16 where they are kept for the backward pass, h is formed from the sums.  dG and dU are formed
+// in fp32 from those and rounded to fp16: the weight gradients take them as fp16, and dX's products, which fp32 would make 16 times as slow, the same numbers.
 //
 // Bound by the matrix units from a few hundred tokens on, by the weights' bytes below.
 //  - glu_kernel: a tile of 256 tokens by 128 features of both G and U (128 by 128, 64 or 32 for calls of few tiles), which so meet in one
@@ -202,6 +203,8 @@ __device__ __forceinline__ bool pick_tile(int tiles_t, int tiles_f, int copies, 
     return true;
 }
 
+// G, U and h.  8192 tokens, 4096 x 10928: 1214 us, 1210 TFLOP/s, bound by the chip's power; 2048, 2560 x 6832: 157 us, 910 (432 tiles in two rounds of
+// the compute units); 1003, 1024 x 2736: 26 us (176 tiles, fewer than there are compute units).
 template <int AB, int BB, int STEPS, int ACT>
 __global__ void __launch_bounds__(kGluThreads, 2) glu_kernel(const GluArgs A)
 {
@@ -264,7 +267,8 @@ __global__ void __launch_bounds__(kGluThreads, 2) glu_kernel(const GluArgs A)
     }
 }
 
-// dX: 64 BB tokens x 32 AB columns by a workgroup, over the part of the summation that is its own.
+// dX: 64 BB tokens x 32 AB columns by a workgroup, over the part of the summation that is its own.  8192 tokens, 4096 x 10928: 1304 us, 1125 TFLOP/s; 2048,
+// 2560 x 6832, in three parts: 146 us, 980, and 12 for the sums.
 template <int AB, int BB, int STEPS>
 __global__ void __launch_bounds__(kGluThreads, 2) glu_dx_kernel(const GluArgs A)
 {
@@ -348,6 +352,7 @@ __global__ void __launch_bounds__(256) glu_sum_kernel(const float *partial, int 
     *reinterpret_cast<half8 *>(dx + at) = x;
 }
 
+// dG and dU: bound by HBM, 190 us for 8192 x 10928 (895 MB, 4.7 TB/s), 23.8 for 2048 x 6832.
 template <int ACT>
 __global__ void __launch_bounds__(256) glu_pointwise_kernel(const _Float16 *dh, const _Float16 *gate, const _Float16 *up, _Float16 *dgate, _Float16 *dup, int64_t n)
 {
@@ -371,7 +376,8 @@ __global__ void __launch_bounds__(256) glu_pointwise_kernel(const _Float16 *dh, 
 
 // Up to 16 NB tokens: a workgroup of eight waves has 16 features of G and of U, a wave every eighth 128 bytes of the rows, two steps of 32 at a time,
 // the loads of kAhead such pairs on their way together.  The waves' sums are added up by halves in LDS.  Bound by the weights' bytes: 2560 x 6832
-// (70 MB), one token 17.6 us; 16 23.4, 32 29.3, where the tiles take 28.6 (and this kernel for 64 tokens 32 to 40).
+// (70 MB), one token 17.9 us, 3.9 TB/s: 427 workgroups, two on some compute units and one on others, and of a wave's two trips the second is a quarter
+// full; 16 tokens 22.4, 32 28.7, where the tiles take 28.5 (and this kernel for 64 tokens 32 to 40).
 constexpr int kSkinnyWaves = 8;
 template <int NB, int ACT>
 __global__ void __launch_bounds__(64 * kSkinnyWaves, 2) glu_skinny_kernel(const GluArgs A)

@@ -307,7 +307,8 @@ __device__ __forceinline__ int group_bounds(const samo_layer8 &L, int64_t group,
     return bound < 0 ? 0 : bound > (int)L.nnz ? (int)L.nnz : bound;
 }
 
-// WIDE: for layers that keep a fifth and more, whose blocks pass 256 elements: twice the registers, four workgroups to a compute unit.
+// WIDE: for layers that keep a fifth and more, whose blocks pass 256 elements: twice the registers, four workgroups to a compute unit.  Bound by HBM: 24
+// blocks of the 350M shape, 10 % kept, 273 to 325 us by card (5.2 to 6.2 TB/s); 400 M elements, 25 % kept 595 us, 50 % 885 (5.4).
 template <bool WIDE>
 __global__ void __launch_bounds__(kStep8Threads, WIDE ? 4 : 6) step8_pruned_kernel(const Step8Launch ls, const Step8Args A)
 {
@@ -341,7 +342,8 @@ __global__ void __launch_bounds__(kStep8Threads, WIDE ? 4 : 6) step8_pruned_kern
     }
 }
 
-// Unpruned layers: position = entry; a lane has eight consecutive elements of either half of the segment.
+// Unpruned layers: position = entry; a lane has eight consecutive elements of either half of the segment.  206 M elements: 527 to 606 us by card, 6.3 to 5.4
+// TB/s.
 __global__ void __launch_bounds__(kStep8Threads, 4) step8_dense_kernel(const Step8Launch ls, const Step8Args A)
 {
     bool skip;
@@ -431,7 +433,8 @@ __global__ void __launch_bounds__(kStep8Threads, 4) step8_dense_kernel(const Ste
     if (lane == 0) *reinterpret_cast<uint16_t *>(L.s8 + 2 * seg) = (uint16_t)(sm | sv << 8);
 }
 
-// m and v in 32 bits from the codes; a wave to a segment, whose first 128 elements are asked for before the last round's are stored.
+// m and v in 32 bits from the codes; a wave to a segment, whose first 128 elements are asked for before the last round's are stored.  10 % kept of 400 M elements
+// 93 us, 4.3 TB/s (a segment's 102 elements are short rows), 50 % 568, 3.5; 206 M unpruned 356 to 382.
 __global__ void __launch_bounds__(kStep8Threads) unpack8_kernel(const Step8Launch ls)
 {
     samo_layer8 L;
@@ -502,7 +505,7 @@ __global__ void __launch_bounds__(kStep8Threads) unpack8_kernel(const Step8Launc
     }
 }
 
-// The codes from m and v, rounded to nearest; a wave to a segment.
+// The codes from m and v, rounded to nearest; a wave to a segment, read twice.  Not on a step's path: 10 % kept of 400 M elements 139 us, 2.9 TB/s, 50 % 582, 3.5.
 __global__ void __launch_bounds__(kStep8Threads) pack8_kernel(const Step8Launch ls)
 {
     samo_layer8 L;
