@@ -17,9 +17,9 @@
 //    rows by one piece and 4 rows by 64 bytes, over all banks.
 //  - Workgroups of a head go to one of the 8 XCDs, where they share its other side in the L2 (pick()).
 // P and dS are rounded to fp16 for the products they enter, as Q, K, V and dO are: 2^-11 of themselves; statistics and all sums are fp32.  (fp32 products
-// have a sixteenth of the rate.)  delta is fp32 of out as it is in memory, rounded: out in 32 bits would be twice the bytes, and the rounding is no larger than that of dS.  dS is rounded as
-// it is, without the scale that dQ and dK take at the end: with a scale of 2^-3 or less in it, the dS of thousands of keys, 2^-10 and less where dO is near 1,
-// would be among fp16's subnormal numbers and lose bits, for a range above 65504 in which a loss scale is too large anyway.
+// have a sixteenth of the rate.)  delta is fp32, of out as memory has it, rounded: an error no larger than that of dS.  dS is rounded without the scale
+// that dQ and dK take at the end: with 2^-3 or less in it, the dS of thousands of keys, 2^-10 and less where dO is near 1, would be among fp16's
+// subnormal numbers and lose bits, for a range above 65504 in which a loss scale is too large anyway.
 // dQ and dK, dV are formed by two kernels, each of which forms S and dP: 7 products for the 5 that one kernel would need, but every
 // sum has one owner and one order, so the same call gives the same bits (with additions to dQ in memory it would not).
 #include "common.h"
