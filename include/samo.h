@@ -483,6 +483,42 @@ samo_status samo_attention_sums_bytes(const samo_attention_desc *h_desc, int32_t
 samo_status samo_attention_workspace_bytes(const samo_attention_desc *h_desc, size_t *bytes);
 samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------- attention with scores of another form
+ * The same attention, forward and backward, whose scores are not plain products: capped by a tanh, falling with the distance, with a learned bias
+ * by the bucket of the distance, or with keys that every query sees.  With i counted from the sequence's end as for the causal mask,
+ *   d = i + k_len - q_len - j,   x = scale q k^T,   z = cap tanh(x / cap) - slope[h] |d| + table[h][column(d)],   out = softmax(z) v,  lse = log sum exp z
+ * each part where it is given:
+ *   cap             0: none; otherwise 2^-10 to 2^20
+ *   d_slopes        float[heads], finite
+ *   d_table         fp16[heads * columns], head by head, finite; d_borders int32[buckets - 1], ascending from 1 or more: a distance's bucket is the number
+ *                   of borders up to it.  1 to SAMO_ATTENTION_MAX_BUCKETS buckets.  two_sided == 0: columns = buckets, column(d) = bucket(max(d, 0));
+ *                   otherwise columns = 2 buckets, column(d) = bucket(d) and, where the key lies behind (d < 0), buckets + bucket(-d).
+ *                   (Borders that do not ascend give other buckets, never a column outside the table.)
+ *   d_first_keys    int32[batch], with causal only: query i sees key j also if j < first_keys[s], whatever the window (from 0 to k_len counts).
+ * Backward: dz = P (dP - delta), dS = dz (1 - (cap tanh(x / cap) / cap)^2) enters dq and dk, and
+ *   d_dtable        fp16[heads * columns] or NULL: the sums of dz over the pairs of every column, rounded once; all of it is written, columns of no pair
+ *                   as zero.  With a loss scale in dout it is the scaled gradient, as any g.
+ * Sums of dz are fp32 within 32 queries of a part, double over those; their order is fixed.  The slopes are constants and have no gradient.
+ * tanh is within 2^-22 of itself where |x| is up to 5/8 of the cap and within 2^-22 elsewhere (and, with a cap up to 128, at a score whose block of 32
+ * queries and 32 keys has such a one).  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
+ * Everything else, alignment and limits, is as for samo_attention; slopes, borders and first_keys 4-byte, table and dtable 2-byte aligned.
+ * samo_attention_scored_workspace_bytes: what the backward call needs (delta, and for d_dtable the parts of its sums) on the current device. */
+#define SAMO_ATTENTION_MAX_BUCKETS 64
+typedef struct {
+    float cap;
+    const float *d_slopes;
+    const uint16_t *d_table;
+    const int32_t *d_borders;
+    int32_t buckets, two_sided;
+    const int32_t *d_first_keys;
+    uint16_t *d_dtable;                              /* backward only */
+} samo_attention_scores;
+samo_status samo_attention_scored(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, void *stream);
+samo_status samo_attention_scored_sums_bytes(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, int32_t backward, size_t *bytes);
+samo_status samo_attention_scored_workspace_bytes(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, size_t *bytes);
+samo_status samo_attention_scored_backward(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, void *d_workspace,
+                                           size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- gated feed-forward block
  * The two up-projections of a gated block, its activation and the product in one kernel, and its backward pass:
  *   G = X Wg^T,  U = X Wu^T,  h = act(G) U;      dG = dh U act'(G),  dU = dh act(G),  dX = dG Wg + dU Wu

@@ -33,6 +33,8 @@ SAMO_OK = 0
 (SAMO_ERR_NULL, SAMO_ERR_SIZE, SAMO_ERR_ARG, SAMO_ERR_WORKSPACE, SAMO_ERR_ALIGN, SAMO_ERR_INDEX, SAMO_ERR_HIP,
  SAMO_ERR_PLAN) = -1, -2, -3, -4, -5, -6, -7, -8
 
+ATTENTION_MAX_BUCKETS = 64
+
 # samo_debug_set knobs
 (KNOB_OCC_TILE_STEP, KNOB_OCC_TILE_STEP32, KNOB_OCC_TILE_DECOMP, KNOB_OCC_TILE_C16, KNOB_OCC_FLAT_GATHER,
  KNOB_OCC_FLAT_STATS, KNOB_OCC_FLAT_STEP, KNOB_INDEX_SPIN_LIMIT, KNOB_WGRAD_TILE, KNOB_WGRAD_ROUND,
@@ -115,6 +117,12 @@ class AttentionDesc(ctypes.Structure):
                 ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
                 ("d_sums", ctypes.c_void_p), ("sums_bytes", ctypes.c_size_t)]
+
+
+class ScoresDesc(ctypes.Structure):
+    """samo_attention_scores"""
+    _fields_ = [("cap", ctypes.c_float), ("d_slopes", ctypes.c_void_p), ("d_table", ctypes.c_void_p), ("d_borders", ctypes.c_void_p),
+                ("buckets", ctypes.c_int32), ("two_sided", ctypes.c_int32), ("d_first_keys", ctypes.c_void_p), ("d_dtable", ctypes.c_void_p)]
 
 
 class StepGuard(ctypes.Structure):
@@ -215,6 +223,13 @@ _SIGNATURES = {
     "samo_state8_pack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
     "samo_state8_unpack_batched": (ctypes.c_int32, [ctypes.POINTER(Plan8Desc), ctypes.c_void_p]),
     "samo_attention": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_void_p]),
+    "samo_attention_scored": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ScoresDesc), ctypes.c_void_p]),
+    "samo_attention_scored_sums_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ScoresDesc), ctypes.c_int32,
+                                                          ctypes.POINTER(ctypes.c_size_t)]),
+    "samo_attention_scored_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ScoresDesc),
+                                                               ctypes.POINTER(ctypes.c_size_t)]),
+    "samo_attention_scored_backward": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ScoresDesc), ctypes.c_void_p,
+                                                        ctypes.c_size_t, ctypes.c_void_p]),
     "samo_attention_sums_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_int32,
                                                    ctypes.POINTER(ctypes.c_size_t)]),
     "samo_attention_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
@@ -1141,12 +1156,77 @@ def _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, 
     return d
 
 
-def _attention_sums(d: AttentionDesc, backward: bool, workspace: Optional[torch.Tensor], used: int) -> Optional[torch.Tensor]:
+class Scores(NamedTuple):
+    """The form of attention's scores where they are not plain products (samo_attention_scores):
+    z = cap tanh(scale q k / cap) - slopes[head] |d| + table[head, column(d)], d the distance i - j counted from the sequence's end.
+
+    cap: 0 for none.  slopes: float32 (heads).  table: float16 (heads, buckets), with two_sided (heads, 2 * buckets), the second half for keys that lie
+    behind the query; borders: int32 (buckets - 1), the distances at which the next bucket begins (samo_bucket_borders; None for one bucket).
+    first_keys: int32 (sequences), causal only: so many keys at a sequence's begin are seen by all of its queries."""
+    cap: float = 0.0
+    slopes: Optional[torch.Tensor] = None
+    table: Optional[torch.Tensor] = None
+    borders: Optional[torch.Tensor] = None
+    two_sided: bool = False
+    first_keys: Optional[torch.Tensor] = None
+
+
+def samo_bucket_borders(buckets: int, far: int, device="cuda") -> Optional[torch.Tensor]:
+    """Borders of `buckets` buckets of a direction: one distance a bucket up to half of them, then by equal steps of the logarithm up to `far`, so that
+    a distance n from half on has bucket half + floor(log(n / half) / log(far / half) * (buckets - half)), at most the last.  Found in whole numbers."""
+    half = buckets // 2
+    rest = buckets - half
+    if not 1 <= buckets <= ATTENTION_MAX_BUCKETS:
+        raise ValueError("buckets is 1 to %d, not %d" % (ATTENTION_MAX_BUCKETS, buckets))
+    if buckets == 1:
+        return None
+    if not half < far < 2 ** 30:
+        raise ValueError("far = %d: it lies behind the %d buckets of one distance each" % (far, half))
+    borders = list(range(1, half + 1))
+    for t in range(1, rest):                              # the least n with (n / half)^rest >= (far / half)^t
+        n = max(half, int(half * (far / half) ** (t / rest)) - 2)
+        while n ** rest < half ** (rest - t) * far ** t:
+            n += 1
+        borders.append(n)
+    return torch.tensor(borders, dtype=torch.int32, device=device)
+
+
+def _scores_desc(s: Scores, d: AttentionDesc, dtable: Optional[torch.Tensor] = None) -> ScoresDesc:
+    """The descriptor; its tensors' sizes are checked against those of d."""
+    c = ScoresDesc()
+    c.cap, c.two_sided = float(s.cap), int(bool(s.two_sided))
+    if s.slopes is not None:
+        c.d_slopes = _dev(s.slopes, torch.float32, "slopes", d.heads)
+    if s.table is not None:
+        ptr, rows, columns = _dev_matrix(s.table, "table")
+        c.buckets = columns // 2 if s.two_sided else columns
+        if rows != d.heads or (s.two_sided and columns % 2):
+            raise ValueError("table is %d x %d, needs %d rows and%s columns" % (rows, columns, d.heads, " an even number of" if s.two_sided else ""))
+        c.d_table = ptr
+        if s.borders is not None or c.buckets > 1:
+            if s.borders is None or s.borders.numel() != c.buckets - 1:
+                raise ValueError("borders holds one number less than there are buckets, %d" % (c.buckets - 1))
+            c.d_borders = _dev(s.borders, torch.int32, "borders")
+        if dtable is not None:
+            c.d_dtable = _dev_matrix_of(dtable, "dtable", rows, columns)
+    elif s.borders is not None or dtable is not None:
+        raise ValueError("borders and dtable belong to a table")
+    if s.first_keys is not None:
+        c.d_first_keys = _dev(s.first_keys, torch.int32, "first_keys", d.batch)
+    return c
+
+
+def _attention_sums(d: AttentionDesc, backward: bool, workspace: Optional[torch.Tensor], used: int,
+                    scores: Optional[ScoresDesc] = None) -> Optional[torch.Tensor]:
     """Gives d the sums' memory behind the first `used` bytes of the workspace, which is taken from torch's allocator if there is none."""
     used = (used + 15) // 16 * 16
     if workspace is None:
         need = ctypes.c_size_t()
-        _check(lib().samo_attention_sums_bytes(ctypes.byref(d), backward, ctypes.byref(need)), "samo_attention_sums_bytes")
+        if scores is None:
+            _check(lib().samo_attention_sums_bytes(ctypes.byref(d), backward, ctypes.byref(need)), "samo_attention_sums_bytes")
+        else:
+            _check(lib().samo_attention_scored_sums_bytes(ctypes.byref(d), ctypes.byref(scores), backward, ctypes.byref(need)),
+                   "samo_attention_scored_sums_bytes")
         workspace = _capture_scratch(used + need.value) if used + need.value else None
         if workspace is None and used:                    # without the sums the call does, without the rest it does not
             workspace = _capture_scratch(used)
@@ -1159,8 +1239,8 @@ def samo_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
                    causal: bool = True, window: int = 0, scale: Optional[float] = None,
                    q_start: Optional[torch.Tensor] = None, k_start: Optional[torch.Tensor] = None,
                    max_q: Optional[int] = None, max_k: Optional[int] = None,
-                   workspace: Optional[torch.Tensor] = None) -> None:
-    """out = softmax(scale q k^T + mask) v and lse, its rows' log-sum-exp, over packed sequences.
+                   workspace: Optional[torch.Tensor] = None, scores: Optional[Scores] = None) -> None:
+    """out = softmax(scale q k^T + mask) v and lse, its rows' log-sum-exp, over packed sequences; with `scores`, of scores of that form.
 
     q, out: (tokens, heads, dim), k, v: (tokens, kv_heads, dim) fp16, strided as slices of a packed projection are; lse: float32
     (heads, tokens).  q_start, k_start: int32 (sequences + 1) on the GPU, the sequences' first tokens; none: one sequence.
@@ -1169,6 +1249,11 @@ def samo_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
     Few heads and rows split the keys over workgroups, whose sums meet in the workspace (uint8; in use until the stream has passed the
     call; too few bytes, or an empty one: not split).  Without one the call takes what it can use from torch's allocator."""
     d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)
+    if scores is not None:
+        c = _scores_desc(scores, d)
+        workspace = _attention_sums(d, False, workspace, 0, c)
+        _check(lib().samo_attention_scored(ctypes.byref(d), ctypes.byref(c), _stream()), "samo_attention_scored")
+        return
     workspace = _attention_sums(d, False, workspace, 0)
     _check(lib().samo_attention(ctypes.byref(d), _stream()), "samo_attention")
 
@@ -1177,17 +1262,29 @@ def samo_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor
                             lse: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, causal: bool = True,
                             window: int = 0, scale: Optional[float] = None, q_start: Optional[torch.Tensor] = None,
                             k_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None,
-                            max_k: Optional[int] = None, workspace: Optional[torch.Tensor] = None) -> None:
-    """dq, dk, dv of samo_attention with the same arguments, from dout and what the forward pass left in out and lse.
+                            max_k: Optional[int] = None, workspace: Optional[torch.Tensor] = None, scores: Optional[Scores] = None,
+                            dtable: Optional[torch.Tensor] = None) -> None:
+    """dq, dk, dv of samo_attention with the same arguments, from dout and what the forward pass left in out and lse; with the table of `scores`
+    also dtable (float16, as the table; None: not wanted), all of which is written.
 
-    workspace (uint8, 4 * heads * tokens bytes; more, from the next multiple of 16, for the sums of calls of few heads and rows) is in use until the
-    stream has passed the call; without one the call takes it from torch's allocator."""
+    workspace (uint8, 4 * heads * tokens bytes, with dtable samo_attention_scored_workspace_bytes; more, from the next multiple of 16, for the sums of calls
+    of few heads and rows) is in use until the stream has passed the call; without one the call takes it from torch's allocator."""
     d = _attention_desc(q, k, v, out, lse, scale, causal, window, q_start, k_start, max_q, max_k)
     like_q, like_k = (d.q_tokens, d.heads, d.dim), (d.k_tokens, d.kv_heads, d.dim)
     _set_heads(d, "dout", dout, *like_q)
     _set_heads(d, "dq", dq, *like_q)
     _set_heads(d, "dk", dk, *like_k)
     _set_heads(d, "dv", dv, *like_k)
+    if scores is not None:
+        c, need = _scores_desc(scores, d, dtable), ctypes.c_size_t()
+        _check(lib().samo_attention_scored_workspace_bytes(ctypes.byref(d), ctypes.byref(c), ctypes.byref(need)), "samo_attention_scored_workspace_bytes")
+        workspace = _attention_sums(d, True, workspace, need.value, c)
+        _check(lib().samo_attention_scored_backward(ctypes.byref(d), ctypes.byref(c), _dev(workspace, torch.uint8, "workspace"),
+                                                    workspace.numel() if workspace is not None else 0, _stream()),
+               "samo_attention_scored_backward")
+        return
+    if dtable is not None:
+        raise ValueError("dtable belongs to the table of scores")
     workspace = _attention_sums(d, True, workspace, 4 * d.q_tokens * d.heads)
     _check(lib().samo_attention_backward(ctypes.byref(d), _dev(workspace, torch.uint8, "workspace"),
                                          workspace.numel() if workspace is not None else 0, _stream()),

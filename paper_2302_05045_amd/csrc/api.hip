@@ -1316,6 +1316,95 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
 
 }  // extern "C"
 
+// ---------------------------------------------------------------- attention with scores of another form
+namespace {
+
+constexpr float kLeastCap = 1.f / 1024.f, kMostCap = 1048576.f;     // what keeps scale / cap and cap log2(e) inside fp32
+
+samo_status check_scores(const samo_attention_scores *s, bool backward, AttnArgs *a)
+{
+    if (!s) return SAMO_ERR_NULL;
+    if (s->cap != 0.f && !(s->cap >= kLeastCap && s->cap <= kMostCap)) return SAMO_ERR_ARG;
+    if ((reinterpret_cast<uintptr_t>(s->d_slopes) | reinterpret_cast<uintptr_t>(s->d_borders) | reinterpret_cast<uintptr_t>(s->d_first_keys)) & 3u)
+        return SAMO_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(s->d_table) | reinterpret_cast<uintptr_t>(s->d_dtable)) & 1u) return SAMO_ERR_ALIGN;
+    if (s->d_table) {
+        if (s->buckets < 1 || s->buckets > SAMO_ATTENTION_MAX_BUCKETS) return SAMO_ERR_SIZE;
+        if (s->buckets > 1 && !s->d_borders) return SAMO_ERR_NULL;
+    } else if (backward && s->d_dtable) return SAMO_ERR_NULL;
+    if (s->d_first_keys && !a->causal) return SAMO_ERR_ARG;
+    a->scored = 1;
+    a->form.cap = s->cap;
+    a->form.slopes = s->d_slopes;
+    a->form.table = reinterpret_cast<const _Float16 *>(s->d_table);
+    a->form.borders = s->d_borders;
+    a->form.buckets = s->d_table ? s->buckets : 0;
+    a->form.two_sided = s->two_sided != 0;
+    a->form.first_keys = s->d_first_keys;
+    a->form.dtable = backward ? reinterpret_cast<_Float16 *>(s->d_dtable) : nullptr;
+    return SAMO_OK;
+}
+
+samo_status scored_workspace(const AttnArgs &a, size_t *delta, size_t *bytes)
+{
+    *delta = ((size_t)a.heads * (size_t)a.q_tokens * sizeof(float) + 15) / 16 * 16;
+    const size_t table = (size_t)attention_table_bytes(a);
+    *bytes = table > 0 ? *delta + table : (size_t)a.heads * (size_t)a.q_tokens * sizeof(float);
+    return SAMO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+samo_status samo_attention_scored(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, void *stream)
+{
+    AttnArgs a;
+    if (samo_status s = check_attention(h_desc, false, &a)) return s;
+    if (samo_status s = check_scores(h_scores, false, &a)) return s;
+    if (overlaps(h_desc->out, a.q_tokens, a.heads, a.dim)) return SAMO_ERR_SIZE;
+    return hip_status(launch_attention(a, h_desc->sums_bytes, as_stream(stream)));
+}
+
+samo_status samo_attention_scored_sums_bytes(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, int32_t backward, size_t *bytes)
+{
+    if (!bytes) return SAMO_ERR_NULL;
+    AttnArgs a;
+    if (samo_status s = check_attention(h_desc, backward != 0, &a)) return s;
+    if (samo_status s = check_scores(h_scores, backward != 0, &a)) return s;
+    *bytes = (size_t)attention_sums_bytes(a, backward != 0);
+    return SAMO_OK;
+}
+
+samo_status samo_attention_scored_workspace_bytes(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, size_t *bytes)
+{
+    if (!bytes) return SAMO_ERR_NULL;
+    AttnArgs a;
+    size_t delta = 0;
+    if (samo_status s = check_attention(h_desc, true, &a)) return s;
+    if (samo_status s = check_scores(h_scores, true, &a)) return s;
+    return scored_workspace(a, &delta, bytes);
+}
+
+samo_status samo_attention_scored_backward(const samo_attention_desc *h_desc, const samo_attention_scores *h_scores, void *d_workspace,
+                                           size_t workspace_bytes, void *stream)
+{
+    AttnArgs a;
+    size_t need = 0, delta = 0;
+    if (samo_status s = check_attention(h_desc, true, &a)) return s;
+    if (samo_status s = check_scores(h_scores, true, &a)) return s;
+    if (overlaps(h_desc->dq, a.q_tokens, a.heads, a.dim) || overlaps(h_desc->dk, a.k_tokens, a.kv_heads, a.dim) || overlaps(h_desc->dv, a.k_tokens, a.kv_heads, a.dim))
+        return SAMO_ERR_SIZE;
+    if (samo_status s = scored_workspace(a, &delta, &need)) return s;
+    if (need > 0 && (!d_workspace || workspace_bytes < need)) return SAMO_ERR_WORKSPACE;
+    if (misaligned(d_workspace)) return SAMO_ERR_ALIGN;
+    a.delta = static_cast<float *>(d_workspace);
+    if (a.form.dtable) a.form.dtable_parts = reinterpret_cast<float *>(static_cast<unsigned char *>(d_workspace) + delta);
+    return hip_status(launch_attention_backward(a, h_desc->sums_bytes, as_stream(stream)));
+}
+
+}  // extern "C"
+
 // ---------------------------------------------------------------- gated feed-forward block
 namespace {
 

@@ -235,25 +235,24 @@ __device__ __forceinline__ void leave(float *parts, int64_t slot, int wave, int 
         for (int g = 0; g < 4; ++g) to[(4 * db + g) * 64] = f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
 }
 
-// A part's share of the tiles first .. end: whole tiles of 64, in order.
-__device__ __forceinline__ void share_of(const AttnArgs &A, int part, int &first, int &end)
-{
-    const int tiles = end > first ? (end - first + kTileRows - 1) / kTileRows : 0, each = (tiles + A.splits - 1) / A.splits;
-    first += min(tiles, part * each) * kTileRows;
-    end = min(end, first + each * kTileRows);
-}
-
 // Which keys a query sees: first_key(query) .. end_key(query) - 1, all of them without `causal`; and which queries see a key.
 struct Mask {
     bool causal;
     int shift, window, q_len, k_len;         // window 2^30: none
+    int first;                               // the first keys that every query sees; 0 but with causal
     __device__ __forceinline__ int first_key(int query) const { return causal ? query + shift - window + 1 : 0; }
     __device__ __forceinline__ int end_key(int query) const { return causal ? min(query + shift + 1, k_len) : k_len; }
-    __device__ __forceinline__ int first_query(int key) const { return causal ? key - shift : 0; }
-    __device__ __forceinline__ int end_query(int key) const { return causal ? min(key - shift + window, q_len) : q_len; }
+    __device__ __forceinline__ int first_query(int key) const { return causal && key >= first ? key - shift : 0; }
+    __device__ __forceinline__ int end_query(int key) const { return causal && key >= first ? min(key - shift + window, q_len) : q_len; }
     // whether all of / any of a block of queries and keys (first and last of each) are seen
-    __device__ __forceinline__ bool all(int q0, int q1, int k0, int k1) const { return k1 < k_len && (!causal || (k1 <= q0 + shift && k0 > q1 + shift - window)); }
-    __device__ __forceinline__ bool any(int q0, int q1, int k0, int k1) const { return !causal || (k0 <= q1 + shift && k1 > q0 + shift - window); }
+    __device__ __forceinline__ bool all(int q0, int q1, int k0, int k1) const
+    {
+        return k1 < k_len && (!causal || k1 < first || (k1 <= q0 + shift && k0 > q1 + shift - window));
+    }
+    __device__ __forceinline__ bool any(int q0, int q1, int k0, int k1) const
+    {
+        return !causal || k0 < first || (k0 <= q1 + shift && k1 > q0 + shift - window);
+    }
 };
 // The numbers from .. end - 1 by one comparison.
 struct Span {
@@ -262,9 +261,11 @@ struct Span {
     __device__ __forceinline__ Span(int first, int end) : from(first), count(end > first ? (unsigned)(end - first) : 0u) {}
     __device__ __forceinline__ bool holds(int x) const { return (unsigned)(x - from) < count; }
 };
-__device__ __forceinline__ Mask mask_of(const AttnArgs &A, const Sequence &s)
+template <bool SCORED>
+__device__ __forceinline__ Mask mask_of(const AttnArgs &A, const Sequence &s, int b)
 {
     Mask m;
+    m.first = SCORED && A.causal && A.form.first_keys ? min(max(A.form.first_keys[b], 0), s.k_len) : 0;
     m.causal = A.causal != 0;
     m.shift = s.k_len - s.q_len;
     m.window = A.window > 0 ? min(A.window, 1 << 30) : 1 << 30;
@@ -273,33 +274,297 @@ __device__ __forceinline__ Mask mask_of(const AttnArgs &A, const Sequence &s)
     return m;
 }
 
-// The tiles of keys that any of the queries q0 .. q1 sees: [first, end) in rows, first a multiple of the tile.
-__device__ __forceinline__ void key_range(const Mask &M, int q0, int q1, int k_len, int &first, int &end)
-{
-    first = 0;
-    end = k_len;
-    if (M.causal) {
-        const int last = q1 + M.shift + 1, begin = q0 + M.shift - M.window + 1;
-        end = last < end ? last : end;
-        first = begin > 0 ? begin / kTileRows * kTileRows : 0;
+// A part's share of the tiles of keys that any of the queries q0 .. q1 sees: those of the first keys, then from what the window leaves on.
+struct KeyTiles {
+    int first, count, head, near;            // the first tile's first row; the tiles; the end of the first keys' tiles and where the others begin, in rows
+    __device__ __forceinline__ KeyTiles(const AttnArgs &A, const Mask &M, int q0, int q1, int part)
+    {
+        int end = M.k_len, begin = 0;
+        if (M.causal) {
+            end = min(end, max(q1 + M.shift + 1, M.first));
+            begin = max(q0 + M.shift - M.window + 1, 0) / kTileRows * kTileRows;
+        }
+        head = (M.first + kTileRows - 1) / kTileRows * kTileRows;
+        near = max(begin, head);
+        const int heads = head / kTileRows, all = heads + (end > near ? (end - near + kTileRows - 1) / kTileRows : 0), each = (all + A.splits - 1) / A.splits;
+        const int from = min(all, part * each);
+        count = min(all - from, each);
+        first = from < heads ? from * kTileRows : near + (from - heads) * kTileRows;
     }
+    __device__ __forceinline__ int after(int k0) const { return k0 + kTileRows == head ? near : k0 + kTileRows; }
+};
+
+// Scores of another form (SCORED): z = cap tanh(x / cap) + bias(d), x the scaled product.  All of it in units of `unit` and log 2: a product, or its tanh,
+// and a bias are added and enter the exponent by the same multiplication as a plain product.  Without a cap the bias is what the matrix instructions
+// start from, so that it costs the making of its 16 registers; with one it is added behind the tanh.  Biases of a block of queries and keys, whose
+// distances are those of its diagonals, come in three kinds:
+//   kSame    one number, where all distances have one bucket: nothing to do for an element (most blocks of long sequences)
+//   kLinear  a slope, the block on one side of the diagonal: one multiplication and addition for each element
+//   kLaid    anything: the wave works out its diagonals' biases, a lane each, and lays them into LDS
+// The table's columns and borders live in the wave's lanes: the bucket of a distance that the lanes agree on is the number of set bits of a comparison.
+constexpr int kMaxBuckets = SAMO_ATTENTION_MAX_BUCKETS;
+enum { kSame, kLinear, kLaid };
+struct Bias {
+    int kind, column;                        // column: of all the block's pairs, the second half behind kMaxBuckets; -1 where they differ
+    int diagonal;                            // where they differ: of the lane's diagonal, row - column + 31 (blocks of 32 rows)
+    float same, step, base;                  // kSame; kLinear: from row to row, and at the lane's first
+};
+struct Form {
+    bool capped, tabled, biased, two_sided;
+    float unit, into, small, slope;          // into: scale / cap; small: the largest product that the tanh's polynomial is for
+    int border;                              // lane l: where bucket l + 1 begins
+    float past, ahead;                       // lane l: the bias of bucket l, and where the key lies behind
+    __device__ __forceinline__ Form(const AttnArgs &A, int head)
+    {
+        const int lane = threadIdx.x & 63;
+        const AttnForm &F = A.form;
+        capped = F.cap > 0.f;
+        unit = (capped ? F.cap : A.scale) * kLog2e;
+        const float of_bias = capped ? 1.f / F.cap : 1.f / A.scale;
+        into = capped ? A.scale / F.cap : 0.f;
+        small = capped ? kSmall / into : 0.f;
+        slope = F.slopes ? F.slopes[head] * of_bias : 0.f;
+        tabled = F.table != nullptr;
+        biased = tabled || F.slopes;
+        two_sided = F.two_sided != 0;
+        const int columns = two_sided ? 2 * F.buckets : F.buckets;
+        const _Float16 *table = F.table + (int64_t)head * columns;
+        border = tabled && lane < F.buckets - 1 ? min(max(F.borders[lane], 0), kFar) : kFar;
+        past = tabled && lane < F.buckets ? (float)table[lane] * of_bias : 0.f;
+        ahead = tabled && two_sided && lane < F.buckets ? (float)table[F.buckets + lane] * of_bias : 0.f;
+    }
+    static constexpr int kFar = 1 << 30;     // behind every distance
+    __device__ __forceinline__ int away(int d) const { return two_sided ? abs(d) : max(d, 0); }      // a distance as the buckets count it
+    __device__ __forceinline__ int bucket(int away) const { return __builtin_popcountll(__ballot(border <= away)); }
+    // tanh(t) of t = scale x / cap, two ways.  For |t| up to kSmall t times a polynomial in t^2, the one of its degree whose largest relative error is least
+    // (1.1e-7; found by exchange).  Anywhere: sign (1 - e) / (1 + e), e = exp(-2 |t|), within 2^-22, which is much for the small scores beside a
+    // large one where the cap is large: there each element takes its own.
+    static constexpr float kSmall = 0.625f, kMuchCap = 128.f * kLog2e;
+    __device__ __forceinline__ float tanh_small(float x) const
+    {
+        const float t = x * into, u = t * t;
+        return t * fmaf(fmaf(fmaf(fmaf(0.0150509449f, u, -0.0518218651f), u, 0.133045256f), u, -0.333319545f), u, 0.999999881f);
+    }
+    __device__ __forceinline__ float tanh_any(float x) const
+    {
+        const float e = __builtin_amdgcn_exp2f(fabsf(x) * (-2.f * kLog2e * into));
+        return copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x);
+    }
+    __device__ __forceinline__ f32x16 tanhs(f32x16 s) const
+    {
+        float most = fabsf(s[0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, fabsf(s[i]));
+        if (!__ballot(most > small)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = tanh_small(s[i]);
+        } else if (unit <= kMuchCap) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = tanh_any(s[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = fabsf(s[i]) <= small ? tanh_small(s[i]) : tanh_any(s[i]);
+        }
+        return s;
+    }
+    // The biases of a block of ROWS rows and 32 columns, d = base + SIGN (row - column).
+    template <int ROWS, int SIGN>
+    __device__ __forceinline__ Bias plan(float *room, int base) const
+    {
+        Bias b = {kSame, -1, -1, 0.f, 0.f, 0.f};
+        if (!biased) return b;
+        const int lane = threadIdx.x & 63, lo = SIGN > 0 ? base - 31 : base - (ROWS - 1), hi = SIGN > 0 ? base + ROWS - 1 : base + 31;
+        int b0 = 0, b1 = 0;
+        if (tabled) {
+            const bool one_side = !two_sided || lo >= 0 || hi < 0, behind = two_sided && hi < 0;
+            b0 = bucket(behind ? -hi : max(lo, 0));
+            b1 = bucket(two_sided ? max(-lo, hi) : max(hi, 0));
+            if (one_side && b0 == b1) {
+                b.column = behind ? kMaxBuckets + b0 : b0;
+                if (slope == 0.f) {
+                    b.same = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, behind ? ahead : past), b0));
+                    return b;
+                }
+            }
+        } else if (lo >= 0 || hi <= 0) {
+            const float down = lo >= 0 ? -slope : slope;
+            b.kind = kLinear;
+            b.step = SIGN * down;
+            b.base = down * (float)(base - SIGN * ((lane & 31) - 4 * (lane >> 5)));
+            return b;
+        }
+        b.kind = kLaid;
+#pragma unroll
+        for (int part = 0; part < (ROWS + 31 + 63) / 64; ++part) {
+            const int e = part * 64 + lane, d = base + SIGN * (e - 31), n = away(d);
+            float bias = -slope * fabsf((float)d);
+            if (tabled) {
+                int at = b0;
+                for (int i = b0; i < b1; ++i) at += n >= __builtin_amdgcn_readlane(border, i);
+                const int before = __builtin_amdgcn_ds_bpermute(4 * at, __builtin_bit_cast(int, past)), behind = __builtin_amdgcn_ds_bpermute(4 * at, __builtin_bit_cast(int, ahead));
+                bias += __builtin_bit_cast(float, two_sided && d < 0 ? behind : before);
+                if (part == 0) b.diagonal = two_sided && d < 0 ? kMaxBuckets + at : at;
+            }
+            if (e < ROWS + 31) room[e] = bias;
+        }
+        __builtin_amdgcn_wave_barrier();
+        return b;
+    }
+    // Those of rows 32 block .. (not kSame), as an accumulator holds them.
+    __device__ __forceinline__ f32x16 biases(const Bias &b, const float *room, int block) const
+    {
+        f32x16 x;
+        const float *at = room + 31 + 32 * block - (int)(threadIdx.x & 31);
+        if (b.kind == kLinear) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = fmaf(b.step, (float)(32 * block + 8 * (i >> 2) + (i & 3)), b.base);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = at[acc_row(i)];
+        }
+        return x;
+    }
+    // What the products' sums start from, and what becomes of them.
+    __device__ __forceinline__ bool starts(const Bias &b) const { return b.kind != kSame && !capped; }
+    __device__ __forceinline__ f32x16 scores(f32x16 s, const Bias &b, const float *room, int block) const
+    {
+        if (!capped) return s;
+        s = tanhs(s);
+        if (b.kind != kSame) {
+            const f32x16 x = biases(b, room, block);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] += x[i];
+        }
+        return s;
+    }
+};
+constexpr int kBiasRoom = 96;                // floats of a wave's biases
+struct NoForm {};
+template <bool SCORED>
+__device__ __forceinline__ auto form_of(const AttnArgs &A, int head)
+{
+    if constexpr (SCORED) return Form(A, head);
+    else return NoForm{};
 }
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) x += __shfl_xor(x, step);
+    return x;
+}
+// x of the lanes up to this one that have its column, added; lanes of a column are neighbours.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ void scan_step(float &x, int column)
+{
+    const float other = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, ROWS, 0xf, false));
+    x += __builtin_amdgcn_update_dpp(-1, column, CONTROL, ROWS, 0xf, false) == column ? other : 0.f;
+}
+__device__ __forceinline__ float scan_of_column(float x, int column)
+{
+    scan_step<0x111, 0xf>(x, column);        // one lane to the right within rows of 16, two, four, eight
+    scan_step<0x112, 0xf>(x, column);
+    scan_step<0x114, 0xf>(x, column);
+    scan_step<0x118, 0xf>(x, column);
+    scan_step<0x142, 0xa>(x, column);        // a row's last lane to the next row; the second row's to the third and fourth
+    scan_step<0x143, 0xc>(x, column);
+    return x;
+}
+__device__ __forceinline__ float of_lane(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * lane, __builtin_bit_cast(int, x))); }
+
+// The table's gradient: lane l holds the sums of dS over the pairs of bucket l so far.  A block whose pairs have one column adds to its lanes' own sums, which meet
+// when the column changes.  Of another one the diagonals are added: half of its rows at a time go to LDS, each shifted by its number, so that a
+// diagonal is a column; rows keep their places, and what is beside them zero.  A scan over the lanes of a bucket's diagonals leaves its sum in their last.
+constexpr int kSkewed = 47, kSkewRoom = 16 * kSkewed;
+struct BucketSums {
+    float past = 0.f, ahead = 0.f, run = 0.f;
+    int column = 0;
+    __device__ __forceinline__ void start(float *room) const
+    {
+        for (int i = threadIdx.x & 63; i < kSkewRoom; i += 64) room[i] = 0.f;
+        __builtin_amdgcn_wave_barrier();
+    }
+    __device__ __forceinline__ void flush()
+    {
+        const float sum = wave_sum(run);
+        const int lane = threadIdx.x & 63;
+        past += lane == column ? sum : 0.f;
+        ahead += lane + kMaxBuckets == column ? sum : 0.f;
+        run = 0.f;
+    }
+    __device__ __forceinline__ void add(const Form &F, const f32x16 &ds, const Bias &b, float *room, int base)       // d = base - row + column
+    {
+        const int lane = threadIdx.x & 63;
+        if (b.column >= 0) {
+            if (b.column != column) {
+                flush();
+                column = b.column;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) run += ds[i];
+            return;
+        }
+        const int half = lane >> 5, col = min(lane, kSkewed - 1);
+        float *to = room + 4 * half * (kSkewed + 1) + 31 - (lane & 31);
+        float diagonal[2];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[(8 * (i >> 2) + (i & 3)) * (kSkewed + 1)] = ds[8 * part + i];
+            __builtin_amdgcn_wave_barrier();
+            float sum = 0.f;
+#pragma unroll
+            for (int row = 0; row < 16; ++row) sum += room[row * kSkewed + col];
+            __builtin_amdgcn_wave_barrier();
+            diagonal[part] = lane < kSkewed ? sum : 0.f;
+        }
+        const float second = of_lane(diagonal[1], lane - 16);
+        const float sums = scan_of_column(diagonal[0] + (lane >= 16 ? second : 0.f), b.diagonal);     // lane: row - column + 31
+        const int zero = base + 31;                                                       // the lane of distance 0
+        const int before = __shfl_up(F.border, 1), begin = lane == 0 ? 0 : before, end = F.border;       // of the lane's bucket
+        auto last_of = [&](int from, int to) {                                            // the sum of lanes from .. to
+            to = min(to, 62);
+            const float sum = of_lane(sums, to);
+            return max(from, 0) <= to ? sum : 0.f;
+        };
+        if (zero >= 0 || !F.two_sided) past += last_of(zero - end + 1, lane == 0 && !F.two_sided ? 62 : zero - begin);
+        if (zero < 62 && F.two_sided) ahead += last_of(zero + max(begin, 1), zero + end - 1);
+    }
+    // all waves' sums, one float a column
+    __device__ __forceinline__ void leave(const Form &F, int buckets, float (*meeting)[2 * kMaxBuckets], float *to)
+    {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, columns = F.two_sided ? 2 * buckets : buckets;
+        flush();
+        if (lane < buckets) {
+            meeting[wave][lane] = past;
+            if (F.two_sided) meeting[wave][buckets + lane] = ahead;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < columns) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kAttnThreads / 64; ++w) sum += meeting[w][threadIdx.x];
+            to[threadIdx.x] = sum;
+        }
+    }
+};
 
 // The forward pass.  Four waves of 32 queries: with two tiles of keys and values in LDS two workgroups fit a compute unit up to heads of 128, which is
 // what covers the copies' latency and the softmax of one by the products of the other.  8192 causal tokens, 32 heads of 128 on 8: 595 us,
 // 920 TFLOP/s, bound by the chip's power (zeros: 1230); two sequences of 4096, not causal, 935; 4 x 2048 causal, 32 heads of 80:
 // 140 to 153 us by card, 600 (80 is padded to 96 in the second product; 17 tiles a workgroup pay for its start and for what lies behind the diagonal in two).
-template <int KS>
+template <int KS, bool SCORED>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnArgs A)
 {
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
+    __shared__ float biases[SCORED ? kAttnThreads / 64 : 1][kBiasRoom];
     Place at;
     if (!pick(A, A.heads, at)) return;
     const int b = at.b, head = at.head, tile = at.tile;
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.q_len) return;
-    const Mask M = mask_of(A, seq);
+    const Mask M = mask_of<SCORED>(A, seq, b);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int q_first = tile * kOwnRows, q_last = min(q_first + kOwnRows, seq.q_len) - 1;
     const int w_first = q_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.q_len) - 1;   // of the wave; none where last < first
@@ -308,48 +573,61 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
     const Tiles<KS> K(Rows{A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim});
     const Tiles<KS> V(Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim});
-    int k_first, k_end;
-    key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
-    share_of(A, at.part, k_first, k_end);
+    const KeyTiles tiles(A, M, q_first, q_last, at.part);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
 
-    if (k_first < k_end) {
-        K.bring(k_first, lds_at);
-        V.bring(k_first, lds_at + 2 * kTile);
+    if (tiles.count > 0) {
+        K.bring(tiles.first, lds_at);
+        V.bring(tiles.first, lds_at + 2 * kTile);
     }
     half8 own[KS];
     load_own<KS>(Q, w_first, own);
     const Span seen(M.first_key(query), M.end_key(query));
     f32x16 out[DB];
     clear(out);
-    const float c = A.scale * kLog2e;
+    [[maybe_unused]] const auto form = form_of<SCORED>(A, head);
+    float c = A.scale * kLog2e;
+    if constexpr (SCORED) c = form.unit;
     float top = -INFINITY, sum = 0.f;                        // top: what the exponents are taken against, within 8 of the largest so far
     int buffer = 0;
-    for (int k0 = k_first; k0 < k_end; k0 += kTileRows, buffer ^= 1) {
+    for (int n = 0, k0 = tiles.first; n < tiles.count; ++n, k0 = tiles.after(k0), buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         meet();                                              // the tile is there, and the other one has been read by every wave
-        if (k0 + kTileRows < k_end) {
-            K.bring(k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
-            V.bring(k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
+        if (n + 1 < tiles.count) {
+            K.bring(tiles.after(k0), lds_at + (buffer ^ 1) * kTile);
+            V.bring(tiles.after(k0), lds_at + (2 + (buffer ^ 1)) * kTile);
         }
         if (w_last < w_first || !M.any(w_first, w_last, k0, k0 + kTileRows - 1)) continue;
         const unsigned char *kt = lds + buffer * kTile, *vt = lds + (2 + buffer) * kTile;
         f32x16 s[2];
         clear(s);
+        [[maybe_unused]] Bias bias;
+        if constexpr (SCORED) {
+            bias = form.template plan<kTileRows, -1>(biases[wave], w_first + M.shift - k0);
+            if (form.starts(bias)) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) s[kb] = form.biases(bias, biases[wave], kb);
+            }
+        }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(kt, kb, ks), own[ks], s[kb], 0, 0, 0);
+        if constexpr (SCORED) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) s[kb] = form.scores(s[kb], bias, biases[wave], kb);
+        }
         if (!M.all(w_first, w_last, k0, k0 + kTileRows - 1)) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[kb][i] = seen.holds(k0 + 32 * kb + acc_row(i)) ? s[kb][i] : -INFINITY;
+                for (int i = 0; i < 16; ++i) s[kb][i] = seen.holds(k0 + 32 * kb + acc_row(i)) || (SCORED && k0 + 32 * kb + acc_row(i) < M.first) ? s[kb][i] : -INFINITY;
         }
         float most = s[0][0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) most = fmaxf(most, s[i >> 4][i & 15]);
         most = fmaxf(most, other_half(most));
+        if constexpr (SCORED) most += bias.same;
         // Only where a row's largest score passes what its exponents are taken against by 2^8 are the sums so far brought down: P stays
         // below 2^8 otherwise, which fp16 holds as well as numbers below 1.
         if (__ballot(most * c > top * c + 8.f)) {
@@ -362,7 +640,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
 #pragma unroll
                 for (int i = 0; i < 16; ++i) out[db][i] *= down;
         }
-        const float against = top == -INFINITY ? 0.f : top * c;       // a row that has seen no key yet
+        float against = top == -INFINITY ? 0.f : top * c;    // a row that has seen no key yet
+        if constexpr (SCORED) against -= bias.same * c;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -386,21 +665,28 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     }
     const float factor = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;      // a row that sees no key: zero; NaN stays
     store_own<DB>(A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, query, seq.q_len, A.dim, out, factor);
-    if (lane < 32 && query < seq.q_len) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : top * A.scale + __logf(sum);
+    if (lane < 32 && query < seq.q_len) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : (SCORED ? top * c * kLn2 : top * A.scale) + __logf(sum);
 }
 
 // dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 825 us, 1000 TFLOP/s; 4 x 2048, 32 heads of 80: 180 us.
-template <int KS>
+template <int KS, bool SCORED>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const AttnArgs A)
 {
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];
+    __shared__ float biases[SCORED ? kAttnThreads / 64 : 1][kBiasRoom];
+    __shared__ float skewed[SCORED ? kAttnThreads / 64 : 1][kSkewRoom];
+    __shared__ float meeting[SCORED ? kAttnThreads / 64 : 1][2 * kMaxBuckets];
     Place at;
     if (!pick(A, A.heads, at)) return;
     const int b = at.b, head = at.head, tile = at.tile;
     const Sequence seq = sequence_of(A, b);
-    if (tile * kOwnRows >= seq.q_len) return;
-    const Mask M = mask_of(A, seq);
+    const int columns = SCORED ? (A.form.two_sided ? 2 : 1) * A.form.buckets : 0;
+    if (tile * kOwnRows >= seq.q_len) {                      // nothing to the table's gradient
+        if (SCORED && A.form.dtable_parts && (int)threadIdx.x < columns) A.form.dtable_parts[at.slot * columns + threadIdx.x] = 0.f;
+        return;
+    }
+    const Mask M = mask_of<SCORED>(A, seq, b);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int q_first = tile * kOwnRows, q_last = min(q_first + kOwnRows, seq.q_len) - 1;
     const int w_first = q_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.q_len) - 1;
@@ -411,13 +697,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
     const Tiles<KS> V(Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim});
     const Rows DO = {A.dout + seq.q0 * A.dout_row + head * A.dout_head, A.dout_row, seq.q_len, A.dim};
     const Rows O = {A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, seq.q_len, A.dim};
-    int k_first, k_end;
-    key_range(M, q_first, q_last, seq.k_len, k_first, k_end);
-    share_of(A, at.part, k_first, k_end);
+    const KeyTiles tiles(A, M, q_first, q_last, at.part);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
-    if (k_first < k_end) {
-        K.bring(k_first, lds_at);
-        V.bring(k_first, lds_at + 2 * kTile);
+    if (tiles.count > 0) {
+        K.bring(tiles.first, lds_at);
+        V.bring(tiles.first, lds_at + 2 * kTile);
     }
     half8 own[KS], down[KS];
     load_own<KS>(Q, w_first, own);
@@ -433,7 +717,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
         delta += other_half(delta);
     }
     const int64_t stat = (int64_t)head * A.q_tokens + seq.q0 + query;
-    const float c = A.scale * kLog2e;
+    [[maybe_unused]] const auto form = form_of<SCORED>(A, head);
+    [[maybe_unused]] BucketSums buckets;
+    if (SCORED && A.form.dtable_parts) buckets.start(skewed[wave]);
+    float c = A.scale * kLog2e;
+    if constexpr (SCORED) c = form.unit;
     float lse = 0.f;
     if (query < seq.q_len) {
         lse = A.lse[stat] * kLog2e;
@@ -443,12 +731,12 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
     f32x16 acc[DB];
     clear(acc);
     int buffer = 0;
-    for (int k0 = k_first; k0 < k_end; k0 += kTileRows, buffer ^= 1) {
+    for (int n = 0, k0 = tiles.first; n < tiles.count; ++n, k0 = tiles.after(k0), buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         meet();
-        if (k0 + kTileRows < k_end) {
-            K.bring(k0 + kTileRows, lds_at + (buffer ^ 1) * kTile);
-            V.bring(k0 + kTileRows, lds_at + (2 + (buffer ^ 1)) * kTile);
+        if (n + 1 < tiles.count) {
+            K.bring(tiles.after(k0), lds_at + (buffer ^ 1) * kTile);
+            V.bring(tiles.after(k0), lds_at + (2 + (buffer ^ 1)) * kTile);
         }
         const unsigned char *kt = lds + buffer * kTile, *vt = lds + (2 + buffer) * kTile;
 #pragma unroll
@@ -458,16 +746,39 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
             f32x16 s[1], dp[1];
             clear(s);
             clear(dp);
+            [[maybe_unused]] Bias bias;
+            float less = lse;
+            if constexpr (SCORED) {
+                bias = form.template plan<32, -1>(biases[wave], w_first + M.shift - k1);
+                if (form.starts(bias)) s[0] = form.biases(bias, biases[wave], 0);
+                less = fmaf(-bias.same, c, lse);
+            }
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(kt, kb, ks), own[ks], s[0], 0, 0, 0);
                 dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(vt, kb, ks), down[ks], dp[0], 0, 0, 0);
             }
+            [[maybe_unused]] f32x16 t;
+            if constexpr (SCORED) {
+                if (form.capped) s[0] = t = form.tanhs(s[0]);
+                if (form.capped && bias.kind != kSame) {
+                    const f32x16 x = form.biases(bias, biases[wave], 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse)) * (dp[0][i] - delta);
+                    for (int i = 0; i < 16; ++i) s[0][i] += x[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -less)) * (dp[0][i] - delta);
             if (!M.all(w_first, w_last, k1, k1 + 31)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[0][i] = seen.holds(k1 + acc_row(i)) ? s[0][i] : 0.f;
+                for (int i = 0; i < 16; ++i) s[0][i] = seen.holds(k1 + acc_row(i)) || (SCORED && k1 + acc_row(i) < M.first) ? s[0][i] : 0.f;
+            }
+            if constexpr (SCORED) {
+                if (A.form.dtable_parts) buckets.add(form, s[0], bias, skewed[wave], w_first + M.shift - k1);
+                if (form.capped) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[0][i] *= fmaf(-t[i], t[i], 1.f);
+                }
             }
 #pragma unroll
             for (int step = 0; step < 2; ++step) {
@@ -479,6 +790,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (SCORED) {
+        if (A.form.dtable_parts) buckets.leave(form, A.form.buckets, meeting, A.form.dtable_parts + at.slot * columns);
+    }
     if (A.splits > 1) leave<DB>(A.parts, at.slot, wave, query, seq.q_len, acc);
     else store_own<DB>(A.dq + seq.q0 * A.dq_row + head * A.dq_head, A.dq_row, query, seq.q_len, A.dim, acc, A.scale);
 }
@@ -499,19 +813,20 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 // Four products a tile: 1220 us for those 8192 tokens, 900 TFLOP/s; 4 x 2048, 32 heads of 80 (one wave to its keys): 240 us.
 // Two waves to a SIMD have 256 registers each.  Heads of more than 96 fill half of them with their sums: there the rows of V stay in LDS, from where
 // they are read for every block.
-template <int KS, int SIDES>
+template <int KS, int SIDES, bool SCORED>
 __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {
     constexpr bool kWide = KS > 6;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide ? kOwnRows * PITCH : 0)];       // Q, dO; two tiles each; V
     __shared__ __attribute__((aligned(16))) float stats[2][2][kTileRows];         // lse, delta
+    __shared__ float biases[SCORED ? SIDES * kAttnThreads / 64 : 1][kBiasRoom];
     Place at;
     if (!pick(A, A.kv_heads, at)) return;
     const int b = at.b, kv = at.head, tile = A.tiles - 1 - at.tile;        // the first keys are seen by the most queries
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.k_len) return;
-    const Mask M = mask_of(A, seq);
+    const Mask M = mask_of<SCORED>(A, seq, b);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, side = wave >> 2;
     const int k_first = tile * kOwnRows, k_last = min(k_first + kOwnRows, seq.k_len) - 1;
     const int w_first = k_first + (wave & 3) * kWaveRows, w_last = min(w_first + kWaveRows, seq.k_len) - 1;
@@ -533,7 +848,7 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
     Coming first_operand = coming_of(side), second_operand = coming_of(1);
     // the queries that see any of the workgroup's keys
     int q_first = 0, q_end = seq.q_len;
-    if (M.causal) {
+    if (M.causal && k_first >= M.first) {
         const int begin = k_first - M.shift;
         q_first = begin > 0 ? begin / kTileRows * kTileRows : 0;
         const int64_t end = (int64_t)k_last - M.shift + M.window;
@@ -565,12 +880,16 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
     f32x16 dk[DB], dv[DB];
     clear(dk);
     clear(dv);
-    const float c = A.scale * kLog2e;
+    // P's exponents by the group's first head; the form of another is taken when its queries come
+    [[maybe_unused]] auto form = form_of<SCORED>(A, kv * A.group + min(shared, A.group - 1));
+    float c = A.scale * kLog2e;
+    if constexpr (SCORED) c = form.unit;
     int buffer = 0;
     for (int n = 0; n < count; ++n, buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         meet();
         const int q0 = q_first + t * kTileRows;
+        if (SCORED && t == 0 && n > 0) form = form_of<SCORED>(A, kv * A.group + shared);
         if (++t == tiles) {
             t = 0;
             ++shared;
@@ -585,21 +904,46 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
             f32x16 s[1], dp[1];
             clear(s);
             clear(dp);
+            [[maybe_unused]] Bias bias;
+            float more = 0.f;
+            if constexpr (SCORED) {
+                bias = form.template plan<32, 1>(biases[wave], q1 + M.shift - w_first);
+                if (form.starts(bias)) s[0] = form.biases(bias, biases[wave], 0);
+                more = bias.same * c;
+            }
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
                 const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
                 dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
             }
+            const float *lse_at = &stats[buffer][0][32 * qb + 4 * (lane >> 5)], *delta_at = &stats[buffer][1][32 * qb + 4 * (lane >> 5)];
+            if constexpr (SCORED) {                          // dP - delta, times the cap's slope
+                if (form.capped) s[0] = form.tanhs(s[0]);
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 delta = *reinterpret_cast<const f32x4 *>(delta_at + 8 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[0][4 * g + e] -= delta[e];
+                }
+                if (form.capped) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dp[0][i] *= fmaf(-s[0][i], s[0][i], 1.f);
+                    if (bias.kind != kSame) {
+                        const f32x16 x = form.biases(bias, biases[wave], 0);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[0][i] += x[i];
+                    }
+                }
+            }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int at = 32 * qb + 8 * g + 4 * (lane >> 5);
-                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][at]), delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][at]);
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(lse_at + 8 * g), delta = *reinterpret_cast<const f32x4 *>(delta_at + 8 * g);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = 4 * g + e;
-                    s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -lse[e] * kLog2e));
-                    dp[0][i] = s[0][i] * (dp[0][i] - delta[e]);
+                    s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, SCORED ? fmaf(-lse[e], kLog2e, more) : -lse[e] * kLog2e));
+                    dp[0][i] = s[0][i] * (SCORED ? dp[0][i] : dp[0][i] - delta[e]);
                 }
             }
             if (!M.all(q1, q1 + 31, w_first, w_last)) {
@@ -721,6 +1065,22 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
     store_own<1>(to + 32 * db, stride, row, count, A.dim - 32 * db, acc, factor);
 }
 
+// The table's gradient: a head's workgroup adds what the workgroups of dQ left, in order, a column to a thread.
+constexpr int kTableThreads = 1024, kTableRows = kTableThreads / (2 * kMaxBuckets);
+__global__ void __launch_bounds__(kTableThreads) table_gradient_kernel(const float *parts, int64_t slots, int columns, _Float16 *to)
+{
+    __shared__ double sums[kTableRows][2 * kMaxBuckets];
+    const int column = threadIdx.x % (2 * kMaxBuckets), row = threadIdx.x / (2 * kMaxBuckets);
+    double sum = 0.0;
+    if (column < columns)
+        for (int64_t at = row; at < slots; at += kTableRows) sum += parts[(blockIdx.x * slots + at) * columns + column];
+    sums[row][column] = sum;
+    __syncthreads();
+    if (row > 0 || column >= columns) return;
+    for (int other = 1; other < kTableRows; ++other) sum += sums[other][column];
+    to[(int64_t)blockIdx.x * columns + column] = (_Float16)(float)sum;
+}
+
 // The workgroups of dK and dV from which a wave has its keys for itself; below, where the longest workgroup is what the call waits for, two share them.
 // Whole backward pass of heads of 64, one wave / two, us: 32 workgroups, 512 tokens of 8 heads 31 / 29; 256, 2048 of 16 heads 76 / 75; 512,
 // two times 2048 of 16 heads 111 / 103; 512, 16384 of 16 heads on 4 2108 / 2204; 1024, 8192 in 16 sequences of 16 heads 73 / 86; 2048, 8192 of 32
@@ -735,16 +1095,16 @@ int64_t places_of(int64_t all, int64_t tiles)
     return share ? share * tiles : ceil_div(all * tiles, 8);
 }
 
-template <int KS>
+template <int KS, bool SCORED>
 hipError_t launch_dim(int which, const AttnArgs &a, int64_t items, hipStream_t s)
 {
     constexpr int DB = blocks_of(KS);
     const dim3 grid((unsigned)(places_of(items / a.tiles, a.tiles) * a.splits * 8)), joins((unsigned)(items * 4), which == kDkv ? 2 : 1);
-    if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
-    else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS>), grid, dim3(kAttnThreads), 0, s, a);
+    if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS, SCORED>), grid, dim3(kAttnThreads), 0, s, a);
+    else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS, SCORED>), grid, dim3(kAttnThreads), 0, s, a);
     else if (KS <= 6 && items * a.splits >= one_side_from(a.dim))
-        hipLaunchKernelGGL((attention_dkv_kernel<KS, KS <= 6 ? 1 : 2>), grid, dim3(kAttnThreads), 0, s, a);
-    else hipLaunchKernelGGL((attention_dkv_kernel<KS, 2>), grid, dim3(2 * kAttnThreads), 0, s, a);
+        hipLaunchKernelGGL((attention_dkv_kernel<KS, KS <= 6 ? 1 : 2, SCORED>), grid, dim3(kAttnThreads), 0, s, a);
+    else hipLaunchKernelGGL((attention_dkv_kernel<KS, 2, SCORED>), grid, dim3(2 * kAttnThreads), 0, s, a);
     if (a.splits > 1) {
         if (hipError_t e = hipGetLastError()) return e;
         if (which == kForward) hipLaunchKernelGGL((attention_join_kernel<DB, kForward>), joins, dim3(DB * 64), 0, s, a);
@@ -819,21 +1179,29 @@ int splits_of(int which, const AttnArgs &a)
     return best;
 }
 
-hipError_t launch(int which, AttnArgs a, size_t bytes, hipStream_t s)
+template <bool SCORED>
+hipError_t launch_scored(int which, const AttnArgs &a, int64_t items, hipStream_t s)
+{
+    switch ((a.dim + 15) / 16) {                             // padded: a kernel for each of the sizes in use, and the next one up for the others
+    case 1: case 2: return launch_dim<2, SCORED>(which, a, items, s);
+    case 3: case 4: return launch_dim<4, SCORED>(which, a, items, s);
+    case 5: return launch_dim<5, SCORED>(which, a, items, s);
+    case 6: return launch_dim<6, SCORED>(which, a, items, s);
+    default: return launch_dim<8, SCORED>(which, a, items, s);
+    }
+}
+
+// taken: the parts that it was split into, if that is asked for.
+hipError_t launch(int which, AttnArgs a, size_t bytes, hipStream_t s, int *taken = nullptr)
 {
     a.tiles = (int)ceil_div(which == kDkv ? a.max_k : a.max_q, kOwnRows);
     const int64_t items = items_of(which, a);
     if (items == 0) return hipSuccess;
     a.splits = splits_of(which, a);
     if (!a.parts || (size_t)sums_bytes(which, a, a.splits) > bytes) a.splits = 1;
+    if (taken) *taken = a.splits;
     a.part_stats = reinterpret_cast<f32x2 *>(a.parts + items * a.splits * kOwnRows * 32 * blocks_of_dim(a.dim));
-    switch ((a.dim + 15) / 16) {                             // padded: a kernel for each of the sizes in use, and the next one up for the others
-    case 1: case 2: return launch_dim<2>(which, a, items, s);
-    case 3: case 4: return launch_dim<4>(which, a, items, s);
-    case 5: return launch_dim<5>(which, a, items, s);
-    case 6: return launch_dim<6>(which, a, items, s);
-    default: return launch_dim<8>(which, a, items, s);
-    }
+    return a.scored ? launch_scored<true>(which, a, items, s) : launch_scored<false>(which, a, items, s);
 }
 
 }  // namespace
@@ -858,9 +1226,21 @@ int64_t attention_sums_bytes(const AttnArgs &a, bool backward)
 
 hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s) { return launch(kForward, a, bytes, s); }
 
+int64_t attention_table_bytes(const AttnArgs &a)
+{
+    return a.form.dtable ? items_of(kDq, a) * splits_of(kDq, a) * (a.form.two_sided ? 2 : 1) * a.form.buckets * (int64_t)sizeof(float) : 0;
+}
+
 hipError_t launch_attention_backward(const AttnArgs &a, size_t bytes, hipStream_t s)
 {
-    if (hipError_t e = launch(kDq, a, bytes, s)) return e;   // delta first: the other kernel reads it
+    int splits = 1;
+    if (hipError_t e = launch(kDq, a, bytes, s, &splits)) return e;      // delta first: the other kernel reads it
+    if (a.form.dtable) {
+        const int columns = (a.form.two_sided ? 2 : 1) * a.form.buckets;
+        hipLaunchKernelGGL(table_gradient_kernel, dim3((unsigned)a.heads), dim3(kTableThreads), 0, s, a.form.dtable_parts,
+                           items_of(kDq, a) / a.heads * splits, columns, a.form.dtable);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
     return launch(kDkv, a, bytes, s);
 }
 

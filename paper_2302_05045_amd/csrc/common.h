@@ -244,6 +244,16 @@ hipError_t launch_state8(const Step8Launch &ls, bool pack, hipStream_t s);
 
 // Attention (attention.hip): tensors of tokens x heads x dim, a row's elements adjacent, strides in elements.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+struct AttnForm {                           // of the scores; all zero: scale q k
+    float cap;                              // 0: none
+    const float *slopes;                    // heads, NULL: none
+    const _Float16 *table;                  // heads x columns, NULL: none
+    const int32_t *borders;                 // buckets - 1
+    int buckets, two_sided;                 // of a direction; columns: buckets, twice as many if two_sided
+    const int32_t *first_keys;              // batch, NULL: none
+    _Float16 *dtable;                       // NULL: not wanted
+    float *dtable_parts;
+};
 struct AttnArgs {
     const _Float16 *q, *k, *v, *dout;
     _Float16 *out, *dq, *dk, *dv;
@@ -256,11 +266,15 @@ struct AttnArgs {
     float scale;
     float *parts;                           // NULL: a launch is not split
     f32x2 *part_stats;
+    int scored;                             // whether form is looked at
+    AttnForm form;
 };
 // Whether the call's launches can be made.
 bool attention_fits(const samo_attention_desc &d, bool backward);
 // Bytes that a call can use at `parts`; with less a launch that would need them is not split.
 int64_t attention_sums_bytes(const AttnArgs &a, bool backward);
+// Bytes that a backward call needs at form.dtable_parts.
+int64_t attention_table_bytes(const AttnArgs &a);
 hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s);
 hipError_t launch_attention_backward(const AttnArgs &a, size_t bytes, hipStream_t s);
 
