@@ -541,6 +541,43 @@ samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, cons
                               const uint16_t *d_w_up, int64_t tokens, int64_t in, int64_t ffn, int32_t act, uint16_t *d_dgate,
                               uint16_t *d_dup, uint16_t *d_dx, void *d_workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------- norms around a block
+ * What lies between a block's output y and the next block's input: a norm behind the block, its gate and residual scale, the sum with the residual
+ * stream s and the next block's norm in one kernel, and its backward pass.  Row by row, with N(x) = (x - m) / sqrt(mean((x - m)^2) + eps), m = mean(x)
+ * (SAMO_NORM_LAYER) or 0 (SAMO_NORM_RMS),
+ *   n = N(y) y_weight + y_bias (y_norm != 0) or y,   s' = s + scale gate n,   out = N(s') weight + bias
+ * d_y NULL: there is no block before, s' = s and nothing is written to d_new_stream (y_norm, scale, the gate and y's vectors are not looked at).
+ * tokens x hidden row-major: d_stream and d_new_stream fp32 (stream_fp32 != 0) or fp16, d_y and d_out fp16; the vectors fp16[hidden], each may be
+ * NULL (1 for a weight or the gate, 0 for a bias).  d_stats: float[4 tokens], 16-byte aligned as everything here, for the backward pass, or NULL.
+ * Backward, from dout and dnew (of the stream's type; the gradient that reaches s' from further on; NULL: none) with what the forward pass left in
+ * d_new_stream (d_y NULL: d_stream's contents, given there) and d_stats:
+ *   d_dstream (of the stream's type) = dnew + the gradient through the norm,   d_dy (with d_y),
+ *   and of each vector the sum over the tokens, fp16[hidden], rounded once; NULL: not wanted.  With a loss scale in dout they are the scaled gradients.
+ * Arithmetic is fp32, out is formed from s' before its rounding, sums over a row and over the tokens are fp32 in a fixed order; each result is rounded once.
+ * The backward pass forms N(s') from the stored s' and the stats.  Squares are fp32: rows of 2^62 and more have no finite norm.
+ * d_new_stream may be d_stream and d_dstream d_dnew (in place); other results overlap nothing.  hidden: a multiple of 8 up to 16384; tokens below 2^31,
+ * 0 of them give vectors of zeros; eps > 0.
+ * d_workspace: samo_norm_workspace_bytes on the current device, 16-byte aligned, for the vectors' gradients (0 bytes where none is wanted); in use until
+ * the stream has passed the call. */
+enum { SAMO_NORM_RMS = 0, SAMO_NORM_LAYER = 1 };
+typedef struct {
+    int64_t tokens;
+    int32_t hidden, kind, y_norm, stream_fp32;
+    float eps, scale;
+    const void *d_stream;
+    const uint16_t *d_y, *d_weight, *d_bias, *d_y_weight, *d_y_bias, *d_gate;
+    void *d_new_stream;
+    uint16_t *d_out;
+    float *d_stats;
+    const uint16_t *d_dout;                          /* from here on backward only */
+    const void *d_dnew;
+    void *d_dstream;
+    uint16_t *d_dy, *d_dweight, *d_dbias, *d_dy_weight, *d_dy_bias, *d_dgate;
+} samo_norm_desc;
+samo_status samo_norm(const samo_norm_desc *h_desc, void *stream);
+samo_status samo_norm_workspace_bytes(const samo_norm_desc *h_desc, size_t *bytes);
+samo_status samo_norm_backward(const samo_norm_desc *h_desc, void *d_workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- compression inside the backward pass
  * (Section III-C: a layer's dense gradient is compressed as soon as the backward
  * pass has produced it; Section VI-C, discussion of the compute overhead: fusing

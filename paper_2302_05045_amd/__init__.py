@@ -125,6 +125,15 @@ class ScoresDesc(ctypes.Structure):
                 ("buckets", ctypes.c_int32), ("two_sided", ctypes.c_int32), ("d_first_keys", ctypes.c_void_p), ("d_dtable", ctypes.c_void_p)]
 
 
+class NormDesc(ctypes.Structure):
+    """samo_norm_desc"""
+    _fields_ = [("tokens", ctypes.c_int64), ("hidden", ctypes.c_int32), ("kind", ctypes.c_int32), ("y_norm", ctypes.c_int32),
+                ("stream_fp32", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)] + [
+        (name, ctypes.c_void_p) for name in ("d_stream", "d_y", "d_weight", "d_bias", "d_y_weight", "d_y_bias", "d_gate", "d_new_stream", "d_out",
+                                             "d_stats", "d_dout", "d_dnew", "d_dstream", "d_dy", "d_dweight", "d_dbias", "d_dy_weight", "d_dy_bias",
+                                             "d_dgate")]
+
+
 class StepGuard(ctypes.Structure):
     """samo_step_guard"""
     _fields_ = [("d_stats", ctypes.c_void_p), ("max_grad_norm", ctypes.c_float), ("skip_on_nonfinite", ctypes.c_int32)]
@@ -235,6 +244,9 @@ _SIGNATURES = {
     "samo_attention_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
     "samo_attention_backward": (ctypes.c_int32, [ctypes.POINTER(AttentionDesc), ctypes.c_void_p, ctypes.c_size_t,
                                                  ctypes.c_void_p]),
+    "samo_norm": (ctypes.c_int32, [ctypes.POINTER(NormDesc), ctypes.c_void_p]),
+    "samo_norm_workspace_bytes": (ctypes.c_int32, [ctypes.POINTER(NormDesc), ctypes.POINTER(ctypes.c_size_t)]),
+    "samo_norm_backward": (ctypes.c_int32, [ctypes.POINTER(NormDesc), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "samo_glu": (ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
                                   ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                   ctypes.c_void_p]),
@@ -1351,6 +1363,114 @@ def samo_glu_backward(dh: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, w_
                                    None if dx is None else _dev_matrix_of(dx, "dx", tokens, features),
                                    _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0,
                                    _stream()), "samo_glu_backward")
+
+
+NORMS = {"rms": 0, "layer": 1}
+
+
+class Norm(NamedTuple):
+    """The norms around a block and what is between them: n = N(y) y_weight + y_bias (y_norm) or y, s' = s + scale gate n, out = N(s') weight + bias.
+
+    kind: a key of NORMS, for both norms.  The vectors: float16 (hidden), None for 1 (weights, gate) or 0 (biases)."""
+    kind: str = "rms"
+    eps: float = 1e-5
+    weight: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    y_norm: bool = False
+    y_weight: Optional[torch.Tensor] = None
+    y_bias: Optional[torch.Tensor] = None
+    gate: Optional[torch.Tensor] = None
+    scale: float = 1.0
+
+
+class NormGrads(NamedTuple):
+    """Where samo_norm_backward leaves the vectors' gradients: float16 (hidden); None: not wanted."""
+    weight: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    y_weight: Optional[torch.Tensor] = None
+    y_bias: Optional[torch.Tensor] = None
+    gate: Optional[torch.Tensor] = None
+
+
+def _rows_of(t: torch.Tensor, dtype: torch.dtype, name: str, shape: tuple) -> Optional[int]:
+    """Device pointer of a contiguous 2-D tensor of that type and shape."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a tensor on the GPU" % name)
+    if t.dtype != dtype or t.dim() != 2 or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous 2-D %s tensor" % (name, dtype))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s has shape %s, needs %s" % (name, tuple(t.shape), shape))
+    return t.data_ptr() if t.numel() else None
+
+
+def _vector_of(t: Optional[torch.Tensor], name: str, hidden: int) -> Optional[int]:
+    if t is not None and t.numel() != hidden:
+        raise ValueError("%s holds %d elements, needs %d" % (name, t.numel(), hidden))
+    return _dev(t, _F16, name)
+
+
+def _norm_desc(norm: Norm, stream: torch.Tensor, y: Optional[torch.Tensor]) -> tuple:
+    """The descriptor of what both passes read but the stream, the stream's type and shape, and its pointer."""
+    if norm.kind not in NORMS:
+        raise ValueError("kind is one of %s, not %r" % (", ".join(NORMS), norm.kind))
+    if not isinstance(stream, torch.Tensor) or stream.dtype not in (_F16, torch.float32) or stream.dim() != 2:
+        raise TypeError("the stream must be a 2-D float16 or float32 tensor (tokens, hidden)")
+    shape, dtype = tuple(stream.shape), stream.dtype
+    at = _rows_of(stream, dtype, "stream", shape)
+    d = NormDesc()
+    d.tokens, d.hidden, d.kind, d.eps, d.scale = shape[0], _int32(shape[1], "hidden"), NORMS[norm.kind], norm.eps, norm.scale
+    d.y_norm, d.stream_fp32 = int(bool(norm.y_norm)), int(dtype == torch.float32)
+    for name in ("weight", "bias", "y_weight", "y_bias", "gate"):
+        setattr(d, "d_" + name, _vector_of(getattr(norm, name), name, shape[1]))
+    if y is not None:
+        d.d_y = _rows_of(y, _F16, "y", shape)
+    return d, dtype, shape, at
+
+
+def samo_norm(norm: Norm, stream: torch.Tensor, out: torch.Tensor, y: Optional[torch.Tensor] = None, new_stream: Optional[torch.Tensor] = None,
+              stats: Optional[torch.Tensor] = None) -> None:
+    """out = N(s') weight + bias of the residual stream s' = stream + scale gate n, n the block's output y or its norm; without y s' is the stream.
+
+    stream: (tokens, hidden) float16 or float32; new_stream: as the stream, receives s' (with y; it may be the stream itself); y, out: float16 of that
+    shape.  stats: float32 (tokens, 4), kept for samo_norm_backward."""
+    d, dtype, shape, d.d_stream = _norm_desc(norm, stream, y)
+    d.d_out = _rows_of(out, _F16, "out", shape)
+    if (y is None) != (new_stream is None):
+        raise ValueError("y and new_stream are given together or not at all")
+    if y is not None:
+        d.d_new_stream = _rows_of(new_stream, dtype, "new_stream", shape)
+    if stats is not None:
+        d.d_stats = _rows_of(stats, torch.float32, "stats", (shape[0], 4))
+    _check(lib().samo_norm(ctypes.byref(d), _stream()), "samo_norm")
+
+
+def samo_norm_backward(norm: Norm, dout: torch.Tensor, new_stream: torch.Tensor, stats: torch.Tensor, dstream: torch.Tensor,
+                       dnew: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
+                       grads: Optional[NormGrads] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """dstream, dy (with y) and the wanted vectors' gradients of samo_norm, from dout and dnew, the gradient that reaches the new stream from further on
+    (None: none; dstream may be dnew itself).  new_stream: what the forward pass left there, without y its stream; stats: what it kept.
+
+    workspace (uint8, samo_norm_workspace_bytes of the descriptor; for the vectors' gradients) is in use until the stream has passed the call; without
+    one the call takes it from torch's allocator."""
+    d, dtype, shape, d.d_new_stream = _norm_desc(norm, new_stream, y)
+    d.d_dout = _rows_of(dout, _F16, "dout", shape)
+    d.d_stats = _rows_of(stats, torch.float32, "stats", (shape[0], 4))
+    d.d_dstream = _rows_of(dstream, dtype, "dstream", shape)
+    if dnew is not None:
+        d.d_dnew = _rows_of(dnew, dtype, "dnew", shape)
+    if (y is None) != (dy is None):
+        raise ValueError("y and dy are given together or not at all")
+    if y is not None:
+        d.d_dy = _rows_of(dy, _F16, "dy", shape)
+    if grads is not None:
+        for name in ("weight", "bias", "y_weight", "y_bias", "gate"):
+            setattr(d, "d_d" + name, _vector_of(getattr(grads, name), "the gradient of " + name, shape[1]))
+    if workspace is None:
+        need = ctypes.c_size_t()
+        _check(lib().samo_norm_workspace_bytes(ctypes.byref(d), ctypes.byref(need)), "samo_norm_workspace_bytes")
+        workspace = _capture_scratch(need.value) if need.value else None
+    _check(lib().samo_norm_backward(ctypes.byref(d), _dev(workspace, torch.uint8, "workspace"), workspace.numel() if workspace is not None else 0,
+                                    _stream()), "samo_norm_backward")
 
 
 def samo_memory_model(n_total: int, nnz_total: int):

@@ -1490,6 +1490,94 @@ samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, cons
     return hip_status(launch_glu_backward(act, a, shape, as_stream(stream)));
 }
 
+}  // extern "C"
+
+// ---------------------------------------------------------------- norms around a block
+namespace {
+
+constexpr int32_t kMaxHidden = 16384;
+
+// Sizes, and the vectors; of the wanted gradients those that belong to nothing are refused.
+samo_status check_norm(const samo_norm_desc *d, bool backward, NormArgs *a)
+{
+    if (!d) return SAMO_ERR_NULL;
+    if (d->tokens < 0 || d->tokens > INT32_MAX || d->hidden < 8 || d->hidden > kMaxHidden || d->hidden % 8) return SAMO_ERR_SIZE;
+    if (d->kind != SAMO_NORM_RMS && d->kind != SAMO_NORM_LAYER) return SAMO_ERR_ARG;
+    if (!(std::isfinite(d->eps) && d->eps > 0.f) || (d->d_y && !std::isfinite(d->scale))) return SAMO_ERR_ARG;
+    const void *vectors[] = {d->d_weight, d->d_bias, d->d_y_weight, d->d_y_bias, d->d_gate, d->d_y, d->d_stats, d->d_stream, d->d_new_stream, d->d_out};
+    for (const void *p : vectors)
+        if (misaligned(p)) return SAMO_ERR_ALIGN;
+    std::memset(a, 0, sizeof(*a));
+    a->tokens = d->tokens;
+    a->hidden = d->hidden;
+    a->layer = d->kind == SAMO_NORM_LAYER;
+    a->y_norm = d->d_y && d->y_norm != 0;
+    a->stream_fp32 = d->stream_fp32 != 0;
+    a->eps = d->eps;
+    a->scale = d->d_y ? d->scale : 0.f;
+    a->stream = d->d_stream;
+    a->y = halves(d->d_y);
+    a->weight = halves(d->d_weight);
+    a->bias = halves(d->d_bias);
+    a->gate = d->d_y ? halves(d->d_gate) : nullptr;
+    a->y_weight = a->y_norm ? halves(d->d_y_weight) : nullptr;
+    a->y_bias = a->y_norm ? halves(d->d_y_bias) : nullptr;
+    a->new_stream = d->d_new_stream;
+    a->out = halves(d->d_out);
+    a->stats = d->d_stats;
+    if (!backward) return SAMO_OK;
+    const void *more[] = {d->d_dout, d->d_dnew, d->d_dstream, d->d_dy, d->d_dweight, d->d_dbias, d->d_dy_weight, d->d_dy_bias, d->d_dgate};
+    for (const void *p : more)
+        if (misaligned(p)) return SAMO_ERR_ALIGN;
+    if ((!a->y_norm && (d->d_dy_weight || d->d_dy_bias)) || (!d->d_y && (d->d_dgate || d->d_dy))) return SAMO_ERR_ARG;
+    a->dout = halves(d->d_dout);
+    a->dnew = d->d_dnew;
+    a->dstream = d->d_dstream;
+    a->dy = halves(d->d_dy);
+    a->dweight = halves(d->d_dweight);
+    a->dbias = halves(d->d_dbias);
+    a->dy_weight = halves(d->d_dy_weight);
+    a->dy_bias = halves(d->d_dy_bias);
+    a->dgate = halves(d->d_dgate);
+    return SAMO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+samo_status samo_norm(const samo_norm_desc *h_desc, void *stream)
+{
+    NormArgs a;
+    if (samo_status s = check_norm(h_desc, false, &a)) return s;
+    if (a.tokens == 0) return SAMO_OK;
+    if (!a.stream || !a.out || (a.y && !a.new_stream)) return SAMO_ERR_NULL;
+    if (a.y && a.new_stream == static_cast<void *>(a.out)) return SAMO_ERR_ARG;
+    return hip_status(launch_norm(a, as_stream(stream)));
+}
+
+samo_status samo_norm_workspace_bytes(const samo_norm_desc *h_desc, size_t *bytes)
+{
+    if (!bytes) return SAMO_ERR_NULL;
+    NormArgs a;
+    if (samo_status s = check_norm(h_desc, true, &a)) return s;
+    *bytes = norm_workspace(a);
+    return SAMO_OK;
+}
+
+samo_status samo_norm_backward(const samo_norm_desc *h_desc, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    NormArgs a;
+    if (samo_status s = check_norm(h_desc, true, &a)) return s;
+    if (a.tokens > 0 && (!a.dout || !a.new_stream || !a.stats || !a.dstream || (a.y && !a.dy))) return SAMO_ERR_NULL;
+    if (a.dy && a.dstream == static_cast<void *>(a.dy)) return SAMO_ERR_ARG;
+    const size_t need = norm_workspace(a);
+    if (need > 0 && (!d_workspace || workspace_bytes < need)) return SAMO_ERR_WORKSPACE;
+    if (misaligned(d_workspace)) return SAMO_ERR_ALIGN;
+    a.partial = static_cast<float *>(d_workspace);
+    return hip_status(launch_norm_backward(a, as_stream(stream)));
+}
+
 samo_status samo_memory_model(int64_t n_total, int64_t nnz_total, int64_t *paper_default, int64_t *paper_samo,
                               int64_t *resident)
 {

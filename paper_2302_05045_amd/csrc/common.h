@@ -302,6 +302,27 @@ bool glu_backward_fits(int64_t tokens, int64_t in, int64_t ffn, const GluShape &
 hipError_t launch_glu(int act, const GluArgs &a, hipStream_t s);
 hipError_t launch_glu_backward(int act, GluArgs a, const GluShape &shape, hipStream_t s);
 
+// The norms around a block (norm.hip).
+struct NormArgs {
+    int64_t tokens;
+    int hidden, layer, y_norm, stream_fp32;
+    float eps, scale;
+    const void *stream;
+    const _Float16 *y, *weight, *bias, *y_weight, *y_bias, *gate;     // NULL: none
+    void *new_stream;                       // read in the backward pass
+    _Float16 *out;
+    float *stats;                           // tokens x 4, NULL: not kept
+    const _Float16 *dout;
+    const void *dnew;
+    void *dstream;
+    _Float16 *dy, *dweight, *dbias, *dy_weight, *dy_bias, *dgate;     // NULL: not wanted
+    float *partial;
+    int of_sum[4];                          // which row of partial a sum has; set by the launch
+};
+size_t norm_workspace(NormArgs a);
+hipError_t launch_norm(const NormArgs &a, hipStream_t s);
+hipError_t launch_norm_backward(NormArgs a, hipStream_t s);
+
 hipError_t launch_copy(void *dst, const void *src, int64_t bytes, hipStream_t s);
 
 }  // namespace samo

@@ -1,0 +1,397 @@
+// What lies between a block's output y and the next block's input, forward and backward, a pass over the rows each: a norm behind the block, its gate and
+// residual scale, the sum with the residual stream s, and the next block's norm.  With N(x) = (x - m) r, r = 1 / sqrt(mean((x - m)^2) + eps), m the
+// row's mean (layer) or 0 (rms), and f = scale gate,
+//   n = N(y) wy + by (or y),   s' = s + f n,   out = N(s') w + b
+// and with N'(g, x) = r (g - x mean(g x) - mean(g) (layer only)) of a normed x
+//   D = dnew + N'(dout w, x),   dy = N'(f D wy, yn) (or f D),
+//   dw = sum dout x,  db = sum dout,  dgate = scale (wy sum D yn + by sum D) (or scale sum D y),  dwy = f sum D yn,  dby = f sum D
+// Bound by HBM: forward reads s and y and writes s' and out, backward reads dout, dnew, s' and y and writes D and dy.
+//
+// A workgroup has a row at a time, 8 V elements of it in a thread's registers from the load to the store, and goes on to rows a grid further: the five
+// vectors are loaded once, and the sums over the tokens are a thread's own columns, left to a second kernel as one row of fp32 a workgroup.
+// Statistics are fp32 of fp32 values (of s' before its rounding), the variance from the differences from the mean, and meet over the row in a fixed order.
+#include "common.h"
+
+#include <algorithm>
+
+namespace samo {
+namespace {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kNormThreads = 512, kNormWaves = kNormThreads / 64;
+
+// Eight elements in a row, as they lie in memory.
+template <typename T> struct Eight;
+template <> struct Eight<_Float16> {
+    half8 x;
+    __device__ __forceinline__ float operator[](int i) const { return (float)x[i]; }
+    __device__ __forceinline__ void set(int i, float v) { x[i] = (_Float16)v; }
+};
+template <> struct Eight<float> {
+    f32x4 lo, hi;
+    __device__ __forceinline__ float operator[](int i) const { return i < 4 ? lo[i] : hi[i - 4]; }
+    __device__ __forceinline__ void set(int i, float v)
+    {
+        if (i < 4) lo[i] = v;
+        else hi[i - 4] = v;
+    }
+};
+template <typename T>
+__device__ __forceinline__ Eight<T> all_of(float v)
+{
+    Eight<T> e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e.set(i, v);
+    return e;
+}
+
+// A thread's share of a row: vector v of 8 elements is the (v blockDim + thread)th.
+template <int V>
+struct Columns {
+    int at[V];
+    bool there[V];
+    __device__ __forceinline__ explicit Columns(int hidden)
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            at[v] = (v * (int)blockDim.x + (int)threadIdx.x) * 8;
+            there[v] = at[v] < hidden;
+        }
+    }
+    // NULL, and what is behind the row, as `other`
+    template <typename T>
+    __device__ __forceinline__ void load(const T *from, Eight<T> (&to)[V], float other) const
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) to[v] = from && there[v] ? *reinterpret_cast<const Eight<T> *>(from + at[v]) : all_of<T>(other);
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T *to, const Eight<T> (&from)[V]) const
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (there[v]) *reinterpret_cast<Eight<T> *>(to + at[v]) = from[v];
+    }
+};
+
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ float plus_lane(float x)
+{
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, ROWS, 0xf, false));
+}
+// The sum over a wave, the same in all lanes.
+__device__ __forceinline__ float wave_total(float x)
+{
+    x = plus_lane<0x111, 0xf>(x);            // one lane to the right within rows of 16, two, four, eight; rows
+    x = plus_lane<0x112, 0xf>(x);
+    x = plus_lane<0x114, 0xf>(x);
+    x = plus_lane<0x118, 0xf>(x);
+    x = plus_lane<0x142, 0xa>(x);
+    x = plus_lane<0x143, 0xc>(x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// Sums over the workgroup, the same in all threads.  Two rooms in turn: a barrier for each sum, before it is read.
+struct Totals {
+    f32x4 (*room)[kNormWaves / 2];           // two numbers a wave
+    int turn;
+    __device__ __forceinline__ void operator()(float &a, float &b)
+    {
+        const int waves = (int)blockDim.x >> 6, wave = (int)threadIdx.x >> 6;
+        a = wave_total(a);
+        b = wave_total(b);
+        if (waves == 1) return;
+        float *to = reinterpret_cast<float *>(room[turn]);
+        if ((threadIdx.x & 63) == 0) {
+            to[2 * wave] = a;
+            to[2 * wave + 1] = b;
+        }
+        __syncthreads();
+        a = b = 0.f;
+        for (int w = 0; w < waves; ++w) {
+            a += to[2 * w];
+            b += to[2 * w + 1];
+        }
+        turn ^= 1;
+    }
+};
+
+// m and r of a row whose elements behind `there` are not counted.
+template <int V>
+__device__ __forceinline__ void statistics(const float (&x)[V][8], const Columns<V> &C, bool layer, float over, float eps, Totals &total, float &m, float &r)
+{
+    float sum = 0.f, none = 0.f;
+    m = 0.f;
+    if (layer) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += C.there[v] ? x[v][i] : 0.f;
+        total(sum, none);
+        m = sum * over;
+    }
+    float squares = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = C.there[v] ? x[v][i] - m : 0.f;
+            squares = fmaf(d, d, squares);
+        }
+    none = 0.f;
+    total(squares, none);
+    r = __builtin_amdgcn_rsqf(fmaf(squares, over, eps));
+}
+
+enum { kNoBlock, kPlainBlock, kNormedBlock };
+
+template <typename S, int V, int Y>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs A)
+{
+    __shared__ f32x4 room[2][kNormWaves / 2];
+    Totals total = {room, 0};
+    const Columns<V> C(A.hidden);
+    const S *stream = static_cast<const S *>(A.stream);
+    S *new_stream = static_cast<S *>(A.new_stream);
+    const float over = 1.f / (float)A.hidden;
+    const bool layer = A.layer;
+    Eight<_Float16> w[V], b[V], wy[V], by[V], gate[V];
+    C.load(A.weight, w, 1.f);
+    C.load(A.bias, b, 0.f);
+    if (Y == kNormedBlock) {
+        C.load(A.y_weight, wy, 1.f);
+        C.load(A.y_bias, by, 0.f);
+    }
+    if (Y != kNoBlock) C.load(A.gate, gate, 1.f);
+    for (int64_t row = blockIdx.x; row < A.tokens; row += gridDim.x) {
+        Eight<S> s[V];
+        Eight<_Float16> y[V];
+        C.load(stream + row * A.hidden, s, 0.f);
+        if (Y != kNoBlock) C.load(A.y + row * A.hidden, y, 0.f);
+        float x[V][8], my = 0.f, ry = 1.f, m, r;
+        if (Y != kNoBlock) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[v][i] = y[v][i];
+            if (Y == kNormedBlock) statistics<V>(x, C, layer, over, A.eps, total, my, ry);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float n = Y == kNormedBlock ? fmaf((x[v][i] - my) * ry, wy[v][i], by[v][i]) : x[v][i];
+                    x[v][i] = fmaf(A.scale * gate[v][i], n, s[v][i]);
+                    s[v].set(i, x[v][i]);
+                }
+            C.store(new_stream + row * A.hidden, s);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[v][i] = s[v][i];
+        }
+        statistics<V>(x, C, layer, over, A.eps, total, m, r);
+        Eight<_Float16> out[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[v].set(i, fmaf((x[v][i] - m) * r, w[v][i], b[v][i]));
+        C.store(A.out + row * A.hidden, out);
+        if (A.stats && threadIdx.x == 0) *reinterpret_cast<f32x4 *>(A.stats + 4 * row) = f32x4{my, ry, m, r};
+    }
+}
+
+// The sums over the tokens that a call wants, each a row of fp32 for each workgroup: dout x, dout, D yn (D y), D.
+enum { kSumOutX, kSumOut, kSumDY, kSumD, kSums };
+
+template <typename S, int V, int Y>
+__global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormArgs A)
+{
+    __shared__ f32x4 room[2][kNormWaves / 2];
+    Totals total = {room, 0};
+    const Columns<V> C(A.hidden);
+    const S *stream = static_cast<const S *>(A.new_stream), *dnew = static_cast<const S *>(A.dnew);
+    S *dstream = static_cast<S *>(A.dstream);
+    const float over = 1.f / (float)A.hidden;
+    const bool layer = A.layer;
+    Eight<_Float16> w[V], wy[V], gate[V];
+    C.load(A.weight, w, 1.f);
+    if (Y == kNormedBlock) C.load(A.y_weight, wy, 1.f);
+    if (Y != kNoBlock) C.load(A.gate, gate, 1.f);
+    float sums[kSums][V][8] = {};
+    for (int64_t row = blockIdx.x; row < A.tokens; row += gridDim.x) {
+        Eight<S> s[V], d[V];
+        Eight<_Float16> dout[V], y[V];
+        C.load(A.dout + row * A.hidden, dout, 0.f);
+        C.load(stream + row * A.hidden, s, 0.f);
+        C.load(dnew ? dnew + row * A.hidden : nullptr, d, 0.f);
+        const bool with_y = Y == kNormedBlock || (Y == kPlainBlock && A.of_sum[kSumDY] >= 0);
+        if (with_y) C.load(A.y + row * A.hidden, y, 0.f);
+        const f32x4 stat = *reinterpret_cast<const f32x4 *>(A.stats + 4 * row);
+        const float my = stat[0], ry = stat[1], m = stat[2], r = stat[3];
+        float x[V][8], dx[V][8], gx = 0.f, g = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[v][i] = (s[v][i] - m) * r;
+                dx[v][i] = dout[v][i] * w[v][i];
+                gx = fmaf(dx[v][i], x[v][i], gx);            // behind the row dout is zero
+                g += dx[v][i];
+                sums[kSumOutX][v][i] = fmaf(dout[v][i], x[v][i], sums[kSumOutX][v][i]);
+                sums[kSumOut][v][i] += dout[v][i];
+            }
+        total(gx, g);
+        gx *= over;
+        g = layer ? g * over : 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dx[v][i] = fmaf(r, dx[v][i] - g - x[v][i] * gx, d[v][i]);
+                d[v].set(i, dx[v][i]);
+            }
+        C.store(dstream + row * A.hidden, d);
+        if (Y == kNoBlock) continue;
+        gx = g = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (with_y) {
+                    x[v][i] = Y == kNormedBlock ? (y[v][i] - my) * ry : y[v][i];
+                    sums[kSumDY][v][i] = fmaf(dx[v][i], x[v][i], sums[kSumDY][v][i]);
+                }
+                sums[kSumD][v][i] += dx[v][i];
+                dx[v][i] *= A.scale * gate[v][i];
+                if (Y == kNormedBlock) {
+                    dx[v][i] *= C.there[v] ? (float)wy[v][i] : 0.f;
+                    gx = fmaf(dx[v][i], x[v][i], gx);
+                    g += dx[v][i];
+                }
+            }
+        Eight<_Float16> dy[V];
+        if (Y == kNormedBlock) {
+            total(gx, g);
+            gx *= over;
+            g = layer ? g * over : 0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dy[v].set(i, Y == kNormedBlock ? ry * (dx[v][i] - g - x[v][i] * gx) : dx[v][i]);
+        C.store(A.dy + row * A.hidden, dy);
+    }
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        if (A.of_sum[k] < 0) continue;
+        float *to = A.partial + ((int64_t)A.of_sum[k] * gridDim.x + blockIdx.x) * A.hidden;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            Eight<float> e;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e.set(i, sums[k][v][i]);
+            if (C.there[v]) *reinterpret_cast<Eight<float> *>(to + C.at[v]) = e;
+        }
+    }
+}
+
+// The vectors' gradients from the workgroups' sums: 64 columns to a workgroup, a wave takes every 16th row.
+constexpr int kJoinThreads = 1024, kJoinRows = kJoinThreads / 64;
+__global__ void __launch_bounds__(kJoinThreads) norm_join_kernel(const NormArgs A, int rows)
+{
+    __shared__ float meeting[kSums][kJoinRows][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = (int)blockIdx.x * 64 + lane;
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        float sum = 0.f;
+        if (A.of_sum[k] >= 0 && column < A.hidden)
+            for (int row = wave; row < rows; row += kJoinRows) sum += A.partial[((int64_t)A.of_sum[k] * rows + row) * A.hidden + column];
+        meeting[k][wave][lane] = sum;
+    }
+    __syncthreads();
+    if (wave > 0 || column >= A.hidden) return;
+    float sum[kSums];
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        sum[k] = 0.f;
+        for (int w = 0; w < kJoinRows; ++w) sum[k] += meeting[k][w][lane];
+    }
+    const float f = A.scale * (A.gate ? (float)A.gate[column] : 1.f), wy = A.y_weight ? (float)A.y_weight[column] : 1.f, by = A.y_bias ? (float)A.y_bias[column] : 0.f;
+    if (A.dweight) A.dweight[column] = (_Float16)sum[kSumOutX];
+    if (A.dbias) A.dbias[column] = (_Float16)sum[kSumOut];
+    if (A.dgate) A.dgate[column] = (_Float16)(A.scale * (A.y_norm ? fmaf(wy, sum[kSumDY], by * sum[kSumD]) : sum[kSumDY]));
+    if (A.dy_weight) A.dy_weight[column] = (_Float16)(f * sum[kSumDY]);
+    if (A.dy_bias) A.dy_bias[column] = (_Float16)(f * sum[kSumD]);
+}
+
+struct NormShape {
+    int v, threads, grid;
+};
+NormShape shape_of(const NormArgs &a, bool backward)
+{
+    NormShape s;
+    s.v = a.hidden <= 8 * kNormThreads ? 1 : a.hidden <= 16 * kNormThreads ? 2 : 4;
+    s.threads = (int)ceil_div(ceil_div(a.hidden, 8 * s.v), 64) * 64;
+    s.grid = (int)std::min<int64_t>(a.tokens, (int64_t)compute_units() * (backward ? 2 : 4));
+    return s;
+}
+
+template <typename S, int V>
+void launch_block(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
+{
+    const dim3 grid((unsigned)shape.grid), threads((unsigned)shape.threads);
+    const int y = !a.y ? kNoBlock : a.y_norm ? kNormedBlock : kPlainBlock;
+    if (backward) {
+        if (y == kNoBlock) hipLaunchKernelGGL((norm_backward_kernel<S, V, kNoBlock>), grid, threads, 0, s, a);
+        else if (y == kPlainBlock) hipLaunchKernelGGL((norm_backward_kernel<S, V, kPlainBlock>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((norm_backward_kernel<S, V, kNormedBlock>), grid, threads, 0, s, a);
+    } else {
+        if (y == kNoBlock) hipLaunchKernelGGL((norm_kernel<S, V, kNoBlock>), grid, threads, 0, s, a);
+        else if (y == kPlainBlock) hipLaunchKernelGGL((norm_kernel<S, V, kPlainBlock>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((norm_kernel<S, V, kNormedBlock>), grid, threads, 0, s, a);
+    }
+}
+template <typename S>
+void launch_stream(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
+{
+    if (shape.v == 1) launch_block<S, 1>(backward, a, shape, s);
+    else if (shape.v == 2) launch_block<S, 2>(backward, a, shape, s);
+    else launch_block<S, 4>(backward, a, shape, s);
+}
+hipError_t launch_rows(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
+{
+    if (shape.grid == 0) return hipSuccess;
+    if (a.stream_fp32) launch_stream<float>(backward, a, shape, s);
+    else launch_stream<_Float16>(backward, a, shape, s);
+    return hipGetLastError();
+}
+
+// Which sums the wanted vectors need, in order; their number.
+int number_sums(NormArgs &a)
+{
+    const bool wanted[kSums] = {a.dweight != nullptr, a.dbias != nullptr, a.dgate || a.dy_weight, a.dy_bias || (a.dgate && a.y_norm && a.y_bias)};
+    int count = 0;
+    for (int k = 0; k < kSums; ++k) a.of_sum[k] = wanted[k] ? count++ : -1;
+    return count;
+}
+
+}  // namespace
+
+size_t norm_workspace(NormArgs a) { return (size_t)number_sums(a) * (size_t)shape_of(a, true).grid * (size_t)a.hidden * sizeof(float); }
+
+hipError_t launch_norm(const NormArgs &a, hipStream_t s) { return launch_rows(false, a, shape_of(a, false), s); }
+
+hipError_t launch_norm_backward(NormArgs a, hipStream_t s)
+{
+    const NormShape shape = shape_of(a, true);
+    const int count = number_sums(a);
+    if (hipError_t e = launch_rows(true, a, shape, s)) return e;
+    if (count == 0) return hipSuccess;
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)ceil_div(a.hidden, 64)), dim3(kJoinThreads), 0, s, a, shape.grid);
+    return hipGetLastError();
+}
+
+}  // namespace samo
