@@ -1392,6 +1392,9 @@ class NormGrads(NamedTuple):
     gate: Optional[torch.Tensor] = None
 
 
+_NO_GRADS = NormGrads()
+
+
 def _rows_of(t: torch.Tensor, dtype: torch.dtype, name: str, shape: tuple) -> Optional[int]:
     """Device pointer of a contiguous 2-D tensor of that type and shape."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -1404,27 +1407,48 @@ def _rows_of(t: torch.Tensor, dtype: torch.dtype, name: str, shape: tuple) -> Op
 
 
 def _vector_of(t: Optional[torch.Tensor], name: str, hidden: int) -> Optional[int]:
+    at = _dev(t, _F16, name)
     if t is not None and t.numel() != hidden:
         raise ValueError("%s holds %d elements, needs %d" % (name, t.numel(), hidden))
-    return _dev(t, _F16, name)
+    return at
 
 
-def _norm_desc(norm: Norm, stream: torch.Tensor, y: Optional[torch.Tensor]) -> tuple:
-    """The descriptor of what both passes read but the stream, the stream's type and shape, and its pointer."""
-    if norm.kind not in NORMS:
-        raise ValueError("kind is one of %s, not %r" % (", ".join(NORMS), norm.kind))
+_NORM_FIELDS = ("stream", "y", "weight", "bias", "y_weight", "y_bias", "gate", "new_stream", "out", "stats", "dout", "dnew", "dstream", "dy",
+                "dweight", "dbias", "dy_weight", "dy_bias", "dgate")
+_NORM_OF_STREAM, _NORM_ROWS = ("stream", "new_stream", "dnew", "dstream"), ("y", "out", "dout", "dy")
+
+
+def _norm_pointers(d: NormDesc, tensors: tuple) -> None:
+    """The descriptor's sizes and pointers from the tensors in _NORM_FIELDS' order: the checks of _marshal.norm, with what is wrong."""
+    stream = tensors[0] if tensors[0] is not None else tensors[7]
     if not isinstance(stream, torch.Tensor) or stream.dtype not in (_F16, torch.float32) or stream.dim() != 2:
         raise TypeError("the stream must be a 2-D float16 or float32 tensor (tokens, hidden)")
     shape, dtype = tuple(stream.shape), stream.dtype
-    at = _rows_of(stream, dtype, "stream", shape)
+    d.tokens, d.hidden, d.stream_fp32 = shape[0], _int32(shape[1], "hidden"), int(dtype == torch.float32)
+    for name, t in zip(_NORM_FIELDS, tensors):
+        if t is None:
+            at = None
+        elif name in _NORM_OF_STREAM:
+            at = _rows_of(t, dtype, name, shape)
+        elif name in _NORM_ROWS:
+            at = _rows_of(t, _F16, name, shape)
+        elif name == "stats":
+            at = _rows_of(t, torch.float32, name, (shape[0], 4))
+        else:
+            at = _vector_of(t, name, shape[1])
+        setattr(d, "d_" + name, at)
+
+
+def _norm_desc(norm: Norm, *tensors) -> NormDesc:
+    """The descriptor; tensors in _NORM_FIELDS' order."""
+    kind = NORMS.get(norm.kind)
+    if kind is None:
+        raise ValueError("kind is one of %s, not %r" % (", ".join(NORMS), norm.kind))
     d = NormDesc()
-    d.tokens, d.hidden, d.kind, d.eps, d.scale = shape[0], _int32(shape[1], "hidden"), NORMS[norm.kind], norm.eps, norm.scale
-    d.y_norm, d.stream_fp32 = int(bool(norm.y_norm)), int(dtype == torch.float32)
-    for name in ("weight", "bias", "y_weight", "y_bias", "gate"):
-        setattr(d, "d_" + name, _vector_of(getattr(norm, name), name, shape[1]))
-    if y is not None:
-        d.d_y = _rows_of(y, _F16, "y", shape)
-    return d, dtype, shape, at
+    if _marshal is None or not _marshal.norm(ctypes.addressof(d), tensors):
+        _norm_pointers(d, tensors)
+    d.kind, d.eps, d.scale, d.y_norm = kind, norm.eps, norm.scale, bool(norm.y_norm)
+    return d
 
 
 def samo_norm(norm: Norm, stream: torch.Tensor, out: torch.Tensor, y: Optional[torch.Tensor] = None, new_stream: Optional[torch.Tensor] = None,
@@ -1433,14 +1457,10 @@ def samo_norm(norm: Norm, stream: torch.Tensor, out: torch.Tensor, y: Optional[t
 
     stream: (tokens, hidden) float16 or float32; new_stream: as the stream, receives s' (with y; it may be the stream itself); y, out: float16 of that
     shape.  stats: float32 (tokens, 4), kept for samo_norm_backward."""
-    d, dtype, shape, d.d_stream = _norm_desc(norm, stream, y)
-    d.d_out = _rows_of(out, _F16, "out", shape)
     if (y is None) != (new_stream is None):
         raise ValueError("y and new_stream are given together or not at all")
-    if y is not None:
-        d.d_new_stream = _rows_of(new_stream, dtype, "new_stream", shape)
-    if stats is not None:
-        d.d_stats = _rows_of(stats, torch.float32, "stats", (shape[0], 4))
+    d = _norm_desc(norm, stream, y, norm.weight, norm.bias, norm.y_weight, norm.y_bias, norm.gate, new_stream, out, stats,
+                   None, None, None, None, None, None, None, None, None)
     _check(lib().samo_norm(ctypes.byref(d), _stream()), "samo_norm")
 
 
@@ -1452,20 +1472,11 @@ def samo_norm_backward(norm: Norm, dout: torch.Tensor, new_stream: torch.Tensor,
 
     workspace (uint8, samo_norm_workspace_bytes of the descriptor; for the vectors' gradients) is in use until the stream has passed the call; without
     one the call takes it from torch's allocator."""
-    d, dtype, shape, d.d_new_stream = _norm_desc(norm, new_stream, y)
-    d.d_dout = _rows_of(dout, _F16, "dout", shape)
-    d.d_stats = _rows_of(stats, torch.float32, "stats", (shape[0], 4))
-    d.d_dstream = _rows_of(dstream, dtype, "dstream", shape)
-    if dnew is not None:
-        d.d_dnew = _rows_of(dnew, dtype, "dnew", shape)
     if (y is None) != (dy is None):
         raise ValueError("y and dy are given together or not at all")
-    if y is not None:
-        d.d_dy = _rows_of(dy, _F16, "dy", shape)
-    if grads is not None:
-        for name in ("weight", "bias", "y_weight", "y_bias", "gate"):
-            setattr(d, "d_d" + name, _vector_of(getattr(grads, name), "the gradient of " + name, shape[1]))
-    if workspace is None:
+    d = _norm_desc(norm, None, y, norm.weight, norm.bias, norm.y_weight, norm.y_bias, norm.gate, new_stream, None, stats, dout, dnew, dstream, dy,
+                   *(grads or _NO_GRADS))
+    if workspace is None and grads is not None:
         need = ctypes.c_size_t()
         _check(lib().samo_norm_workspace_bytes(ctypes.byref(d), ctypes.byref(need)), "samo_norm_workspace_bytes")
         workspace = _capture_scratch(need.value) if need.value else None

@@ -1,7 +1,7 @@
 // Argument marshalling of the Python binding in native code: a tensor argument's checks and its device
 // pointer in one call.  In Python the same checks are eight attribute reads, about 1 us per tensor, and an
 // entry point takes up to seven tensors: more host time than the kernel of a small layer runs.
-// Nothing but reads of tensor metadata happens in vector(), matrix() and heads().  Whatever is not a plain torch.Tensor or Parameter
+// Nothing but reads of tensor metadata happens in vector(), matrix(), heads() and norm().  Whatever is not a plain torch.Tensor or Parameter
 // (subclasses may override attributes, other objects have to be refused) goes to the Python function that makes the
 // same checks, given once by use().
 //
@@ -14,6 +14,7 @@
 #include <torch/csrc/utils/object_ptr.h>
 
 #include <chrono>
+#include <cstddef>
 #include <vector>
 
 #include "samo.h"
@@ -99,6 +100,49 @@ PyObject *heads(PyObject *, PyObject *const *args, Py_ssize_t count)
     to->d_data = t.numel() ? t.data_ptr() : nullptr;
     to->row = t.size(0) > 1 ? t.stride(0) : 0;
     to->head = t.size(1) > 1 ? t.stride(1) : 0;
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// norm(address, tensors): writes the sizes and pointers of a samo_norm_desc to the address from its 19 tensors (a tuple, in the order of the
+// descriptor; None: NULL) and returns True.  False, and the descriptor undefined, where one of them is not what it has to be: the Python function that makes
+// the same checks says which.
+PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    HANDLE_TH_ERRORS
+    enum Kind { kStream, kMatrix, kVector, kStats };
+    static const Kind kinds[] = {kStream, kMatrix, kVector, kVector, kVector, kVector, kVector, kStream, kMatrix, kStats,
+                                 kMatrix, kStream, kStream, kMatrix, kVector, kVector, kVector, kVector, kVector};
+    constexpr Py_ssize_t kPointers = sizeof(kinds) / sizeof(kinds[0]);
+    static_assert(offsetof(samo_norm_desc, d_dgate) - offsetof(samo_norm_desc, d_stream) == (kPointers - 1) * sizeof(void *), "the pointers lie in a row");
+    if (count != 2 || !PyTuple_Check(args[1]) || PyTuple_GET_SIZE(args[1]) != kPointers) {
+        PyErr_SetString(PyExc_TypeError, "norm(address, tensors)");
+        return nullptr;
+    }
+    samo_norm_desc *to = static_cast<samo_norm_desc *>(PyLong_AsVoidPtr(args[0]));
+    if (PyErr_Occurred()) return nullptr;
+    PyObject *first = PyTuple_GET_ITEM(args[1], 0) != Py_None ? PyTuple_GET_ITEM(args[1], 0) : PyTuple_GET_ITEM(args[1], 7);
+    if (!to || !THPVariable_CheckExact(first)) Py_RETURN_FALSE;
+    const at::Tensor &stream = THPVariable_Unpack(first);
+    const at::ScalarType type = stream.scalar_type();
+    if (stream.dim() != 2 || (type != at::kHalf && type != at::kFloat) || stream.size(1) > INT32_MAX) Py_RETURN_FALSE;
+    const int64_t tokens = stream.size(0), hidden = stream.size(1);
+    void **pointers = reinterpret_cast<void **>(reinterpret_cast<char *>(to) + offsetof(samo_norm_desc, d_stream));
+    for (Py_ssize_t i = 0; i < kPointers; ++i) {
+        PyObject *item = PyTuple_GET_ITEM(args[1], i);
+        pointers[i] = nullptr;
+        if (item == Py_None) continue;
+        if (!THPVariable_CheckExact(item)) Py_RETURN_FALSE;
+        const at::Tensor &t = THPVariable_Unpack(item);
+        const at::ScalarType want = kinds[i] == kStream ? type : kinds[i] == kStats ? at::kFloat : at::kHalf;
+        if (!t.is_cuda() || t.scalar_type() != want || !t.is_contiguous()) Py_RETURN_FALSE;
+        if (kinds[i] == kVector ? t.dim() != 1 || t.size(0) != hidden : t.dim() != 2 || t.size(0) != tokens || t.size(1) != (kinds[i] == kStats ? 4 : hidden))
+            Py_RETURN_FALSE;
+        if (t.numel()) pointers[i] = t.data_ptr();
+    }
+    to->tokens = tokens;
+    to->hidden = (int32_t)hidden;
+    to->stream_fp32 = type == at::kFloat;
     Py_RETURN_TRUE;
     END_HANDLE_TH_ERRORS
 }
@@ -286,6 +330,7 @@ PyMethodDef methods[] = {
     {"vector", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(vector)), METH_FASTCALL, nullptr},
     {"matrix", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(matrix)), METH_FASTCALL, nullptr},
     {"heads", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(heads)), METH_FASTCALL, nullptr},
+    {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm)), METH_FASTCALL, nullptr},
     {"build_indices", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(build_indices)), METH_FASTCALL, nullptr},
     {"use", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(use)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -20,7 +20,7 @@ namespace {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kNormThreads = 512, kNormWaves = kNormThreads / 64;
+constexpr int kNormThreads = 512, kWideThreads = 1024;
 
 // Eight elements in a row, as they lie in memory.
 template <typename T> struct Eight;
@@ -47,32 +47,57 @@ __device__ __forceinline__ Eight<T> all_of(float v)
     return e;
 }
 
-// A thread's share of a row: vector v of 8 elements is the (v blockDim + thread)th.
+// A thread's share of a row: vector v of 8 elements is the (v blockDim + thread)th.  A row is a buffer of its own, so that a thread behind its end reads
+// zeros and writes nothing, without a branch and with one offset for all arrays of a type.
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
 template <int V>
 struct Columns {
-    int at[V];
-    bool there[V];
-    __device__ __forceinline__ explicit Columns(int hidden)
+    int hidden;
+    __device__ __forceinline__ int at(int v) const { return (v * (int)blockDim.x + (int)threadIdx.x) * 8; }
+    __device__ __forceinline__ bool there(int v) const { return at(v) < hidden; }
+    template <typename T>
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_of(T *base, int64_t row) const
     {
+        void *from = const_cast<void *>(static_cast<const void *>(base + row * hidden));
+        return __builtin_amdgcn_make_buffer_rsrc(from, 0, base ? hidden * (int)sizeof(T) : 0, 0x27000);
+    }
+    // row `row` of an array, zeros of none
+    __device__ __forceinline__ void load(const _Float16 *base, int64_t row, Eight<_Float16> (&to)[V]) const
+    {
+        const __amdgpu_buffer_rsrc_t from = row_of(base, row);
+#pragma unroll
+        for (int v = 0; v < V; ++v) to[v].x = __builtin_bit_cast(half8, __builtin_amdgcn_raw_buffer_load_b128(from, at(v) * 2, 0, 0));
+    }
+    __device__ __forceinline__ void load(const float *base, int64_t row, Eight<float> (&to)[V]) const
+    {
+        const __amdgpu_buffer_rsrc_t from = row_of(base, row);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            at[v] = (v * (int)blockDim.x + (int)threadIdx.x) * 8;
-            there[v] = at[v] < hidden;
+            to[v].lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at(v) * 4, 0, 0));
+            to[v].hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at(v) * 4 + 16, 0, 0));
         }
     }
-    // NULL, and what is behind the row, as `other`
-    template <typename T>
-    __device__ __forceinline__ void load(const T *from, Eight<T> (&to)[V], float other) const
+    __device__ __forceinline__ void vector(const _Float16 *base, Eight<_Float16> (&to)[V], float other) const
     {
+        if (base) load(base, 0, to);
+        else
 #pragma unroll
-        for (int v = 0; v < V; ++v) to[v] = from && there[v] ? *reinterpret_cast<const Eight<T> *>(from + at[v]) : all_of<T>(other);
+            for (int v = 0; v < V; ++v) to[v] = all_of<_Float16>(other);
     }
-    template <typename T>
-    __device__ __forceinline__ void store(T *to, const Eight<T> (&from)[V]) const
+    __device__ __forceinline__ void store(_Float16 *base, int64_t row, const Eight<_Float16> (&from)[V]) const
     {
+        const __amdgpu_buffer_rsrc_t to = row_of(base, row);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (there[v]) *reinterpret_cast<Eight<T> *>(to + at[v]) = from[v];
+        for (int v = 0; v < V; ++v) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, from[v].x), to, at(v) * 2, 0, 0);
+    }
+    __device__ __forceinline__ void store(float *base, int64_t row, const Eight<float> (&from)[V]) const
+    {
+        const __amdgpu_buffer_rsrc_t to = row_of(base, row);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, from[v].lo), to, at(v) * 4, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, from[v].hi), to, at(v) * 4 + 16, 0, 0);
+        }
     }
 };
 
@@ -94,33 +119,43 @@ __device__ __forceinline__ float wave_total(float x)
 }
 
 // Sums over the workgroup, the same in all threads.  Two rooms in turn: a barrier for each sum, before it is read.
+template <int WAVES>
 struct Totals {
-    f32x4 (*room)[kNormWaves / 2];           // two numbers a wave
+    f32x4 (*room)[WAVES / 2];                // two numbers a wave, zero where there is none
     int turn;
+    __device__ __forceinline__ explicit Totals(f32x4 (*r)[WAVES / 2]) : room(r), turn(0)
+    {
+        if (blockDim.x == 64) return;
+        if (threadIdx.x < WAVES) room[threadIdx.x / (WAVES / 2)][threadIdx.x % (WAVES / 2)] = f32x4{0.f, 0.f, 0.f, 0.f};
+        __syncthreads();
+    }
     __device__ __forceinline__ void operator()(float &a, float &b)
     {
-        const int waves = (int)blockDim.x >> 6, wave = (int)threadIdx.x >> 6;
         a = wave_total(a);
         b = wave_total(b);
-        if (waves == 1) return;
-        float *to = reinterpret_cast<float *>(room[turn]);
+        if (blockDim.x == 64) return;
         if ((threadIdx.x & 63) == 0) {
-            to[2 * wave] = a;
-            to[2 * wave + 1] = b;
+            float *to = reinterpret_cast<float *>(room[turn]) + 2 * (threadIdx.x >> 6);
+            to[0] = a;
+            to[1] = b;
         }
         __syncthreads();
         a = b = 0.f;
-        for (int w = 0; w < waves; ++w) {
-            a += to[2 * w];
-            b += to[2 * w + 1];
+#pragma unroll
+        for (int w = 0; w < WAVES / 2; ++w) {
+            const f32x4 two = room[turn][w];
+            a += two[0];
+            b += two[1];
+            a += two[2];
+            b += two[3];
         }
         turn ^= 1;
     }
 };
 
 // m and r of a row whose elements behind `there` are not counted.
-template <int V>
-__device__ __forceinline__ void statistics(const float (&x)[V][8], const Columns<V> &C, bool layer, float over, float eps, Totals &total, float &m, float &r)
+template <int V, int WAVES>
+__device__ __forceinline__ void statistics(const float (&x)[V][8], const Columns<V> &C, bool layer, float over, float eps, Totals<WAVES> &total, float &m, float &r)
 {
     float sum = 0.f, none = 0.f;
     m = 0.f;
@@ -128,7 +163,7 @@ __device__ __forceinline__ void statistics(const float (&x)[V][8], const Columns
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += C.there[v] ? x[v][i] : 0.f;
+            for (int i = 0; i < 8; ++i) sum += C.there(v) ? x[v][i] : 0.f;
         total(sum, none);
         m = sum * over;
     }
@@ -137,7 +172,7 @@ __device__ __forceinline__ void statistics(const float (&x)[V][8], const Columns
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float d = C.there[v] ? x[v][i] - m : 0.f;
+            const float d = C.there(v) ? x[v][i] - m : 0.f;
             squares = fmaf(d, d, squares);
         }
     none = 0.f;
@@ -147,36 +182,49 @@ __device__ __forceinline__ void statistics(const float (&x)[V][8], const Columns
 
 enum { kNoBlock, kPlainBlock, kNormedBlock };
 
-template <typename S, int V, int Y>
-__global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs A)
+template <typename S, int V, int THREADS, int Y>
+__global__ void __launch_bounds__(THREADS) norm_kernel(const NormArgs A)
 {
-    __shared__ f32x4 room[2][kNormWaves / 2];
-    Totals total = {room, 0};
-    const Columns<V> C(A.hidden);
+    __shared__ f32x4 room[2][THREADS / 128];
+    Totals<THREADS / 64> total(room);
+    const Columns<V> C = {A.hidden};
     const S *stream = static_cast<const S *>(A.stream);
     S *new_stream = static_cast<S *>(A.new_stream);
     const float over = 1.f / (float)A.hidden;
     const bool layer = A.layer;
     Eight<_Float16> w[V], b[V], wy[V], by[V], gate[V];
-    C.load(A.weight, w, 1.f);
-    C.load(A.bias, b, 0.f);
+    C.vector(A.weight, w, 1.f);
+    C.load(A.bias, 0, b);
     if (Y == kNormedBlock) {
-        C.load(A.y_weight, wy, 1.f);
-        C.load(A.y_bias, by, 0.f);
+        C.vector(A.y_weight, wy, 1.f);
+        C.load(A.y_bias, 0, by);
     }
-    if (Y != kNoBlock) C.load(A.gate, gate, 1.f);
+    if (Y != kNoBlock) C.vector(A.gate, gate, 1.f);
+    Eight<S> coming_s[V];
+    Eight<_Float16> coming_y[V];
+    auto bring = [&](int64_t row) {
+        C.load(stream, row, coming_s);
+        if (Y != kNoBlock) C.load(A.y, row, coming_y);
+    };
+    constexpr bool kAhead = THREADS != kWideThreads;         // a row under way while the one before it is worked on
+    if (kAhead && blockIdx.x < A.tokens) bring(blockIdx.x);
     for (int64_t row = blockIdx.x; row < A.tokens; row += gridDim.x) {
+        if (!kAhead) bring(row);
         Eight<S> s[V];
         Eight<_Float16> y[V];
-        C.load(stream + row * A.hidden, s, 0.f);
-        if (Y != kNoBlock) C.load(A.y + row * A.hidden, y, 0.f);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            s[v] = coming_s[v];
+            if (Y != kNoBlock) y[v] = coming_y[v];
+        }
+        if (kAhead && row + gridDim.x < A.tokens) bring(row + gridDim.x);
         float x[V][8], my = 0.f, ry = 1.f, m, r;
         if (Y != kNoBlock) {
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[v][i] = y[v][i];
-            if (Y == kNormedBlock) statistics<V>(x, C, layer, over, A.eps, total, my, ry);
+            if (Y == kNormedBlock) statistics(x, C, layer, over, A.eps, total, my, ry);
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -185,20 +233,20 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs A)
                     x[v][i] = fmaf(A.scale * gate[v][i], n, s[v][i]);
                     s[v].set(i, x[v][i]);
                 }
-            C.store(new_stream + row * A.hidden, s);
+            C.store(new_stream, row, s);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[v][i] = s[v][i];
         }
-        statistics<V>(x, C, layer, over, A.eps, total, m, r);
+        statistics(x, C, layer, over, A.eps, total, m, r);
         Eight<_Float16> out[V];
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) out[v].set(i, fmaf((x[v][i] - m) * r, w[v][i], b[v][i]));
-        C.store(A.out + row * A.hidden, out);
+        C.store(A.out, row, out);
         if (A.stats && threadIdx.x == 0) *reinterpret_cast<f32x4 *>(A.stats + 4 * row) = f32x4{my, ry, m, r};
     }
 }
@@ -206,30 +254,47 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs A)
 // The sums over the tokens that a call wants, each a row of fp32 for each workgroup: dout x, dout, D yn (D y), D.
 enum { kSumOutX, kSumOut, kSumDY, kSumD, kSums };
 
-template <typename S, int V, int Y>
-__global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormArgs A)
+template <typename S, int V, int THREADS, int Y, bool BIASES>
+__global__ void __launch_bounds__(THREADS, V == 1 || THREADS == kWideThreads ? 4 : 2) norm_backward_kernel(const NormArgs A)
 {
-    __shared__ f32x4 room[2][kNormWaves / 2];
-    Totals total = {room, 0};
-    const Columns<V> C(A.hidden);
+    __shared__ f32x4 room[2][THREADS / 128];
+    Totals<THREADS / 64> total(room);
+    const Columns<V> C = {A.hidden};
     const S *stream = static_cast<const S *>(A.new_stream), *dnew = static_cast<const S *>(A.dnew);
     S *dstream = static_cast<S *>(A.dstream);
     const float over = 1.f / (float)A.hidden;
     const bool layer = A.layer;
     Eight<_Float16> w[V], wy[V], gate[V];
-    C.load(A.weight, w, 1.f);
-    if (Y == kNormedBlock) C.load(A.y_weight, wy, 1.f);
-    if (Y != kNoBlock) C.load(A.gate, gate, 1.f);
+    C.vector(A.weight, w, 1.f);
+    if (Y == kNormedBlock) C.vector(A.y_weight, wy, 1.f);
+    if (Y != kNoBlock) C.vector(A.gate, gate, 1.f);
     float sums[kSums][V][8] = {};
+    const _Float16 *y_at = Y == kNormedBlock || A.of_sum[kSumDY] >= 0 ? A.y : nullptr;       // of a plain y only the gate's gradient asks
+    Eight<S> coming_s[V], coming_d[V];
+    Eight<_Float16> coming_dout[V], coming_y[V];
+    f32x4 coming_stat;
+    auto bring = [&](int64_t row) {
+        C.load(A.dout, row, coming_dout);
+        C.load(stream, row, coming_s);
+        C.load(dnew, row, coming_d);
+        if (Y != kNoBlock) C.load(y_at, row, coming_y);
+        coming_stat = *reinterpret_cast<const f32x4 *>(A.stats + 4 * row);
+    };
+    constexpr bool kAhead = THREADS != kWideThreads;         // a row under way while the one before it is worked on
+    if (kAhead && blockIdx.x < A.tokens) bring(blockIdx.x);
     for (int64_t row = blockIdx.x; row < A.tokens; row += gridDim.x) {
+        if (!kAhead) bring(row);
         Eight<S> s[V], d[V];
         Eight<_Float16> dout[V], y[V];
-        C.load(A.dout + row * A.hidden, dout, 0.f);
-        C.load(stream + row * A.hidden, s, 0.f);
-        C.load(dnew ? dnew + row * A.hidden : nullptr, d, 0.f);
-        const bool with_y = Y == kNormedBlock || (Y == kPlainBlock && A.of_sum[kSumDY] >= 0);
-        if (with_y) C.load(A.y + row * A.hidden, y, 0.f);
-        const f32x4 stat = *reinterpret_cast<const f32x4 *>(A.stats + 4 * row);
+        const f32x4 stat = coming_stat;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            s[v] = coming_s[v];
+            d[v] = coming_d[v];
+            dout[v] = coming_dout[v];
+            if (Y != kNoBlock) y[v] = coming_y[v];
+        }
+        if (kAhead && row + gridDim.x < A.tokens) bring(row + gridDim.x);
         const float my = stat[0], ry = stat[1], m = stat[2], r = stat[3];
         float x[V][8], dx[V][8], gx = 0.f, g = 0.f;
 #pragma unroll
@@ -241,7 +306,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormA
                 gx = fmaf(dx[v][i], x[v][i], gx);            // behind the row dout is zero
                 g += dx[v][i];
                 sums[kSumOutX][v][i] = fmaf(dout[v][i], x[v][i], sums[kSumOutX][v][i]);
-                sums[kSumOut][v][i] += dout[v][i];
+                if (BIASES) sums[kSumOut][v][i] += dout[v][i];
             }
         total(gx, g);
         gx *= over;
@@ -253,21 +318,19 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormA
                 dx[v][i] = fmaf(r, dx[v][i] - g - x[v][i] * gx, d[v][i]);
                 d[v].set(i, dx[v][i]);
             }
-        C.store(dstream + row * A.hidden, d);
+        C.store(dstream, row, d);
         if (Y == kNoBlock) continue;
         gx = g = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (with_y) {
-                    x[v][i] = Y == kNormedBlock ? (y[v][i] - my) * ry : y[v][i];
-                    sums[kSumDY][v][i] = fmaf(dx[v][i], x[v][i], sums[kSumDY][v][i]);
-                }
-                sums[kSumD][v][i] += dx[v][i];
+                x[v][i] = Y == kNormedBlock ? (y[v][i] - my) * ry : y[v][i];
+                sums[kSumDY][v][i] = fmaf(dx[v][i], x[v][i], sums[kSumDY][v][i]);
+                if (BIASES) sums[kSumD][v][i] += dx[v][i];
                 dx[v][i] *= A.scale * gate[v][i];
                 if (Y == kNormedBlock) {
-                    dx[v][i] *= C.there[v] ? (float)wy[v][i] : 0.f;
+                    dx[v][i] *= C.there(v) ? (float)wy[v][i] : 0.f;
                     gx = fmaf(dx[v][i], x[v][i], gx);
                     g += dx[v][i];
                 }
@@ -282,49 +345,54 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormA
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) dy[v].set(i, Y == kNormedBlock ? ry * (dx[v][i] - g - x[v][i] * gx) : dx[v][i]);
-        C.store(A.dy + row * A.hidden, dy);
+        C.store(A.dy, row, dy);
     }
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
-        if (A.of_sum[k] < 0) continue;
-        float *to = A.partial + ((int64_t)A.of_sum[k] * gridDim.x + blockIdx.x) * A.hidden;
+        if (A.of_sum[k] < 0 || (!BIASES && (k == kSumOut || k == kSumD))) continue;
+        Eight<float> mine[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            Eight<float> e;
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e.set(i, sums[k][v][i]);
-            if (C.there[v]) *reinterpret_cast<Eight<float> *>(to + C.at[v]) = e;
-        }
+            for (int i = 0; i < 8; ++i) mine[v].set(i, sums[k][v][i]);
+        C.store(A.partial, (int64_t)A.of_sum[k] * gridDim.x + blockIdx.x, mine);
     }
 }
 
-// The vectors' gradients from the workgroups' sums: 64 columns to a workgroup, a wave takes every 16th row.
-constexpr int kJoinThreads = 1024, kJoinRows = kJoinThreads / 64;
+// The vectors' gradients from the workgroups' sums: 32 columns to a workgroup, half a wave takes every 32nd row.
+constexpr int kJoinThreads = 1024, kJoinColumns = 32, kJoinRows = kJoinThreads / kJoinColumns;
 __global__ void __launch_bounds__(kJoinThreads) norm_join_kernel(const NormArgs A, int rows)
 {
-    __shared__ float meeting[kSums][kJoinRows][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = (int)blockIdx.x * 64 + lane;
+    __shared__ float meeting[kSums][kJoinRows][kJoinColumns + 1];
+    const int first = threadIdx.x / kJoinColumns, lane = threadIdx.x % kJoinColumns, column = (int)blockIdx.x * kJoinColumns + lane;
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         float sum = 0.f;
-        if (A.of_sum[k] >= 0 && column < A.hidden)
-            for (int row = wave; row < rows; row += kJoinRows) sum += A.partial[((int64_t)A.of_sum[k] * rows + row) * A.hidden + column];
-        meeting[k][wave][lane] = sum;
+        if (A.of_sum[k] >= 0 && column < A.hidden) {
+            const float *from = A.partial + (int64_t)A.of_sum[k] * rows * A.hidden + column;
+#pragma unroll 8
+            for (int row = first; row < rows; row += kJoinRows) sum += from[(int64_t)row * A.hidden];
+        }
+        meeting[k][first][lane] = sum;
     }
     __syncthreads();
-    if (wave > 0 || column >= A.hidden) return;
-    float sum[kSums];
+    // the sums of a column by as many lanes as there are sums
+    const int k = threadIdx.x / kJoinColumns;
+    if (k < kSums) {
+        float sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) {
-        sum[k] = 0.f;
-        for (int w = 0; w < kJoinRows; ++w) sum[k] += meeting[k][w][lane];
+        for (int row = 0; row < kJoinRows; ++row) sum += meeting[k][row][lane];
+        meeting[k][0][lane] = sum;
     }
+    __syncthreads();
+    if (k > 0 || column >= A.hidden) return;
+    const float out_x = meeting[kSumOutX][0][lane], out = meeting[kSumOut][0][lane], dy = meeting[kSumDY][0][lane], d = meeting[kSumD][0][lane];
     const float f = A.scale * (A.gate ? (float)A.gate[column] : 1.f), wy = A.y_weight ? (float)A.y_weight[column] : 1.f, by = A.y_bias ? (float)A.y_bias[column] : 0.f;
-    if (A.dweight) A.dweight[column] = (_Float16)sum[kSumOutX];
-    if (A.dbias) A.dbias[column] = (_Float16)sum[kSumOut];
-    if (A.dgate) A.dgate[column] = (_Float16)(A.scale * (A.y_norm ? fmaf(wy, sum[kSumDY], by * sum[kSumD]) : sum[kSumDY]));
-    if (A.dy_weight) A.dy_weight[column] = (_Float16)(f * sum[kSumDY]);
-    if (A.dy_bias) A.dy_bias[column] = (_Float16)(f * sum[kSumD]);
+    if (A.dweight) A.dweight[column] = (_Float16)out_x;
+    if (A.dbias) A.dbias[column] = (_Float16)out;
+    if (A.dgate) A.dgate[column] = (_Float16)(A.scale * (A.y_norm ? fmaf(wy, dy, by * d) : dy));
+    if (A.dy_weight) A.dy_weight[column] = (_Float16)(f * dy);
+    if (A.dy_bias) A.dy_bias[column] = (_Float16)(f * d);
 }
 
 struct NormShape {
@@ -333,33 +401,33 @@ struct NormShape {
 NormShape shape_of(const NormArgs &a, bool backward)
 {
     NormShape s;
-    s.v = a.hidden <= 8 * kNormThreads ? 1 : a.hidden <= 16 * kNormThreads ? 2 : 4;
+    s.v = a.hidden <= 8 * kNormThreads ? 1 : 2;
     s.threads = (int)ceil_div(ceil_div(a.hidden, 8 * s.v), 64) * 64;
     s.grid = (int)std::min<int64_t>(a.tokens, (int64_t)compute_units() * (backward ? 2 : 4));
     return s;
 }
 
-template <typename S, int V>
-void launch_block(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
+template <typename S, int V, int THREADS, int Y>
+void launch_kernel(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
 {
     const dim3 grid((unsigned)shape.grid), threads((unsigned)shape.threads);
-    const int y = !a.y ? kNoBlock : a.y_norm ? kNormedBlock : kPlainBlock;
-    if (backward) {
-        if (y == kNoBlock) hipLaunchKernelGGL((norm_backward_kernel<S, V, kNoBlock>), grid, threads, 0, s, a);
-        else if (y == kPlainBlock) hipLaunchKernelGGL((norm_backward_kernel<S, V, kPlainBlock>), grid, threads, 0, s, a);
-        else hipLaunchKernelGGL((norm_backward_kernel<S, V, kNormedBlock>), grid, threads, 0, s, a);
-    } else {
-        if (y == kNoBlock) hipLaunchKernelGGL((norm_kernel<S, V, kNoBlock>), grid, threads, 0, s, a);
-        else if (y == kPlainBlock) hipLaunchKernelGGL((norm_kernel<S, V, kPlainBlock>), grid, threads, 0, s, a);
-        else hipLaunchKernelGGL((norm_kernel<S, V, kNormedBlock>), grid, threads, 0, s, a);
-    }
+    if (!backward) hipLaunchKernelGGL((norm_kernel<S, V, THREADS, Y>), grid, threads, 0, s, a);
+    else if (a.of_sum[kSumOut] >= 0 || a.of_sum[kSumD] >= 0) hipLaunchKernelGGL((norm_backward_kernel<S, V, THREADS, Y, true>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((norm_backward_kernel<S, V, THREADS, Y, false>), grid, threads, 0, s, a);
+}
+template <typename S, int V, int THREADS>
+void launch_block(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
+{
+    if (!a.y) launch_kernel<S, V, THREADS, kNoBlock>(backward, a, shape, s);
+    else if (!a.y_norm) launch_kernel<S, V, THREADS, kPlainBlock>(backward, a, shape, s);
+    else launch_kernel<S, V, THREADS, kNormedBlock>(backward, a, shape, s);
 }
 template <typename S>
 void launch_stream(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
 {
-    if (shape.v == 1) launch_block<S, 1>(backward, a, shape, s);
-    else if (shape.v == 2) launch_block<S, 2>(backward, a, shape, s);
-    else launch_block<S, 4>(backward, a, shape, s);
+    if (shape.threads > kNormThreads) launch_block<S, 2, kWideThreads>(backward, a, shape, s);
+    else if (shape.v == 2) launch_block<S, 2, kNormThreads>(backward, a, shape, s);
+    else launch_block<S, 1, kNormThreads>(backward, a, shape, s);
 }
 hipError_t launch_rows(bool backward, const NormArgs &a, const NormShape &shape, hipStream_t s)
 {
@@ -390,7 +458,7 @@ hipError_t launch_norm_backward(NormArgs a, hipStream_t s)
     const int count = number_sums(a);
     if (hipError_t e = launch_rows(true, a, shape, s)) return e;
     if (count == 0) return hipSuccess;
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)ceil_div(a.hidden, 64)), dim3(kJoinThreads), 0, s, a, shape.grid);
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)ceil_div(a.hidden, kJoinColumns)), dim3(kJoinThreads), 0, s, a, shape.grid);
     return hipGetLastError();
 }
 

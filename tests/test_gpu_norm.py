@@ -314,8 +314,7 @@ def test_workspaces_of_the_callers_own():
     s, dout = rnd(t, h), rnd(t, h)
     out, stats, ds, gw, gb = torch.zeros_like(s), torch.zeros(t, 4, device=DEV), torch.zeros_like(s), rnd(h), rnd(h)
     samo.samo_norm(norm, s, out, stats=stats)
-    d = samo._norm_desc(norm, s, None)[0]
-    d.d_dweight, d.d_dbias = gw.data_ptr(), gb.data_ptr()
+    d = samo._norm_desc(norm, None, None, norm.weight, norm.bias, None, None, None, s, None, stats, dout, None, ds, None, gw, gb, None, None, None)
     need = ctypes.c_size_t()
     assert samo.lib().samo_norm_workspace_bytes(ctypes.byref(d), ctypes.byref(need)) == 0 and need.value > 0
     res = []
@@ -348,6 +347,8 @@ def test_refusals_of_the_binding():
         samo.samo_norm(samo.Norm(), s.t(), out)
     with pytest.raises(samo.SamoError):
         samo.samo_norm(samo.Norm(), s[:, :12].contiguous(), out[:, :12].contiguous())
+    with pytest.raises(TypeError):
+        samo.samo_norm(samo.Norm(), s, out.cpu())
     ds = torch.full_like(s, 7.0)
     for kw in (dict(y=s), dict(dy=new), dict(dnew=s.float()), dict(dnew=s[:2]), dict(grads=samo.NormGrads(weight=w[:8]))):
         with pytest.raises((ValueError, TypeError)):
@@ -356,3 +357,27 @@ def test_refusals_of_the_binding():
         with pytest.raises(samo.SamoError):
             samo.samo_norm_backward(samo.Norm(), s, s, stats, ds, **kw)
     assert torch.all(out == 7.0) and torch.all(new == 7.0) and torch.all(ds == 7.0)
+
+
+def test_native_and_python_descriptors_agree():
+    """The descriptor's fields by native code and in Python, for what both take; what one refuses the other refuses."""
+    import ctypes
+    t, h = 6, 16
+    m, v = torch.zeros(t, h, device=DEV).half(), torch.zeros(h, device=DEV).half()
+    good = [m] * 2 + [v] * 5 + [m] * 2 + [torch.zeros(t, 4, device=DEV)] + [m] * 4 + [v] * 5
+    others = [None, m.float(), m[:3], m[:, :8], m.t(), m.cpu(), v.float(), v[:8], v[::2], m[:0], torch.zeros(t, 4, device=DEV), torch.nn.Parameter(m), [1], m[None]]
+    fields = [name for name, _ in samo.NormDesc._fields_]
+    for at in range(-1, len(good)):
+        for other in others if at >= 0 else [None]:
+            tensors = list(good)
+            if at >= 0:
+                tensors[at] = other
+            native, python = samo.NormDesc(), samo.NormDesc()
+            done = samo._marshal.norm(ctypes.addressof(native), tuple(tensors))
+            try:
+                samo._norm_pointers(python, tuple(tensors))
+            except (TypeError, ValueError):
+                assert not done, (at, other)
+                continue
+            if done:
+                assert all(getattr(native, name) == getattr(python, name) for name in fields), at
