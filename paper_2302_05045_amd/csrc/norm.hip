@@ -10,15 +10,13 @@
 // A workgroup has a row at a time, 8 V elements of it in a thread's registers from the load to the store, and goes on to rows a grid further: the five
 // vectors are loaded once, and the sums over the tokens are a thread's own columns, left to a second kernel as one row of fp32 a workgroup.
 // Statistics are fp32 of fp32 values (of s' before its rounding), the variance from the differences from the mean, and meet over the row in a fixed order.
-#include "common.h"
-
 #include <algorithm>
+
+#include "common.h"
+#include "lds_copy.h"
 
 namespace samo {
 namespace {
-
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kNormThreads = 512, kWideThreads = 1024;
 
@@ -139,7 +137,8 @@ struct Totals {
             to[0] = a;
             to[1] = b;
         }
-        __syncthreads();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // not for memory, as __syncthreads() waits: the next row's loads are under way
+        meet();
         a = b = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES / 2; ++w) {
@@ -193,13 +192,16 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const NormArgs A)
     const float over = 1.f / (float)A.hidden;
     const bool layer = A.layer;
     Eight<_Float16> w[V], b[V], wy[V], by[V], gate[V];
-    C.vector(A.weight, w, 1.f);
-    C.load(A.bias, 0, b);
-    if (Y == kNormedBlock) {
-        C.vector(A.y_weight, wy, 1.f);
-        C.load(A.y_bias, 0, by);
-    }
-    if (Y != kNoBlock) C.vector(A.gate, gate, 1.f);
+    auto vectors = [&] {
+        C.vector(A.weight, w, 1.f);
+        C.load(A.bias, 0, b);
+        if (Y == kNormedBlock) {
+            C.vector(A.y_weight, wy, 1.f);
+            C.load(A.y_bias, 0, by);
+        }
+        if (Y != kNoBlock) C.vector(A.gate, gate, 1.f);
+    };
+    vectors();
     Eight<S> coming_s[V];
     Eight<_Float16> coming_y[V];
     auto bring = [&](int64_t row) {
@@ -209,7 +211,10 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const NormArgs A)
     constexpr bool kAhead = THREADS != kWideThreads;         // a row under way while the one before it is worked on
     if (kAhead && blockIdx.x < A.tokens) bring(blockIdx.x);
     for (int64_t row = blockIdx.x; row < A.tokens; row += gridDim.x) {
-        if (!kAhead) bring(row);
+        if (!kAhead) {                                       // nor are the vectors kept: there are no registers for either
+            bring(row);
+            vectors();
+        }
         Eight<S> s[V];
         Eight<_Float16> y[V];
 #pragma unroll
@@ -255,7 +260,7 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const NormArgs A)
 enum { kSumOutX, kSumOut, kSumDY, kSumD, kSums };
 
 template <typename S, int V, int THREADS, int Y, bool BIASES>
-__global__ void __launch_bounds__(THREADS, V == 1 || THREADS == kWideThreads ? 4 : 2) norm_backward_kernel(const NormArgs A)
+__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? 4 : V == 1 ? 3 : 2) norm_backward_kernel(const NormArgs A)
 {
     __shared__ f32x4 room[2][THREADS / 128];
     Totals<THREADS / 64> total(room);
@@ -265,9 +270,12 @@ __global__ void __launch_bounds__(THREADS, V == 1 || THREADS == kWideThreads ? 4
     const float over = 1.f / (float)A.hidden;
     const bool layer = A.layer;
     Eight<_Float16> w[V], wy[V], gate[V];
-    C.vector(A.weight, w, 1.f);
-    if (Y == kNormedBlock) C.vector(A.y_weight, wy, 1.f);
-    if (Y != kNoBlock) C.vector(A.gate, gate, 1.f);
+    auto vectors = [&] {
+        C.vector(A.weight, w, 1.f);
+        if (Y == kNormedBlock) C.vector(A.y_weight, wy, 1.f);
+        if (Y != kNoBlock) C.vector(A.gate, gate, 1.f);
+    };
+    vectors();
     float sums[kSums][V][8] = {};
     const _Float16 *y_at = Y == kNormedBlock || A.of_sum[kSumDY] >= 0 ? A.y : nullptr;       // of a plain y only the gate's gradient asks
     Eight<S> coming_s[V], coming_d[V];
@@ -283,7 +291,10 @@ __global__ void __launch_bounds__(THREADS, V == 1 || THREADS == kWideThreads ? 4
     constexpr bool kAhead = THREADS != kWideThreads;         // a row under way while the one before it is worked on
     if (kAhead && blockIdx.x < A.tokens) bring(blockIdx.x);
     for (int64_t row = blockIdx.x; row < A.tokens; row += gridDim.x) {
-        if (!kAhead) bring(row);
+        if (!kAhead) {                                       // nor are the vectors kept: there are no registers for either
+            bring(row);
+            vectors();
+        }
         Eight<S> s[V], d[V];
         Eight<_Float16> dout[V], y[V];
         const f32x4 stat = coming_stat;
@@ -370,8 +381,13 @@ __global__ void __launch_bounds__(kJoinThreads) norm_join_kernel(const NormArgs 
         float sum = 0.f;
         if (A.of_sum[k] >= 0 && column < A.hidden) {
             const float *from = A.partial + (int64_t)A.of_sum[k] * rows * A.hidden + column;
-#pragma unroll 8
-            for (int row = first; row < rows; row += kJoinRows) sum += from[(int64_t)row * A.hidden];
+            for (int row = first; row < rows; row += 8 * kJoinRows) {       // eight loads under way, the last ones of a row that is there
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = from[(int64_t)std::min(row + i * kJoinRows, rows - 1) * A.hidden];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += row + i * kJoinRows < rows ? x[i] : 0.f;
+            }
         }
         meeting[k][first][lane] = sum;
     }
@@ -395,6 +411,11 @@ __global__ void __launch_bounds__(kJoinThreads) norm_join_kernel(const NormArgs 
     if (A.dy_bias) A.dy_bias[column] = (_Float16)(f * d);
 }
 
+// A thread has 8 elements of a row, 16 of rows of more than 4096; workgroups go on to rows a grid further.
+// Backward: 8 waves a compute unit, of narrow rows 4 workgroups, at least two rows each: what covers the loads' latency with a row under way, and few enough
+// to leave few rows of sums.  Both passes, rms before and after with a gate, us, at 4 / 8 / 12 waves a compute unit and more: 8192 x 4096 - / 125 / 125, 130 at 16;
+// 2048 x 2560 on fp32 - / 34 / 40; 8192 x 2048 (layer, biases) - / 74 / 76, 89 at 24; 8192 x 512 27 / 30 / 35; 1003 x 1024 (layer) one row each 22, two 19.
+// Forward: 16 waves; of rows of 7 and 8 waves and 8 elements 4 workgroups: 8192 x 4096 125 us with 4, 131 with 2; 2048 x 8192 74 and 70; 8192 x 2560 86 with 6, 83 with 3.
 struct NormShape {
     int v, threads, grid;
 };
@@ -403,7 +424,10 @@ NormShape shape_of(const NormArgs &a, bool backward)
     NormShape s;
     s.v = a.hidden <= 8 * kNormThreads ? 1 : 2;
     s.threads = (int)ceil_div(ceil_div(a.hidden, 8 * s.v), 64) * 64;
-    s.grid = (int)std::min<int64_t>(a.tokens, (int64_t)compute_units() * (backward ? 2 : 4));
+    const int64_t waves = s.threads / 64, units = compute_units();
+    int64_t most = units * (s.v == 1 && waves > 6 ? 4 : std::max<int64_t>(1, 16 / waves));
+    if (backward) most = std::max(units, std::min(units * std::min<int64_t>(4, std::max<int64_t>(1, 8 / waves)), (a.tokens + 1) / 2));
+    s.grid = (int)std::min(a.tokens, most);
     return s;
 }
 
