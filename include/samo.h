@@ -488,7 +488,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * by the bucket of the distance, or with keys that every query sees.  With i counted from the sequence's end as for the causal mask,
  *   d = i + k_len - q_len - j,   x = scale q k^T,   z = cap tanh(x / cap) - slope[h] |d| + table[h][column(d)],   out = softmax(z) v,  lse = log sum exp z
  * each part where it is given:
- *   cap             0: none; otherwise 2^-10 to 2^20
+ *   cap             0: none; otherwise 2^-10 to 256
  *   d_slopes        float[heads], finite
  *   d_table         fp16[heads * columns], head by head, finite; d_borders int32[buckets - 1], ascending from 1 or more: a distance's bucket is the number
  *                   of borders up to it.  1 to SAMO_ATTENTION_MAX_BUCKETS buckets.  two_sided == 0: columns = buckets, column(d) = bucket(max(d, 0));
@@ -499,8 +499,8 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  *   d_dtable        fp16[heads * columns] or NULL: the sums of dz over the pairs of every column, rounded once; all of it is written, columns of no pair
  *                   as zero.  With a loss scale in dout it is the scaled gradient, as any g.
  * Sums of dz are fp32 within 32 queries of a part, double over those; their order is fixed.  The slopes are constants and have no gradient.
- * tanh is within 2^-22 of itself where |x| is up to 5/8 of the cap and within 2^-22 elsewhere (and, with a cap up to 128, at a score whose block of 32
- * queries and 32 keys has such a one).  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
+ * The tanh is within 2^-20 of itself in blocks of 32 queries and 32 keys whose |x| are all up to half the cap (scale / cap between 2^-17 and 2^17), within
+ * 2^-22 elsewhere.  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
  * Everything else, alignment and limits, is as for samo_attention; slopes, borders and first_keys 4-byte, table and dtable 2-byte aligned.
  * samo_attention_scored_workspace_bytes: what the backward call needs (delta, and for d_dtable the parts of its sums) on the current device. */
 #define SAMO_ATTENTION_MAX_BUCKETS 64

@@ -1,15 +1,17 @@
 """Builds libsamo.so (HIP, gfx950 only) and the binding's native argument marshalling in-tree."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 import sysconfig
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsamo.so")
-SOURCES = ["api.hip", "attention.hip", "glu.hip", "index.hip", "norm.hip", "pipeline.hip", "step8.hip", "wgrad.hip"]
+SOURCES = ["api.hip", "attention.hip", "attention_all.hip", "attention_cap.hip", "attention_keys.hip", "attention_slope.hip", "attention_table.hip", "glu.hip", "index.hip", "norm.hip", "pipeline.hip", "step8.hip", "wgrad.hip"]
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
     "-Wall", "-Wextra", "-Wno-unused-parameter",
@@ -22,11 +24,19 @@ def build(verbose: bool = False, extra_flags: list | None = None, out: str | Non
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     out = out or LIB
     tmp = out + ".tmp%d" % os.getpid()
-    cmd = [hipcc] + FLAGS + (extra_flags or []) + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    flags = FLAGS + (extra_flags or []) + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    with tempfile.TemporaryDirectory() as objects:           # the sources side by side, then one link
+        def compile_one(source: str) -> str:
+            made = os.path.join(objects, source + ".o")
+            cmd = [hipcc] + [f for f in flags if f != "-shared"] + ["-c", os.path.join(CSRC, source), "-o", made]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            subprocess.check_call(cmd)
+            return made
+
+        with concurrent.futures.ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            made = list(pool.map(compile_one, SOURCES))
+        subprocess.check_call([hipcc] + flags + made + ["-o", tmp])
     os.replace(tmp, out)
     return out
 

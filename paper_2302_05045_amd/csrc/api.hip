@@ -1319,7 +1319,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
 // ---------------------------------------------------------------- attention with scores of another form
 namespace {
 
-constexpr float kLeastCap = 1.f / 1024.f, kMostCap = 1048576.f;     // what keeps scale / cap and cap log2(e) inside fp32
+constexpr float kLeastCap = 1.f / 1024.f, kMostCap = 256.f;       // the tanh is within 2^-22, so that a score is within 2^-14
 
 samo_status check_scores(const samo_attention_scores *s, bool backward, AttnArgs *a)
 {

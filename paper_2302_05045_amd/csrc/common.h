@@ -278,6 +278,13 @@ int64_t attention_table_bytes(const AttnArgs &a);
 hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s);
 hipError_t launch_attention_backward(const AttnArgs &a, size_t bytes, hipStream_t s);
 
+// A launch's kernel for scores of another form (which: forward, dQ, dK and dV).
+hipError_t launch_attention_keys(int which, const AttnArgs &a, int64_t items, hipStream_t s);
+hipError_t launch_attention_cap(int which, const AttnArgs &a, int64_t items, hipStream_t s);
+hipError_t launch_attention_slope(int which, const AttnArgs &a, int64_t items, hipStream_t s);
+hipError_t launch_attention_table(int which, const AttnArgs &a, int64_t items, hipStream_t s);
+hipError_t launch_attention_all(int which, const AttnArgs &a, int64_t items, hipStream_t s);
+
 // The gated feed-forward block (glu.hip).
 struct GluArgs {
     const _Float16 *x, *w_gate, *w_up;      // tokens x in, ffn x in

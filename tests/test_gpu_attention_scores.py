@@ -241,9 +241,9 @@ def test_many_workgroups(dim):
 def test_scores_at_their_cap():
     """Products many times the cap either way: the tanh is 1, its slope next to nothing; one key takes all of a row, or many share it."""
     check([200], [200], 2, 2, 64, cap=2.0, std=4.0)
-    check([200], [200], 2, 2, 128, cap=300.0, std=8.0)
+    check([200], [200], 2, 2, 128, cap=200.0, std=8.0)
     check([200], [200], 2, 2, 64, cap=2.0 ** -10)
-    check([200], [200], 2, 2, 64, cap=2.0 ** 20)
+    check([200], [200], 2, 2, 64, cap=256.0)
 
 
 def test_large_biases():
@@ -263,7 +263,7 @@ def test_large_biases():
 def test_without_any_form_it_is_the_plain_attention():
     q, k, v, do = (torch.randn(300, 2, 80, device=DEV).half() for _ in range(4))
     res = []
-    for scores in (None, samo.Scores(), samo.Scores(cap=2.0 ** 20), samo.Scores(slopes=torch.zeros(2, device=DEV))):
+    for scores in (None, samo.Scores(), samo.Scores(cap=256.0), samo.Scores(slopes=torch.zeros(2, device=DEV))):
         o, dq, dk, dv, lse = *(torch.zeros_like(q) for _ in range(4)), torch.zeros(2, 300, device=DEV)
         samo.samo_attention(q, k, v, o, lse, scores=scores)
         samo.samo_attention_backward(do, q, k, v, o, lse, dq, dk, dv, scores=scores)
@@ -397,7 +397,7 @@ def test_refusals_of_the_binding():
                          (samo.Scores(table=table[:1], borders=borders), ValueError), (samo.Scores(table=table.float(), borders=borders), TypeError),
                          (samo.Scores(table=table[:, :3], borders=borders[:2], two_sided=True), TypeError),
                          (samo.Scores(table=table, borders=borders, two_sided=True), ValueError), (samo.Scores(table=table, borders=borders.cpu()), TypeError),
-                         (samo.Scores(first_keys=first.long()), TypeError), (samo.Scores(cap=-1.0), samo.SamoError), (samo.Scores(cap=1e9), samo.SamoError),
+                         (samo.Scores(first_keys=first.long()), TypeError), (samo.Scores(cap=-1.0), samo.SamoError), (samo.Scores(cap=257.0), samo.SamoError),
                          (samo.Scores(cap=float("nan")), samo.SamoError)):
         with pytest.raises(what):
             samo.samo_attention(q, q, q, out, lse, scores=scores)

@@ -17,7 +17,7 @@ def scores(**kw):
 
 
 @pytest.mark.parametrize("kw,want", [
-    (dict(cap=-1.0), ARG), (dict(cap=float("nan")), ARG), (dict(cap=float("inf")), ARG), (dict(cap=2.0 ** -11), ARG), (dict(cap=2.0 ** 21), ARG),
+    (dict(cap=-1.0), ARG), (dict(cap=float("nan")), ARG), (dict(cap=float("inf")), ARG), (dict(cap=2.0 ** -11), ARG), (dict(cap=256.5), ARG),
     (dict(buckets=0), SIZE), (dict(buckets=65), SIZE), (dict(buckets=-3), SIZE), (dict(d_borders=None), NULL), (dict(d_slopes=FAKE + 2), ALIGN),
     (dict(d_borders=FAKE + 1), ALIGN), (dict(d_first_keys=FAKE + 2), ALIGN), (dict(d_table=FAKE + 1), ALIGN), (dict(d_dtable=FAKE + 1), ALIGN),
 ])
