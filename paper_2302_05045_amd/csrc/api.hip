@@ -1268,6 +1268,7 @@ samo_status check_attention(const samo_attention_desc *d, bool backward, AttnArg
     a->window = d->window;
     a->scale = d->scale;
     a->parts = static_cast<float *>(d->d_sums);
+    a->pack = 1;
     return SAMO_OK;
 }
 
@@ -1342,6 +1343,7 @@ samo_status check_scores(const samo_attention_scores *s, bool backward, AttnArgs
     a->form.two_sided = s->two_sided != 0;
     a->form.first_keys = s->d_first_keys;
     a->form.dtable = backward ? reinterpret_cast<_Float16 *>(s->d_dtable) : nullptr;
+    a->pack = attention_pack(*a);
     return SAMO_OK;
 }
 

@@ -15,40 +15,53 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
     const int item = (int)(blockIdx.x >> 2);
     const Place at = place_of(item / A.tiles, item % A.tiles, 0, A);
     const Sequence seq = sequence_of(A, at.b);
-    const int count = WHICH == kDkv ? seq.k_len : seq.q_len, row = (WHICH == kDkv ? A.tiles - 1 - at.tile : at.tile) * kOwnRows + rows * kWaveRows + (lane & 31);
+    const int pack = WHICH == kForward ? A.pack : 1;
+    const int count = WHICH == kDkv ? seq.k_len : seq.q_len * pack, row = (WHICH == kDkv ? A.tiles - 1 - at.tile : at.tile) * kOwnRows + rows * kWaveRows + (lane & 31);
     if (row >= count) return;
     f32x16 acc[1];
     clear(acc);
     float top = -INFINITY, sum = 0.f;
+    const f32x2 *stats = A.part_stats + (at.slot * 4 + rows) * 32 + (lane & 31);
     if (WHICH == kForward)
-        for (int part = 0; part < A.splits; ++part) {
-            const f32x2 stat = A.part_stats[((at.slot + part) * 4 + rows) * 32 + (lane & 31)];
-            if (stat[1] != 0.f) top = fmaxf(top, stat[0]);
-        }
-    for (int part = 0; part < A.splits; ++part) {
-        float weight = 1.f;
-        if (WHICH == kForward) {
-            const f32x2 stat = A.part_stats[((at.slot + part) * 4 + rows) * 32 + (lane & 31)];
-            if (stat[1] == 0.f) continue;
-            weight = __builtin_amdgcn_exp2f(stat[0] - top);
-            sum = fmaf(stat[1], weight, sum);
-        }
-        const f32x4 *from = sums_of<DB>(A.parts, (at.slot + part) * kTensors + tensor, rows) + 4 * db * 64;
+        for (int part = 0; part < A.splits; part += 4) {
+            f32x2 stat[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 x = from[g * 64];
+            for (int i = 0; i < 4; ++i) stat[i] = stats[min(part + i, A.splits - 1) * 128];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[0][4 * g + e] = fmaf(x[e], weight, acc[0][4 * g + e]);
+            for (int i = 0; i < 4; ++i) top = stat[i][1] != 0.f ? fmaxf(top, stat[i][0]) : top;
+        }
+    for (int part = 0; part < A.splits; part += 4) {         // four parts' loads under way, the last ones of a part that is there
+        f32x2 stat[4];
+        f32x4 x[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int that = min(part + i, A.splits - 1);
+            if (WHICH == kForward) stat[i] = stats[that * 128];
+            const f32x4 *from = sums_of<DB>(A.parts, (at.slot + that) * kTensors + tensor, rows) + 4 * db * 64;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) x[i][g] = from[g * 64];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool counts = part + i < A.splits && (WHICH != kForward || stat[i][1] != 0.f);
+            float weight = 1.f;
+            if (WHICH == kForward) {
+                weight = __builtin_amdgcn_exp2f(stat[i][0] - top);
+                sum = counts ? fmaf(stat[i][1], weight, sum) : sum;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[0][e] = counts ? fmaf(x[i][e >> 2][e & 3], weight, acc[0][e]) : acc[0][e];
         }
     }
+    const int query = pack > 1 ? row / pack : row, head = pack > 1 ? at.head * pack + row - query * pack : at.head;
     _Float16 *to;
     int64_t stride;
     float factor = A.scale;
     if (WHICH == kForward) {
-        to = A.out + seq.q0 * A.out_row + at.head * A.out_head;
-        stride = A.out_row;
+        to = A.out + (seq.q0 + query) * A.out_row + head * A.out_head;
+        stride = 0;
         factor = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-        if (db == 0 && lane < 32) A.lse[(int64_t)at.head * A.q_tokens + seq.q0 + row] = sum == 0.f ? -INFINITY : top * kLn2 + __logf(sum);
+        if (db == 0 && lane < 32) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : top * kLn2 + __logf(sum);
     } else if (WHICH == kDq) {
         to = A.dq + seq.q0 * A.dq_row + at.head * A.dq_head;
         stride = A.dq_row;
@@ -79,10 +92,10 @@ __global__ void __launch_bounds__(kTableThreads) table_gradient_kernel(const flo
     to[(int64_t)blockIdx.x * columns + column] = (_Float16)(float)sum;
 }
 
-int64_t items_of(int which, const AttnArgs &a)
-{
-    return (int64_t)a.batch * (which == kDkv ? a.kv_heads : a.heads) * ceil_div(which == kDkv ? a.max_k : a.max_q, kOwnRows);
-}
+// Heads whose workgroups a launch has, and their rows (pack heads of a query each, where they share them).
+int64_t heads_of(int which, const AttnArgs &a) { return which == kDkv || (which == kForward && a.pack > 1) ? a.kv_heads : a.heads; }
+int64_t most_rows(int which, const AttnArgs &a) { return which == kDkv ? a.max_k : which == kForward ? (int64_t)a.max_q * a.pack : a.max_q; }
+int64_t items_of(int which, const AttnArgs &a) { return a.batch * heads_of(which, a) * ceil_div(most_rows(which, a), kOwnRows); }
 
 int blocks_of_dim(int dim) { return dim <= 32 ? 1 : dim <= 64 ? 2 : dim <= 96 ? 3 : 4; }
 
@@ -110,9 +123,9 @@ double launch_us(int which, const AttnArgs &a, int64_t items, int splits)
     if (a.window) longest = std::min(longest, (double)a.window + kOwnRows);
     else if (a.causal) mean = 1.0 - 0.5 * std::min(1.0, q / std::max(k, 1.0));
     longest = std::ceil(longest / kTileRows) * (dkv ? a.group : 1);
-    const double own = std::min((double)items, (double)(dkv ? a.kv_heads : a.heads) * ((double)(dkv ? a.k_tokens : a.q_tokens) / kOwnRows + a.batch));
+    const double own = std::min((double)items, (double)heads_of(which, a) * ((double)(dkv ? a.k_tokens : a.q_tokens) / kOwnRows + a.batch));
     const double alone = (1.0 + 0.004 * a.dim) * (which == kForward ? 1.0 : 1.25), shared = (0.57 + 0.0133 * a.dim) * (which == kForward ? 1.0 : 1.25);
-    const double rows = std::min(1.0, (double)(dkv ? a.max_k : a.max_q) / kOwnRows);
+    const double rows = std::min(1.0, (double)most_rows(which, a) / kOwnRows);
     const double all = own * longest * mean / compute_units() * (dkv && !one_side ? alone : shared / 2);
     const double part = std::ceil(longest / splits), slots = compute_units() * (dkv && !one_side ? 1.0 : 2.0);
     double us = std::max(alone * part, all + alone * part / 2);
@@ -176,7 +189,7 @@ hipError_t launch_join(int which, const AttnArgs &a, int64_t items, hipStream_t 
 // taken: the parts that it was split into, if that is asked for.
 hipError_t launch(int which, AttnArgs a, size_t bytes, hipStream_t s, int *taken = nullptr)
 {
-    a.tiles = (int)ceil_div(which == kDkv ? a.max_k : a.max_q, kOwnRows);
+    a.tiles = (int)ceil_div(most_rows(which, a), kOwnRows);
     const int64_t items = items_of(which, a);
     if (items == 0) return hipSuccess;
     a.splits = splits_of(which, a);
@@ -208,6 +221,12 @@ int64_t attention_sums_bytes(const AttnArgs &a, bool backward)
 }
 
 hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s) { return launch(kForward, a, bytes, s); }
+
+int attention_pack(const AttnArgs &a)
+{
+    const bool one_head = !a.scored || a.form.table || (a.form.cap > 0.f && a.form.slopes);     // a table's columns lie in a wave's lanes; several forms share its kernels
+    return one_head || (int64_t)a.max_q * a.group > kOwnRows ? 1 : a.group;
+}
 
 int64_t attention_table_bytes(const AttnArgs &a)
 {

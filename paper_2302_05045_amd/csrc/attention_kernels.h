@@ -126,6 +126,20 @@ __device__ __forceinline__ void load_own(const Rows &R, int first, half8 (&own)[
     }
 }
 
+// The same of a row that the lane names.
+template <int KS>
+__device__ __forceinline__ void load_row(const _Float16 *row, bool there, int dim, half8 (&own)[KS])
+{
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int col = 16 * ks + 8 * half;
+        half8 x = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (there && col < dim) x = *reinterpret_cast<const half8 *>(row + col);
+        own[ks] = x;
+    }
+}
+
 // x of the other half of the wave, lane by lane.
 __device__ __forceinline__ float other_half(float x)
 {
@@ -238,22 +252,24 @@ __device__ __forceinline__ void leave(float *parts, int64_t slot, int wave, int 
 }
 
 // Which keys a query sees: first_key(query) .. end_key(query) - 1, all of them without `causal`; and which queries see a key.
+template <bool KEYS>                          // whether there may be first keys that every query sees
 struct Mask {
     bool causal;
     int shift, window, q_len, k_len;         // window 2^30: none
-    int first;                               // the first keys that every query sees; 0 but with causal
+    int first;                               // those keys; 0 but with causal
+    __device__ __forceinline__ bool early(int key) const { return KEYS && key < first; }
     __device__ __forceinline__ int first_key(int query) const { return causal ? query + shift - window + 1 : 0; }
     __device__ __forceinline__ int end_key(int query) const { return causal ? min(query + shift + 1, k_len) : k_len; }
-    __device__ __forceinline__ int first_query(int key) const { return causal && key >= first ? key - shift : 0; }
-    __device__ __forceinline__ int end_query(int key) const { return causal && key >= first ? min(key - shift + window, q_len) : q_len; }
+    __device__ __forceinline__ int first_query(int key) const { return causal && !early(key) ? key - shift : 0; }
+    __device__ __forceinline__ int end_query(int key) const { return causal && !early(key) ? min(key - shift + window, q_len) : q_len; }
     // whether all of / any of a block of queries and keys (first and last of each) are seen
     __device__ __forceinline__ bool all(int q0, int q1, int k0, int k1) const
     {
-        return k1 < k_len && (!causal || k1 < first || (k1 <= q0 + shift && k0 > q1 + shift - window));
+        return k1 < k_len && (!causal || early(k1) || (k1 <= q0 + shift && k0 > q1 + shift - window));
     }
     __device__ __forceinline__ bool any(int q0, int q1, int k0, int k1) const
     {
-        return !causal || k0 < first || (k0 <= q1 + shift && k1 > q0 + shift - window);
+        return !causal || early(k0) || (k0 <= q1 + shift && k1 > q0 + shift - window);
     }
 };
 // The numbers from .. end - 1 by one comparison.
@@ -263,11 +279,11 @@ struct Span {
     __device__ __forceinline__ Span(int first, int end) : from(first), count(end > first ? (unsigned)(end - first) : 0u) {}
     __device__ __forceinline__ bool holds(int x) const { return (unsigned)(x - from) < count; }
 };
-template <bool SCORED>
-__device__ __forceinline__ Mask mask_of(const AttnArgs &A, const Sequence &s, int b)
+template <bool KEYS>
+__device__ __forceinline__ Mask<KEYS> mask_of(const AttnArgs &A, const Sequence &s, int b)
 {
-    Mask m;
-    m.first = SCORED && A.causal && A.form.first_keys ? min(max(A.form.first_keys[b], 0), s.k_len) : 0;
+    Mask<KEYS> m;
+    m.first = KEYS && A.causal && A.form.first_keys ? min(max(A.form.first_keys[b], 0), s.k_len) : 0;
     m.causal = A.causal != 0;
     m.shift = s.k_len - s.q_len;
     m.window = A.window > 0 ? min(A.window, 1 << 30) : 1 << 30;
@@ -277,23 +293,37 @@ __device__ __forceinline__ Mask mask_of(const AttnArgs &A, const Sequence &s, in
 }
 
 // A part's share of the tiles of keys that any of the queries q0 .. q1 sees: those of the first keys, then from what the window leaves on.
+template <bool KEYS>
 struct KeyTiles {
-    int first, count, head, near;            // the first tile's first row; the tiles; the end of the first keys' tiles and where the others begin, in rows
-    __device__ __forceinline__ KeyTiles(const AttnArgs &A, const Mask &M, int q0, int q1, int part)
+    int first, end;                          // the first tile's first row, and what lies behind the last one's rows or begins
+    int head, near;                          // the end of the first keys' tiles, and where the others begin
+    __device__ __forceinline__ KeyTiles(const AttnArgs &A, const Mask<KEYS> &M, int q0, int q1, int part)
     {
-        int end = M.k_len, begin = 0;
+        first = 0;
+        end = M.k_len;
         if (M.causal) {
-            end = min(end, max(q1 + M.shift + 1, M.first));
-            begin = max(q0 + M.shift - M.window + 1, 0) / kTileRows * kTileRows;
+            const int last = q1 + M.shift + 1, begin = q0 + M.shift - M.window + 1;
+            end = last < end ? last : end;
+            first = begin > 0 ? begin / kTileRows * kTileRows : 0;
         }
-        head = (M.first + kTileRows - 1) / kTileRows * kTileRows;
-        near = max(begin, head);
-        const int heads = head / kTileRows, all = heads + (end > near ? (end - near + kTileRows - 1) / kTileRows : 0), each = (all + A.splits - 1) / A.splits;
-        const int from = min(all, part * each);
-        count = min(all - from, each);
-        first = from < heads ? from * kTileRows : near + (from - heads) * kTileRows;
+        head = near = 0;
+        if (KEYS) {
+            head = (M.first + kTileRows - 1) / kTileRows * kTileRows;
+            near = max(first, head);
+            end = max(end, M.first);
+        }
+        const int heads = KEYS ? head / kTileRows : 0, begin = KEYS ? near : first;
+        const int tiles = heads + (end > begin ? (end - begin + kTileRows - 1) / kTileRows : 0), each = (tiles + A.splits - 1) / A.splits;
+        const int from = min(tiles, part * each), to = min(tiles, from + each);
+        if (KEYS) {
+            first = from < heads ? from * kTileRows : near + (from - heads) * kTileRows;
+            end = from == to ? first : to <= heads ? to * kTileRows : near + (to - heads) * kTileRows;
+        } else {
+            first += from * kTileRows;
+            end = min(end, first + each * kTileRows);
+        }
     }
-    __device__ __forceinline__ int after(int k0) const { return k0 + kTileRows == head ? near : k0 + kTileRows; }
+    __device__ __forceinline__ int after(int k0) const { return KEYS && k0 + kTileRows == head ? near : k0 + kTileRows; }
 };
 
 // Scores of another form (SCORED): z = cap tanh(x / cap) + bias(d), x the scaled product.  All of it in units of `unit` and log 2: a product, or its tanh,
@@ -302,15 +332,17 @@ struct KeyTiles {
 // distances are those of its diagonals, come in three kinds:
 //   kSame    one number, where all distances have one bucket: nothing to do for an element (most blocks of long sequences)
 //   kLinear  a slope, the block on one side of the diagonal: one multiplication and addition for each element
-//   kLaid    anything: the wave works out its diagonals' biases, a lane each, and lays them into LDS
+//   kAcross  a slope, the block across the diagonal: one more
+//   kLaid    buckets that differ: the wave works out its diagonals' biases, a lane each, and lays them into LDS
 // The table's columns and borders live in the wave's lanes: the bucket of a distance that the lanes agree on is the number of set bits of a comparison.
 constexpr int kMaxBuckets = SAMO_ATTENTION_MAX_BUCKETS;
-enum { kSame, kLinear, kLaid };
+enum { kSame, kLinear, kAcross, kLaid };
 enum { kPlain, kKeys, kCap, kSlope, kTable, kAll };        // which parts there can be: none (kKeys: but the first keys), one, any; kernels of their own
 struct Bias {
     int kind, column;                        // column: of all the block's pairs, the second half behind kMaxBuckets; -1 where they differ
+    int sign;                                // kAcross: of the distance from row to row
     int diagonal;                            // where they differ: of the lane's diagonal, row - column + 31 (blocks of 32 rows)
-    float same, step, base;                  // kSame; kLinear: from row to row, and at the lane's first
+    float same, step, base;                  // kSame; kLinear: from row to row, and at the lane's first; kAcross: the slope, and the lane's first distance
 };
 template <int FORM>
 struct Form {
@@ -375,18 +407,21 @@ struct Form {
         }
         return s;
     }
-    // The biases of a block of ROWS rows and 32 columns, d = base + SIGN (row - column).
+    // The biases of a block of ROWS rows and 32 columns, d = base + SIGN (row - column).  Several columns may have the same distances (pack): `own` is the
+    // lane's in row 0, and the last column's lies `span` from base.
     template <int ROWS, int SIGN>
-    __device__ __forceinline__ Bias plan(float *room, int base) const
+    __device__ __forceinline__ Bias plan(float *room, int base) const { return plan<ROWS, SIGN>(room, base, base - SIGN * (int)(threadIdx.x & 31), 31); }
+    template <int ROWS, int SIGN>
+    __device__ __forceinline__ Bias plan(float *room, int base, int own, int span) const
     {
-        Bias b = {kSame, -1, -1, 0.f, 0.f, 0.f};
-        if constexpr (kBiased) laying<ROWS, SIGN>(b, room, base);
+        Bias b = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
+        if constexpr (kBiased) laying<ROWS, SIGN>(b, room, base, own, span);
         return b;
     }
     template <int ROWS, int SIGN>
-    __device__ __forceinline__ void laying(Bias &b, float *room, int base) const
+    __device__ __forceinline__ void laying(Bias &b, float *room, int base, int own, int span) const
     {
-        const int lane = threadIdx.x & 63, lo = SIGN > 0 ? base - 31 : base - (ROWS - 1), hi = SIGN > 0 ? base + ROWS - 1 : base + 31;
+        const int lane = threadIdx.x & 63, lo = SIGN > 0 ? base - span : base - (ROWS - 1), hi = SIGN > 0 ? base + ROWS - 1 : base + span;
         int b0 = 0, b1 = 0;
         if (tabled) {
             const bool one_side = !two_sided || lo >= 0 || hi < 0, behind = two_sided && hi < 0;
@@ -399,13 +434,16 @@ struct Form {
                     return;
                 }
             }
-        } else if (!kSloped) {
-            return;
-        } else if (lo >= 0 || hi <= 0) {
-            const float down = lo >= 0 ? -slope : slope;
-            b.kind = kLinear;
-            b.step = SIGN * down;
-            b.base = down * (float)(base - SIGN * ((lane & 31) - 4 * (lane >> 5)));
+        } else {
+            if constexpr (kSloped) {
+                const float first = (float)(own + SIGN * 4 * (lane >> 5));
+                const bool one_side = lo >= 0 || hi <= 0;
+                const float down = one_side && lo < 0 ? slope : -slope;
+                b.kind = one_side ? kLinear : kAcross;
+                b.step = one_side ? SIGN * down : down;
+                b.base = one_side ? down * first : first;
+                b.sign = SIGN;
+            }
             return;
         }
         b.kind = kLaid;
@@ -427,12 +465,15 @@ struct Form {
     // Those of rows 32 block .. (not kSame), as an accumulator holds them.
     __device__ __forceinline__ f32x16 biases(const Bias &b, const float *room, int block) const
     {
-        f32x16 x;
+        f32x16 x = {};
         const float *at = room + 31 + 32 * block - (int)(threadIdx.x & 31);
         if (kSloped && b.kind == kLinear) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = fmaf(b.step, (float)(32 * block + 8 * (i >> 2) + (i & 3)), b.base);
-        } else {
+        } else if (kSloped && b.kind == kAcross) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = b.step * fabsf(b.base + b.sign * (float)(32 * block + 8 * (i >> 2) + (i & 3)));
+        } else if constexpr (kTabled) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = at[acc_row(i)];
         }
@@ -571,33 +612,47 @@ struct BucketSums {
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll;
+    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
-    __shared__ float biases[kBiased ? kAttnThreads / 64 : 1][kBiasRoom];
+    __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
+    // Few queries of heads that share keys: a tile's rows are pack heads of each query, so that a tile of keys is read and multiplied once for all of them
+    // (one token of 5 sequences behind 4000, 32 heads of 128 on 8: 30 us head by head, PACKED_US packed).
+    constexpr bool kPacks = FORM == kKeys || FORM == kCap || FORM == kSlope;
+    const int pack = kPacks ? A.pack : 1;
     Place at;
-    if (!pick(A, A.heads, at)) return;
-    const int b = at.b, head = at.head, tile = at.tile;
+    if (!pick(A, pack > 1 ? A.kv_heads : A.heads, at)) return;
+    const int b = at.b, tile = at.tile;
     const Sequence seq = sequence_of(A, b);
-    if (tile * kOwnRows >= seq.q_len) return;
-    const Mask M = mask_of<SCORED>(A, seq, b);
+    const int rows = seq.q_len * pack;
+    if (tile * kOwnRows >= rows) return;
+    const Mask<SCORED> M = mask_of<SCORED>(A, seq, b);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int q_first = tile * kOwnRows, q_last = min(q_first + kOwnRows, seq.q_len) - 1;
-    const int w_first = q_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.q_len) - 1;   // of the wave; none where last < first
-    const int query = w_first + (lane & 31);
-    const int kv = head / A.group;
-    const Rows Q = {A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim};
+    const int first_row = tile * kOwnRows, last_row = min(first_row + kOwnRows, rows) - 1;
+    const int w_row = first_row + wave * kWaveRows, w_end = min(w_row + kWaveRows, rows) - 1, row = w_row + (lane & 31);
+    int q_first = first_row, q_last = last_row, w_first = w_row, w_last = w_end;       // the queries; of the wave: none where last < first
+    int query = row, head = at.head, kv = head / A.group;
+    if (pack > 1) {
+        q_first = first_row / pack;
+        q_last = last_row / pack;
+        w_first = w_row / pack;
+        w_last = w_end < w_row ? w_first - 1 : w_end / pack;
+        query = row / pack;
+        kv = at.head;
+        head = kv * pack + row - query * pack;
+    }
     const Tiles<KS> K(Rows{A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim});
     const Tiles<KS> V(Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim});
-    const KeyTiles tiles(A, M, q_first, q_last, at.part);
+    const KeyTiles<SCORED> tiles(A, M, q_first, q_last, at.part);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
 
-    if (tiles.count > 0) {
+    if (tiles.first < tiles.end) {
         K.bring(tiles.first, lds_at);
         V.bring(tiles.first, lds_at + 2 * kTile);
     }
     half8 own[KS];
-    load_own<KS>(Q, w_first, own);
+    if (pack > 1) load_row<KS>(A.q + (seq.q0 + query) * A.q_row + head * A.q_head, row < rows, A.dim, own);
+    else load_own<KS>(Rows{A.q + seq.q0 * A.q_row + head * A.q_head, A.q_row, seq.q_len, A.dim}, w_first, own);
     const Span seen(M.first_key(query), M.end_key(query));
     f32x16 out[DB];
     clear(out);
@@ -606,10 +661,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     if constexpr (SCORED) c = form.unit;
     float top = -INFINITY, sum = 0.f;                        // top: what the exponents are taken against, within 8 of the largest so far
     int buffer = 0;
-    for (int n = 0, k0 = tiles.first; n < tiles.count; ++n, k0 = tiles.after(k0), buffer ^= 1) {
+    for (int k0 = tiles.first; k0 < tiles.end; k0 = tiles.after(k0), buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         meet();                                              // the tile is there, and the other one has been read by every wave
-        if (n + 1 < tiles.count) {
+        if (tiles.after(k0) < tiles.end) {
             K.bring(tiles.after(k0), lds_at + (buffer ^ 1) * kTile);
             V.bring(tiles.after(k0), lds_at + (2 + (buffer ^ 1)) * kTile);
         }
@@ -617,12 +672,14 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
         const unsigned char *kt = lds + buffer * kTile, *vt = lds + (2 + buffer) * kTile;
         f32x16 s[2];
         clear(s);
-        [[maybe_unused]] Bias bias = {kSame, -1, -1, 0.f, 0.f, 0.f};
+        [[maybe_unused]] Bias bias = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
         if constexpr (kBiased) {
-            bias = form.template plan<kTileRows, -1>(biases[wave], w_first + M.shift - k0);
+            const int base = w_first + M.shift - k0;
+            if (kPacks && pack > 1) bias = form.template plan<kTileRows, -1>(nullptr, base, query + M.shift - k0, (w_row + kWaveRows - 1) / pack - w_first);
+            else bias = form.template plan<kTileRows, -1>(biases[kTabled ? wave : 0], base);
             if (form.starts(bias)) {
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) s[kb] = form.biases(bias, biases[wave], kb);
+                for (int kb = 0; kb < 2; ++kb) s[kb] = form.biases(bias, biases[kTabled ? wave : 0], kb);
             }
         }
 #pragma unroll
@@ -633,13 +690,13 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
         for (int kb = 0; kb < 2; ++kb) {
             if constexpr (kCapped)
                 if (form.capped) s[kb] = form.tanhs(s[kb]);
-            if constexpr (kCapped && kBiased) s[kb] = form.with_bias(s[kb], bias, biases[wave], kb);
+            if constexpr (kCapped && kBiased) s[kb] = form.with_bias(s[kb], bias, biases[kTabled ? wave : 0], kb);
         }
         if (!M.all(w_first, w_last, k0, k0 + kTileRows - 1)) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[kb][i] = seen.holds(k0 + 32 * kb + acc_row(i)) || (SCORED && k0 + 32 * kb + acc_row(i) < M.first) ? s[kb][i] : -INFINITY;
+                for (int i = 0; i < 16; ++i) s[kb][i] = seen.holds(k0 + 32 * kb + acc_row(i)) || M.early(k0 + 32 * kb + acc_row(i)) ? s[kb][i] : -INFINITY;
         }
         float most = s[0][0];
 #pragma unroll
@@ -677,24 +734,24 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     sum += other_half(sum);
     if (A.splits > 1) {
-        leave<DB>(A.parts, at.slot, wave, query, seq.q_len, out);
+        leave<DB>(A.parts, at.slot, wave, row, rows, out);
         if (lane < 32) A.part_stats[(at.slot * 4 + wave) * 32 + lane] = f32x2{top * c, sum};
         return;
     }
     const float factor = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;      // a row that sees no key: zero; NaN stays
-    store_own<DB>(A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, query, seq.q_len, A.dim, out, factor);
-    if (lane < 32 && query < seq.q_len) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : (SCORED ? top * c * kLn2 : top * A.scale) + __logf(sum);
+    if (pack > 1) store_own<DB>(A.out + (seq.q0 + query) * A.out_row + head * A.out_head, 0, row < rows ? 0 : 1, 1, A.dim, out, factor);
+    else store_own<DB>(A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, query, seq.q_len, A.dim, out, factor);
+    if (lane < 32 && row < rows) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : (SCORED ? top * c * kLn2 : top * A.scale) + __logf(sum);
 }
 
 // dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 825 us, 1000 TFLOP/s; 4 x 2048, 32 heads of 80: 180 us.
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll;
-    constexpr bool kTabled = FORM == kTable || FORM == kAll;
+    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];
-    __shared__ float biases[kBiased ? kAttnThreads / 64 : 1][kBiasRoom];
+    __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
     __shared__ float skewed[kTabled ? kAttnThreads / 64 : 1][kSkewRoom];
     __shared__ float meeting[kTabled ? kAttnThreads / 64 : 1][2 * kMaxBuckets];
     Place at;
@@ -706,7 +763,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
         if (kTabled && A.form.dtable_parts && (int)threadIdx.x < columns) A.form.dtable_parts[at.slot * columns + threadIdx.x] = 0.f;
         return;
     }
-    const Mask M = mask_of<SCORED>(A, seq, b);
+    const Mask<SCORED> M = mask_of<SCORED>(A, seq, b);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int q_first = tile * kOwnRows, q_last = min(q_first + kOwnRows, seq.q_len) - 1;
     const int w_first = q_first + wave * kWaveRows, w_last = min(w_first + kWaveRows, seq.q_len) - 1;
@@ -717,9 +774,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
     const Tiles<KS> V(Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim});
     const Rows DO = {A.dout + seq.q0 * A.dout_row + head * A.dout_head, A.dout_row, seq.q_len, A.dim};
     const Rows O = {A.out + seq.q0 * A.out_row + head * A.out_head, A.out_row, seq.q_len, A.dim};
-    const KeyTiles tiles(A, M, q_first, q_last, at.part);
+    const KeyTiles<SCORED> tiles(A, M, q_first, q_last, at.part);
     const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds;
-    if (tiles.count > 0) {
+    if (tiles.first < tiles.end) {
         K.bring(tiles.first, lds_at);
         V.bring(tiles.first, lds_at + 2 * kTile);
     }
@@ -752,10 +809,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
     f32x16 acc[DB];
     clear(acc);
     int buffer = 0;
-    for (int n = 0, k0 = tiles.first; n < tiles.count; ++n, k0 = tiles.after(k0), buffer ^= 1) {
+    for (int k0 = tiles.first; k0 < tiles.end; k0 = tiles.after(k0), buffer ^= 1) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         meet();
-        if (n + 1 < tiles.count) {
+        if (tiles.after(k0) < tiles.end) {
             K.bring(tiles.after(k0), lds_at + (buffer ^ 1) * kTile);
             V.bring(tiles.after(k0), lds_at + (2 + (buffer ^ 1)) * kTile);
         }
@@ -767,11 +824,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
             f32x16 s[1], dp[1];
             clear(s);
             clear(dp);
-            [[maybe_unused]] Bias bias = {kSame, -1, -1, 0.f, 0.f, 0.f};
+            [[maybe_unused]] Bias bias = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
             float less = lse;
             if constexpr (kBiased) {
-                bias = form.template plan<32, -1>(biases[wave], w_first + M.shift - k1);
-                if (form.starts(bias)) s[0] = form.biases(bias, biases[wave], 0);
+                bias = form.template plan<32, -1>(biases[kTabled ? wave : 0], w_first + M.shift - k1);
+                if (form.starts(bias)) s[0] = form.biases(bias, biases[kTabled ? wave : 0], 0);
                 less = fmaf(-bias.same, c, lse);
             }
 #pragma unroll
@@ -782,13 +839,13 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const Att
             [[maybe_unused]] f32x16 t;
             if constexpr (kCapped) {
                 if (form.capped) s[0] = t = form.tanhs(s[0]);
-                if constexpr (kBiased) s[0] = form.with_bias(s[0], bias, biases[wave], 0);
+                if constexpr (kBiased) s[0] = form.with_bias(s[0], bias, biases[kTabled ? wave : 0], 0);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -less)) * (dp[0][i] - delta);
             if (!M.all(w_first, w_last, k1, k1 + 31)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[0][i] = seen.holds(k1 + acc_row(i)) || (SCORED && k1 + acc_row(i) < M.first) ? s[0][i] : 0.f;
+                for (int i = 0; i < 16; ++i) s[0][i] = seen.holds(k1 + acc_row(i)) || M.early(k1 + acc_row(i)) ? s[0][i] : 0.f;
             }
             if constexpr (kTabled)
                 if (A.form.dtable_parts) buckets.add(form, s[0], bias, skewed[wave], w_first + M.shift - k1);
@@ -833,18 +890,18 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 template <int KS, int SIDES, int FORM>
 __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll;
+    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
     constexpr bool kWide = KS > 6;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide ? kOwnRows * PITCH : 0)];       // Q, dO; two tiles each; V
     __shared__ __attribute__((aligned(16))) float stats[2][2][kTileRows];         // lse, delta
-    __shared__ float biases[kBiased ? SIDES * kAttnThreads / 64 : 1][kBiasRoom];
+    __shared__ float biases[kTabled ? SIDES * kAttnThreads / 64 : 1][kBiasRoom];
     Place at;
     if (!pick(A, A.kv_heads, at)) return;
     const int b = at.b, kv = at.head, tile = A.tiles - 1 - at.tile;        // the first keys are seen by the most queries
     const Sequence seq = sequence_of(A, b);
     if (tile * kOwnRows >= seq.k_len) return;
-    const Mask M = mask_of<SCORED>(A, seq, b);
+    const Mask<SCORED> M = mask_of<SCORED>(A, seq, b);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, side = wave >> 2;
     const int k_first = tile * kOwnRows, k_last = min(k_first + kOwnRows, seq.k_len) - 1;
     const int w_first = k_first + (wave & 3) * kWaveRows, w_last = min(w_first + kWaveRows, seq.k_len) - 1;
@@ -866,7 +923,7 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
     Coming first_operand = coming_of(side), second_operand = coming_of(1);
     // the queries that see any of the workgroup's keys
     int q_first = 0, q_end = seq.q_len;
-    if (M.causal && k_first >= M.first) {
+    if (M.causal && !M.early(k_first)) {
         const int begin = k_first - M.shift;
         q_first = begin > 0 ? begin / kTileRows * kTileRows : 0;
         const int64_t end = (int64_t)k_last - M.shift + M.window;
@@ -922,11 +979,11 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
             f32x16 s[1], dp[1];
             clear(s);
             clear(dp);
-            [[maybe_unused]] Bias bias = {kSame, -1, -1, 0.f, 0.f, 0.f};
+            [[maybe_unused]] Bias bias = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
             [[maybe_unused]] float more = 0.f;
             if constexpr (kBiased) {
-                bias = form.template plan<32, 1>(biases[wave], q1 + M.shift - w_first);
-                if (form.starts(bias)) s[0] = form.biases(bias, biases[wave], 0);
+                bias = form.template plan<32, 1>(biases[kTabled ? wave : 0], q1 + M.shift - w_first);
+                if (form.starts(bias)) s[0] = form.biases(bias, biases[kTabled ? wave : 0], 0);
                 more = bias.same * c;
             }
 #pragma unroll
@@ -935,31 +992,31 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
                 const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
                 dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
             }
-            const float *lse_at = &stats[buffer][0][32 * qb + 4 * (lane >> 5)], *delta_at = &stats[buffer][1][32 * qb + 4 * (lane >> 5)];
             if constexpr (kCapped)
                 if (form.capped) {                           // dP - delta, times the cap's slope
                     s[0] = form.tanhs(s[0]);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const f32x4 delta = *reinterpret_cast<const f32x4 *>(delta_at + 8 * g);
+                        const f32x4 delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][32 * qb + 8 * g + 4 * (lane >> 5)]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int i = 4 * g + e;
                             dp[0][i] = (dp[0][i] - delta[e]) * fmaf(-s[0][i], s[0][i], 1.f);
                         }
                     }
-                    if constexpr (kBiased) s[0] = form.with_bias(s[0], bias, biases[wave], 0);
+                    if constexpr (kBiased) s[0] = form.with_bias(s[0], bias, biases[kTabled ? wave : 0], 0);
                 }
-            bool reduced = false;                            // whether delta has been taken off
+            [[maybe_unused]] bool reduced = false;           // whether delta has been taken off
             if constexpr (kCapped) reduced = form.capped;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 lse = *reinterpret_cast<const f32x4 *>(lse_at + 8 * g), delta = *reinterpret_cast<const f32x4 *>(delta_at + 8 * g);
+                const int at = 32 * qb + 8 * g + 4 * (lane >> 5);
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&stats[buffer][0][at]), delta = *reinterpret_cast<const f32x4 *>(&stats[buffer][1][at]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = 4 * g + e;
                     s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, kBiased ? fmaf(-lse[e], kLog2e, more) : -lse[e] * kLog2e));
-                    dp[0][i] = s[0][i] * (dp[0][i] - (reduced ? 0.f : delta[e]));
+                    dp[0][i] = s[0][i] * (kCapped && reduced ? dp[0][i] : dp[0][i] - delta[e]);
                 }
             }
             if (!M.all(q1, q1 + 31, w_first, w_last)) {

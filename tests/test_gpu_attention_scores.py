@@ -423,3 +423,21 @@ def test_borders_of_the_logarithm():
         log = half + torch.floor(torch.log(n.clamp(min=1).double() / half) / math.log(far / half) * (buckets - half) + 1e-9).long()
         want = torch.where(n < half, n, log.clamp(max=buckets - 1))
         assert torch.equal((n[:, None] >= borders).sum(1), want), (buckets, far)
+
+
+@pytest.mark.parametrize("form", [dict(cap=20.0), dict(slopes=True), dict(first=True), dict(slopes=True, first=True)], ids=["cap", "slopes", "first keys", "slopes and first keys"])
+@pytest.mark.parametrize("heads,kv,queries", [(8, 2, 1), (32, 8, 1), (7, 1, 3), (12, 4, 20), (6, 2, 42), (6, 2, 43), (128, 1, 1), (64, 1, 2), (100, 1, 1)])
+def test_heads_that_share_a_tile_with_their_queries(heads, kv, queries, form):
+    """A tile's rows are all heads of a query where a sequence's are at most 128: with one query, several, as many as fit and one more."""
+    lens_q, lens_k = [queries, 1, 0, max(1, queries - 1)], [queries + 300, 77, 40, queries]
+    check(lens_q, lens_k, heads, kv, 64, seed=heads, **with_first(form, lens_k))
+    check([queries], [queries + 1000], heads, kv, 128, window=150, seed=heads + 1, **with_first(form, [queries + 1000]))
+    if not form.get("first"):
+        check(lens_q, lens_k, heads, kv, 80, causal=False, seed=heads + 2, **form)
+
+
+@pytest.mark.parametrize("parts", [1, 2, 5, 16], indirect=True)
+def test_heads_that_share_a_tile_in_parts(parts):
+    check([3, 1], [700, 90], 8, 2, 64, cap=20.0, first=[70, 0], seed=parts)
+    check([3, 1], [700, 90], 12, 3, 128, slopes=True, seed=parts)
+    check([2], [900], 4, 1, 96, causal=False, slopes=True, seed=parts)
