@@ -1343,7 +1343,7 @@ samo_status check_scores(const samo_attention_scores *s, bool backward, AttnArgs
     a->form.two_sided = s->two_sided != 0;
     a->form.first_keys = s->d_first_keys;
     a->form.dtable = backward ? reinterpret_cast<_Float16 *>(s->d_dtable) : nullptr;
-    a->pack = attention_pack(*a);
+    attention_pack(*a);
     return SAMO_OK;
 }
 

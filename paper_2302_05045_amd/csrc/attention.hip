@@ -145,6 +145,19 @@ int splits_of(int which, const AttnArgs &a)
     // in two parts, backward 1983 and 2107).
     if (items >= (which == kDkv && a.dim > 64 ? 2 : 4) * compute_units()) return 1;
     int best = 1;
+    if (which == kForward && a.few) {                        // four tiles at once in a workgroup, a part besides for the second kernel's 5 us
+        const int64_t longest = a.window ? std::min<int64_t>(a.max_k, a.window + most_rows(which, a)) : a.max_k, tiles = ceil_div(longest, kTileRows);
+        const int64_t slots = compute_units() * (a.dim > 64 ? 1 : 2);
+        double least = 1e30;
+        for (int splits = 1; splits <= kMost && items * splits <= kSlots; ++splits) {
+            const double us = 1.6 * (double)ceil_div(ceil_div(tiles, splits), 4) * (double)ceil_div(items * splits, slots) + (splits > 1 ? 5.0 + 0.15 * splits : 0.0);
+            if (us < least) {
+                least = us;
+                best = splits;
+            }
+        }
+        return best;
+    }
     double least = launch_us(which, a, items, 1);
     if (least < 12.0) return 1;                              // two parts take six of them, and five for the second kernel
     for (int splits = 2; splits <= kMost && items * splits <= kSlots; ++splits) {
@@ -222,10 +235,11 @@ int64_t attention_sums_bytes(const AttnArgs &a, bool backward)
 
 hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s) { return launch(kForward, a, bytes, s); }
 
-int attention_pack(const AttnArgs &a)
+void attention_pack(AttnArgs &a)
 {
     const bool one_head = !a.scored || a.form.table || (a.form.cap > 0.f && a.form.slopes);     // a table's columns lie in a wave's lanes; several forms share its kernels
-    return one_head || (int64_t)a.max_q * a.group > kOwnRows ? 1 : a.group;
+    a.pack = one_head || (int64_t)a.max_q * a.group > kOwnRows ? 1 : a.group;
+    a.few = a.scored && most_rows(kForward, a) <= kWaveRows;
 }
 
 int64_t attention_table_bytes(const AttnArgs &a)

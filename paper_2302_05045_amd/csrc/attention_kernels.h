@@ -89,6 +89,23 @@ struct Tiles {
     }
 };
 
+// A tile copied by one wave: its kWhole instructions.
+template <int KS>
+struct OwnTiles {
+    static constexpr int PITCH = pitch_of(KS), kPieces = PITCH / 16, kRowsPer = 64 / kPieces, kWhole = kTileRows / kRowsPer;
+    Rows R;
+    __device__ __forceinline__ void bring(int first, unsigned lds_at) const
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kWhole; ++i) {
+            const int in_tile = i * kRowsPer + lane / kPieces, row = first + in_tile, piece = lane % kPieces ^ swizzle<PITCH>(in_tile);
+            const bool there = row < R.count && piece * 8 < R.dim;
+            dma16(there ? static_cast<const void *>(R.base + (int64_t)row * R.stride + piece * 8) : zero_row, lds_at + i * 1024);
+        }
+    }
+};
+
 // Operand with the tile's rows as its rows (32 of them from row 32 block) and 16 columns from 16 ks.
 template <int PITCH>
 __device__ __forceinline__ half8 read_rows(const unsigned char *tile, int block, int ks)
@@ -297,6 +314,7 @@ template <bool KEYS>
 struct KeyTiles {
     int first, end;                          // the first tile's first row, and what lies behind the last one's rows or begins
     int head, near;                          // the end of the first keys' tiles, and where the others begin
+    int from, count;                         // of all tiles, those of the part
     __device__ __forceinline__ KeyTiles(const AttnArgs &A, const Mask<KEYS> &M, int q0, int q1, int part)
     {
         first = 0;
@@ -314,7 +332,9 @@ struct KeyTiles {
         }
         const int heads = KEYS ? head / kTileRows : 0, begin = KEYS ? near : first;
         const int tiles = heads + (end > begin ? (end - begin + kTileRows - 1) / kTileRows : 0), each = (tiles + A.splits - 1) / A.splits;
-        const int from = min(tiles, part * each), to = min(tiles, from + each);
+        from = min(tiles, part * each);
+        const int to = min(tiles, from + each);
+        count = to - from;
         if (KEYS) {
             first = from < heads ? from * kTileRows : near + (from - heads) * kTileRows;
             end = from == to ? first : to <= heads ? to * kTileRows : near + (to - heads) * kTileRows;
@@ -322,6 +342,11 @@ struct KeyTiles {
             first += from * kTileRows;
             end = min(end, first + each * kTileRows);
         }
+    }
+    __device__ __forceinline__ int at(int n) const       // the first row of the part's nth tile, where there may be first keys
+    {
+        const int heads = head / kTileRows, i = from + n;
+        return i < heads ? i * kTileRows : near + (i - heads) * kTileRows;
     }
     __device__ __forceinline__ int after(int k0) const { return KEYS && k0 + kTileRows == head ? near : k0 + kTileRows; }
 };
@@ -744,6 +769,158 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnAr
     if (lane < 32 && row < rows) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : (SCORED ? top * c * kLn2 : top * A.scale) + __logf(sum);
 }
 
+// The forward pass of at most 32 rows: a token, or a few, of one sequence, with the heads that share their keys (pack).  The four waves of a workgroup have
+// the same rows and every fourth tile of the part's keys each, which they copy for themselves, multiply and wait for by themselves: with
+// rows for one wave alone it is the chain of a tile (copy, product, softmax, product) that takes the time, and here four go on at once.  The next tile's
+// keys are under way from the first product on, its values from the second.  The waves' sums meet in LDS, the parts' in attention_join_kernel.
+template <int KS, int FORM>
+__global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnArgs A)
+{
+    constexpr bool kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
+    constexpr bool kPacks = FORM == kKeys || FORM == kCap || FORM == kSlope;
+    constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS), kWaves = kAttnThreads / 64;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kWaves][2 * kTile];            // a wave's K, V
+    __shared__ float biases[kTabled ? kWaves : 1][kBiasRoom];
+    __shared__ f32x2 stats[kWaves][kWaveRows];
+    static_assert(DB * 4096 <= 2 * kTile && DB <= kWaves, "a wave's sums lie where its tiles were, and a wave joins 32 dims");
+    const int pack = kPacks ? A.pack : 1;
+    Place at;
+    if (!pick(A, pack > 1 ? A.kv_heads : A.heads, at)) return;
+    const Sequence seq = sequence_of(A, at.b);
+    const int rows = seq.q_len * pack;
+    if (rows == 0) return;
+    const Mask<true> M = mask_of<true>(A, seq, at.b);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 31, query = row / pack;
+    const int kv = pack > 1 ? at.head : at.head / A.group, head = pack > 1 ? kv * pack + row - query * pack : at.head, last = (rows - 1) / pack;
+    const OwnTiles<KS> K = {Rows{A.k + seq.k0 * A.k_row + kv * A.k_head, A.k_row, seq.k_len, A.dim}};
+    const OwnTiles<KS> V = {Rows{A.v + seq.k0 * A.v_row + kv * A.v_head, A.v_row, seq.k_len, A.dim}};
+    const KeyTiles<true> tiles(A, M, 0, last, at.part);
+    const unsigned char *kt = lds[wave], *vt = kt + kTile;
+    const unsigned lds_at = (unsigned)(size_t)(LDS_AS unsigned char *)lds + wave * 2 * kTile;
+    half8 own[KS];
+    load_row<KS>(A.q + (seq.q0 + query) * A.q_row + head * A.q_head, row < rows, A.dim, own);
+    const auto form = form_of<FORM>(A, head < A.heads ? head : A.heads - 1);
+    if (wave < tiles.count) {
+        K.bring(tiles.at(wave), lds_at);
+        V.bring(tiles.at(wave), lds_at + kTile);
+    }
+    const Span seen(M.first_key(query), M.end_key(query));
+    const float c = form.unit;
+    f32x16 out[DB];
+    clear(out);
+    float top = -INFINITY, sum = 0.f;
+    for (int n = wave; n < tiles.count; n += kWaves) {
+        const int k0 = tiles.at(n);
+        const bool more = n + kWaves < tiles.count;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OwnTiles<KS>::kWhole) : "memory");       // but for the values, which were asked for last
+        f32x16 s[2];
+        clear(s);
+        [[maybe_unused]] Bias bias = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
+        if constexpr (kBiased) {
+            const int base = M.shift - k0;
+            if (pack > 1) bias = form.template plan<kTileRows, -1>(nullptr, base, query + base, (kWaveRows - 1) / pack);
+            else bias = form.template plan<kTileRows, -1>(biases[kTabled ? wave : 0], base);
+            if (form.starts(bias)) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) s[kb] = form.biases(bias, biases[kTabled ? wave : 0], kb);
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(kt, kb, ks), own[ks], s[kb], 0, 0, 0);
+        if (more) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                             // the keys have been read
+            K.bring(tiles.at(n + kWaves), lds_at);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            if constexpr (kCapped)
+                if (form.capped) s[kb] = form.tanhs(s[kb]);
+            if constexpr (kCapped && kBiased) s[kb] = form.with_bias(s[kb], bias, biases[kTabled ? wave : 0], kb);
+        }
+        if (!M.all(0, last, k0, k0 + kTileRows - 1)) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kb][i] = seen.holds(k0 + 32 * kb + acc_row(i)) || M.early(k0 + 32 * kb + acc_row(i)) ? s[kb][i] : -INFINITY;
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) most = fmaxf(most, s[i >> 4][i & 15]);
+        most = fmaxf(most, other_half(most));
+        if constexpr (kBiased) most += bias.same;
+        const float next = fmaxf(top, most), down = next == top ? 1.f : __builtin_amdgcn_exp2f((top - next) * c);
+        top = next;
+        sum *= down;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) out[db][i] *= down;
+        float against = top == -INFINITY ? 0.f : top * c;
+        if constexpr (kBiased) against -= bias.same * c;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -against));
+                sum += s[kb][i];
+            }
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OwnTiles<KS>::kWhole) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            const half8 p = to_half8(s[step >> 1], 8 * (step & 1));
+#pragma unroll
+            for (int db = 0; db < DB; ++db) out[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_columns<PITCH>(vt, step, db), p, out[db], 0, 0, 0);
+        }
+        if (more) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            V.bring(tiles.at(n + kWaves), lds_at + kTile);
+        }
+    }
+    sum += other_half(sum);
+    if (lane < kWaveRows) stats[wave][lane] = f32x2{top * c, sum};
+    f32x4 *mine = reinterpret_cast<f32x4 *>(lds[wave]) + lane;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) mine[(4 * db + g) * 64] = f32x4{out[db][4 * g], out[db][4 * g + 1], out[db][4 * g + 2], out[db][4 * g + 3]};
+    __syncthreads();
+    if (wave >= DB) return;
+    // 32 dims of all rows: the waves' sums, weighed by how far their exponents were taken down
+    f32x16 all[1];
+    clear(all);
+    top = -INFINITY;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = stats[w][row][1] != 0.f ? fmaxf(top, stats[w][row][0]) : top;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const f32x2 stat = stats[w][row];
+        const float weight = stat[1] != 0.f ? __builtin_amdgcn_exp2f(stat[0] - top) : 0.f;
+        sum = fmaf(stat[1], weight, sum);
+        const f32x4 *from = reinterpret_cast<const f32x4 *>(lds[w]) + 4 * wave * 64 + lane;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 x = from[g * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) all[0][4 * g + e] = fmaf(x[e], weight, all[0][4 * g + e]);
+        }
+    }
+    if (row >= rows) return;
+    if (A.splits > 1) {
+        f32x4 *to = sums_of<DB>(A.parts, at.slot, 0) + 4 * wave * 64;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) to[g * 64] = f32x4{all[0][4 * g], all[0][4 * g + 1], all[0][4 * g + 2], all[0][4 * g + 3]};
+        if (wave == 0 && lane < kWaveRows) A.part_stats[at.slot * 4 * kWaveRows + lane] = f32x2{top, sum};
+        return;
+    }
+    const float factor = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+    store_own<1>(A.out + (seq.q0 + query) * A.out_row + head * A.out_head + 32 * wave, 0, 0, 1, A.dim - 32 * wave, all, factor);
+    if (wave == 0 && lane < kWaveRows) A.lse[(int64_t)head * A.q_tokens + seq.q0 + query] = sum == 0.f ? -INFINITY : top * kLn2 + __logf(sum);
+}
+
 // dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 825 us, 1000 TFLOP/s; 4 x 2048, 32 heads of 80: 180 us.
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const AttnArgs A)
@@ -1100,6 +1277,11 @@ template <int KS, int FORM>
 hipError_t launch_dim(int which, const AttnArgs &a, int64_t items, hipStream_t s)
 {
     const dim3 grid((unsigned)(places_of(items / a.tiles, a.tiles) * a.splits * 8));
+    if constexpr (FORM != kPlain)
+        if (which == kForward && a.few) {
+            hipLaunchKernelGGL((attention_few_kernel<KS, FORM>), grid, dim3(kAttnThreads), 0, s, a);
+            return hipGetLastError();
+        }
     if (which == kForward) hipLaunchKernelGGL((attention_kernel<KS, FORM>), grid, dim3(kAttnThreads), 0, s, a);
     else if (which == kDq) hipLaunchKernelGGL((attention_dq_kernel<KS, FORM>), grid, dim3(kAttnThreads), 0, s, a);
     else if (KS <= 6 && items * a.splits >= one_side_from(a.dim))

@@ -267,6 +267,7 @@ struct AttnArgs {
     float *parts;                           // NULL: a launch is not split
     f32x2 *part_stats;
     int pack;                               // forward: heads of a query that a tile's rows hold, 1 or group
+    int few;                                // forward: a sequence's rows are at most 32, and scored
     int scored;                             // whether form is looked at
     AttnForm form;
 };
@@ -274,8 +275,8 @@ struct AttnArgs {
 bool attention_fits(const samo_attention_desc &d, bool backward);
 // Bytes that a call can use at `parts`; with less a launch that would need them is not split.
 int64_t attention_sums_bytes(const AttnArgs &a, bool backward);
-// pack: group where a form's kernels can and a sequence's rows are one tile.
-int attention_pack(const AttnArgs &a);
+// Sets pack and few of a scored call: group where a form's kernels can and a sequence's rows are one tile.
+void attention_pack(AttnArgs &a);
 // Bytes that a backward call needs at form.dtable_parts.
 int64_t attention_table_bytes(const AttnArgs &a);
 hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s);

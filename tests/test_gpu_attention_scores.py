@@ -441,3 +441,24 @@ def test_heads_that_share_a_tile_in_parts(parts):
     check([3, 1], [700, 90], 8, 2, 64, cap=20.0, first=[70, 0], seed=parts)
     check([3, 1], [700, 90], 12, 3, 128, slopes=True, seed=parts)
     check([2], [900], 4, 1, 96, causal=False, slopes=True, seed=parts)
+
+
+@pytest.mark.parametrize("form", FORMS, ids=NAMES)
+@pytest.mark.parametrize("dim", [16, 64, 80, 96, 128])
+def test_few_queries_of_every_form(form, dim):
+    """At most 32 rows: the four waves share the keys.  No key, one, tiles for one wave, all of them, one more; 1, 31, 32 and 33 queries of one head."""
+    lens_k = [0, 1, 63, 64, 65, 256, 257, 300, 900]
+    lens_q = [1, 1, 3, 1, 2, 1, 1, 0, 2]
+    check(lens_q, lens_k, 4, 2, dim, seed=dim, **with_first(form, lens_k))
+    for n in (31, 32, 33):
+        check([n, 5], [n + 170, 700], 2, 2, dim, seed=n, **with_first(form, [n + 170, 700]))
+    if not form.get("first"):
+        check(lens_q, lens_k, 4, 4, dim, causal=False, seed=dim, **form)
+
+
+@pytest.mark.parametrize("parts", [1, 2, 3, 9, 16], indirect=True)
+def test_few_queries_in_parts(parts):
+    form = dict(cap=10.0, slopes=True, buckets=32, far=128)
+    check([1, 2, 0, 3], [900, 70, 30, 1], 4, 2, 64, seed=parts, first=[3, 70, 0, 1], **form)
+    check([1, 4], [1500, 90], 2, 1, 128, window=200, first=[130, 0], seed=parts)
+    check([2], [515], 8, 1, 80, causal=False, buckets=16, far=100, seed=parts)
