@@ -377,6 +377,7 @@ struct Form {
     float unit, slope = 0.f;
     float c0, c1, c2, c3, small, into;       // the tanh's polynomial of a product, the largest product that it is for, and scale / cap
     int border = kFar;                       // lane l: where bucket l + 1 begins
+    int single = 0;                          // the first buckets that are one distance each
     float past = 0.f, ahead = 0.f;           // lane l: the bias of bucket l, and where the key lies behind
     __device__ __forceinline__ Form(const AttnArgs &A, int head)
     {
@@ -401,6 +402,7 @@ struct Form {
             const int columns = two_sided ? 2 * F.buckets : F.buckets;
             const _Float16 *table = F.table + (int64_t)head * columns;
             border = tabled && lane < F.buckets - 1 ? min(max(F.borders[lane], 0), kFar) : kFar;
+            single = __builtin_ctzll(~__ballot(border == lane + 1));
             past = tabled && lane < F.buckets ? (float)table[lane] * of_bias : 0.f;
             ahead = tabled && two_sided && lane < F.buckets ? (float)table[F.buckets + lane] * of_bias : 0.f;
         }
@@ -477,8 +479,8 @@ struct Form {
             const int e = part * 64 + lane, d = base + SIGN * (e - 31), n = away(d);
             float bias = kSloped ? -slope * fabsf((float)d) : 0.f;
             if (tabled) {
-                int at = b0;
-                for (int i = b0; i < b1; ++i) at += n >= __builtin_amdgcn_readlane(border, i);
+                int at = max(b0, min(n, single));
+                for (int i = max(b0, single); i < b1; ++i) at += n >= __builtin_amdgcn_readlane(border, i);
                 const int before = __builtin_amdgcn_ds_bpermute(4 * at, __builtin_bit_cast(int, past)), behind = __builtin_amdgcn_ds_bpermute(4 * at, __builtin_bit_cast(int, ahead));
                 bias += __builtin_bit_cast(float, two_sided && d < 0 ? behind : before);
                 if (part == 0) b.diagonal = two_sided && d < 0 ? kMaxBuckets + at : at;
@@ -580,8 +582,10 @@ struct BucketSums {
                 flush();
                 column = b.column;
             }
+            float some[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) run += ds[i];
+            for (int i = 0; i < 16; ++i) some[i & 3] += ds[i];
+            run += (some[0] + some[1]) + (some[2] + some[3]);
             return;
         }
         const int half = lane >> 5, col = min(lane, kSkewed - 1);
@@ -592,11 +596,11 @@ struct BucketSums {
 #pragma unroll
             for (int i = 0; i < 8; ++i) to[(8 * (i >> 2) + (i & 3)) * (kSkewed + 1)] = ds[8 * part + i];
             __builtin_amdgcn_wave_barrier();
-            float sum = 0.f;
+            float some[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int row = 0; row < 16; ++row) sum += room[row * kSkewed + col];
+            for (int row = 0; row < 16; ++row) some[row & 3] += room[row * kSkewed + col];
             __builtin_amdgcn_wave_barrier();
-            diagonal[part] = lane < kSkewed ? sum : 0.f;
+            diagonal[part] = lane < kSkewed ? (some[0] + some[1]) + (some[2] + some[3]) : 0.f;
         }
         const float second = of_lane(diagonal[1], lane - 16);
         const float sums = scan_of_column(diagonal[0] + (lane >= 16 ? second : 0.f), b.diagonal);     // lane: row - column + 31
