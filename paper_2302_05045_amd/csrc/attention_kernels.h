@@ -520,6 +520,12 @@ struct Form {
     }
 };
 constexpr int kBiasRoom = 96;                // floats of a wave's biases
+
+// Waves to a SIMD that the registers of the forms' kernels leave room for, forward and dQ.  Heads of 33 to 64: three without a spilled register; dQ of
+// 32 buckets, 8 x 1024 in both directions, 12 heads of 64, 84 us with two and 68 with three (768 workgroups are one round then); four would spill in the forward
+// pass (4093 tokens in 7, 16 heads, both passes 109 us with three there, 113 with four).
+enum { kForward, kDq, kDkv };
+constexpr int waves_of(int ks, int form) { return form == kPlain || form == kAll || ks > 4 ? 2 : ks == 2 && form != kTable ? 4 : 3; }
 struct NoForm {};
 template <int FORM>
 __device__ __forceinline__ auto form_of(const AttnArgs &A, int head)
@@ -639,7 +645,7 @@ struct BucketSums {
 // 920 TFLOP/s, bound by the chip's power (zeros: 1230); two sequences of 4096, not causal, 935; 4 x 2048 causal, 32 heads of 80:
 // 140 to 153 us by card, 600 (80 is padded to 96 in the second product; 17 tiles a workgroup pay for its start and for what lies behind the diagonal in two).
 template <int KS, int FORM>
-__global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(const AttnArgs A)
+__global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_kernel(const AttnArgs A)
 {
     constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
@@ -927,7 +933,7 @@ __global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnA
 
 // dQ, and delta on the way: three products a tile.  8192 causal tokens, 32 heads of 128 on 8: 825 us, 1000 TFLOP/s; 4 x 2048, 32 heads of 80: 180 us.
 template <int KS, int FORM>
-__global__ void __launch_bounds__(kAttnThreads, 2) attention_dq_kernel(const AttnArgs A)
+__global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_dq_kernel(const AttnArgs A)
 {
     constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
@@ -1259,8 +1265,6 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
     if (SIDES == 1 || side) store_own<DB>(A.dv + seq.k0 * A.dv_row + kv * A.dv_head, A.dv_row, key, seq.k_len, A.dim, dv, 1.f);
     if (SIDES == 1 || !side) store_own<DB>(A.dk + seq.k0 * A.dk_row + kv * A.dk_head, A.dk_row, key, seq.k_len, A.dim, dk, A.scale);
 }
-
-enum { kForward, kDq, kDkv };
 
 // The workgroups of dK and dV from which a wave has its keys for itself; below, where the longest workgroup is what the call waits for, two share them.
 // Whole backward pass of heads of 64, one wave / two, us: 32 workgroups, 512 tokens of 8 heads 31 / 29; 256, 2048 of 16 heads 76 / 75; 512,
