@@ -17,7 +17,8 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
     const Sequence seq = sequence_of(A, at.b);
     const int pack = WHICH == kForward ? A.pack : 1;
     const int count = WHICH == kDkv ? seq.k_len : seq.q_len * pack, row = (WHICH == kDkv ? A.tiles - 1 - at.tile : at.tile) * kOwnRows + rows * kWaveRows + (lane & 31);
-    if (row >= count) return;
+    // Of few rows the parts are asked for before it is known which rows there are (their memory is there for all of them): one wait less in a chain of three.
+    if (WHICH == kForward && A.few ? rows > 0 : row >= count) return;
     f32x16 acc[1];
     clear(acc);
     float top = -INFINITY, sum = 0.f;
@@ -53,6 +54,7 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
             for (int e = 0; e < 16; ++e) acc[0][e] = counts ? fmaf(x[i][e >> 2][e & 3], weight, acc[0][e]) : acc[0][e];
         }
     }
+    if (row >= count) return;
     const int query = pack > 1 ? row / pack : row, head = pack > 1 ? at.head * pack + row - query * pack : at.head;
     _Float16 *to;
     int64_t stride;
