@@ -501,6 +501,8 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * Sums of dz are fp32 within 32 queries of a part, double over those; their order is fixed.  The slopes are constants and have no gradient.
  * The tanh is within 2^-20 of itself in blocks of 32 queries and 32 keys whose |x| are all up to half the cap (scale / cap between 2^-17 and 2^17), within
  * 2^-22 elsewhere.  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
+ * A call of at most 128 rows a sequence, max_q times the heads that share keys, holds them in one tile, and of at most 32 rows its workgroups' waves share the
+ * keys: blocks of queries and keys (where what is not finite reaches) are those rows and 64 keys then.  heads < 2^21 with d_dtable.
  * Everything else, alignment and limits, is as for samo_attention; slopes, borders and first_keys 4-byte, table and dtable 2-byte aligned.
  * samo_attention_scored_workspace_bytes: what the backward call needs (delta, and for d_dtable the parts of its sums) on the current device. */
 #define SAMO_ATTENTION_MAX_BUCKETS 64
@@ -546,7 +548,8 @@ samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, cons
  * stream s and the next block's norm in one kernel, and its backward pass.  Row by row, with N(x) = (x - m) / sqrt(mean((x - m)^2) + eps), m = mean(x)
  * (SAMO_NORM_LAYER) or 0 (SAMO_NORM_RMS),
  *   n = N(y) y_weight + y_bias (y_norm != 0) or y,   s' = s + scale gate n,   out = N(s') weight + bias
- * d_y NULL: there is no block before, s' = s and nothing is written to d_new_stream (y_norm, scale, the gate and y's vectors are not looked at).
+ * d_y NULL: there is no block before, s' = s and nothing is written to d_new_stream (y_norm, scale, the gate and y's vectors are not looked at; nor are y's
+ * vectors with y_norm == 0).
  * tokens x hidden row-major: d_stream and d_new_stream fp32 (stream_fp32 != 0) or fp16, d_y and d_out fp16; the vectors fp16[hidden], each may be
  * NULL (1 for a weight or the gate, 0 for a bias).  d_stats: float[4 tokens], 16-byte aligned as everything here, for the backward pass, or NULL.
  * Backward, from dout and dnew (of the stream's type; the gradient that reaches s' from further on; NULL: none) with what the forward pass left in

@@ -1332,6 +1332,7 @@ samo_status check_scores(const samo_attention_scores *s, bool backward, AttnArgs
     if (s->d_table) {
         if (s->buckets < 1 || s->buckets > SAMO_ATTENTION_MAX_BUCKETS) return SAMO_ERR_SIZE;
         if (s->buckets > 1 && !s->d_borders) return SAMO_ERR_NULL;
+        if (backward && s->d_dtable && a->heads >= 1 << 21) return SAMO_ERR_SIZE;      // a workgroup of 1024 threads a head
     } else if (backward && s->d_dtable) return SAMO_ERR_NULL;
     if (s->d_first_keys && !a->causal) return SAMO_ERR_ARG;
     a->scored = 1;

@@ -462,3 +462,59 @@ def test_few_queries_in_parts(parts):
     check([1, 2, 0, 3], [900, 70, 30, 1], 4, 2, 64, seed=parts, first=[3, 70, 0, 1], **form)
     check([1, 4], [1500, 90], 2, 1, 128, window=200, first=[130, 0], seed=parts)
     check([2], [515], 8, 1, 80, causal=False, buckets=16, far=100, seed=parts)
+
+
+def test_no_queries_and_no_keys():
+    """No query at all: the table's gradient is zero; no key: out is zero, the gradients of nothing are not written."""
+    table, borders = torch.randn(2, 8, device=DEV).half(), samo.samo_bucket_borders(8, 20)
+    scores = samo.Scores(cap=5.0, table=table, borders=borders)
+    for nq, nk in ((0, 5), (5, 0), (0, 0)):
+        t = lambda n: torch.randn(n, 2, 64, device=DEV).half()
+        q, k, v, do = t(nq), t(nk), t(nk), t(nq)
+        out, lse, dtable = torch.full_like(q, 7.0), torch.zeros(2, nq, device=DEV), torch.full_like(table, float("nan"))
+        dq, dk, dv = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+        samo.samo_attention(q, k, v, out, lse, causal=False, scores=scores._replace(table=torch.cat([table, table], 1), two_sided=True))
+        samo.samo_attention(q, k, v, out, lse, scores=scores)
+        samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv, scores=scores, dtable=dtable)
+        assert torch.all(dtable == 0) and torch.all(out == 0) and torch.all(dq == 0) and torch.all(dk == 0) and torch.all(dv == 0)
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Calls with workspaces from the allocator, each on its own stream: the bits of each by itself."""
+    make = lambda n: [torch.randn(n, 2, 64, device=DEV).half() for _ in range(4)]
+    table, borders = torch.randn(2, 32, device=DEV).half(), samo.samo_bucket_borders(32, 128)
+    scores = samo.Scores(table=table, borders=borders)
+
+    def call(q, k, v, do):
+        out, lse, grads, dtable = torch.zeros_like(q), torch.zeros(2, q.shape[0], device=DEV), [torch.zeros_like(q) for _ in range(3)], torch.zeros_like(table)
+        samo.samo_attention(q, k, v, out, lse, scores=scores)
+        samo.samo_attention_backward(do, q, k, v, out, lse, *grads, scores=scores, dtable=dtable)
+        return [out, lse, *grads, dtable]
+
+    data = [make(1500), make(1100)]
+    want = [call(*d) for d in data]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in data]
+    got = []
+    for s, d in zip(streams, data):
+        with torch.cuda.stream(s):
+            got.append(call(*d))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for w, g in zip(want, got) for a, b in zip(w, g))
+
+
+def test_rows_past_two_gibibytes():
+    """Keys and values whose rows lie so far apart that the last ones begin past 2^31 bytes, read by a token and by many."""
+    n, dim, apart = 700, 64, 1 << 21
+    room = torch.zeros((n, apart), dtype=torch.float16, device=DEV)
+    k, v = room[:, :dim].unsqueeze(1), room[:, 64:64 + dim].unsqueeze(1)
+    kk, vv = (torch.randn(n, 1, dim, device=DEV).half() for _ in range(2))
+    k.copy_(kk)
+    v.copy_(vv)
+    for form in (dict(cap=20.0), dict(slopes=torch.rand(4, device=DEV)), dict(first_keys=torch.tensor([3], dtype=torch.int32, device=DEV))):
+        for queries in (1, 200):
+            q = torch.randn(queries, 4, dim, device=DEV).half()
+            a, b, lse = torch.zeros_like(q), torch.zeros_like(q), torch.zeros(4, queries, device=DEV)
+            samo.samo_attention(q, k, v, a, lse, scores=samo.Scores(**form))
+            samo.samo_attention(q, kk, vv, b, lse, scores=samo.Scores(**form))
+            assert torch.equal(a, b)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2302_05045_amd as samo
+import test_operators_cpu
 from test_operators_cpu import ALIGN, ARG, FAKE, NULL, OK, SIZE, WORKSPACE, attention
 
 
@@ -79,3 +80,17 @@ def test_bucket_borders():
     for buckets, far in ((0, 10), (65, 100), (8, 4), (8, 3), (8, 2 ** 30)):
         with pytest.raises(ValueError):
             cpu(buckets, far)
+
+
+@pytest.mark.parametrize("form", ["keys", "cap", "slope", "table", "all"])
+def test_m0_is_touched_only_by_the_copies_into_lds_in_the_forms_kernels(tmp_path, form):
+    test_operators_cpu.test_m0_is_touched_only_by_the_copies_into_lds(tmp_path, "attention_%s.hip" % form)
+
+
+def test_a_table_of_too_many_heads_is_refused():
+    """Its gradient takes a workgroup of 1024 threads a head; a launch's threads are counted in 32 bits."""
+    L, need = samo.lib(), ctypes.c_size_t()
+    for heads, want in ((2 ** 21, SIZE), (2 ** 21 - 8, OK)):
+        d = attention(heads=heads, kv_heads=heads)
+        assert L.samo_attention_scored_workspace_bytes(ctypes.byref(d), ctypes.byref(scores(d_dtable=FAKE)), ctypes.byref(need)) == want, heads
+    assert L.samo_attention_scored_workspace_bytes(ctypes.byref(attention(heads=2 ** 21, kv_heads=2 ** 21)), ctypes.byref(scores()), ctypes.byref(need)) == OK
