@@ -11,7 +11,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsamo.so")
-SOURCES = ["api.hip", "attention.hip", "attention_all.hip", "attention_cap.hip", "attention_keys.hip", "attention_slope.hip", "attention_table.hip", "glu.hip", "index.hip", "norm.hip", "pipeline.hip", "step8.hip", "wgrad.hip"]
+SOURCES = ["api.hip", "attention.hip", "attention_all.hip", "attention_cap.hip", "attention_cap_slope.hip",
+           "attention_cap_table.hip", "attention_keys.hip", "attention_slope.hip", "attention_table.hip", "glu.hip", "index.hip", "norm.hip", "pipeline.hip", "step8.hip", "wgrad.hip"]
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
     "-Wall", "-Wextra", "-Wno-unused-parameter",

@@ -176,10 +176,11 @@ int splits_of(int which, const AttnArgs &a)
 hipError_t launch_kernel(int which, const AttnArgs &a, int64_t items, hipStream_t s)
 {
     if (!a.scored) return launch_form<kPlain>(which, a, items, s);
-    const int parts = (a.form.cap > 0.f) + (a.form.slopes != nullptr) + (a.form.table != nullptr);
-    if (parts == 0) return launch_attention_keys(which, a, items, s);
-    if (parts > 1) return launch_attention_all(which, a, items, s);
-    return a.form.slopes ? launch_attention_slope(which, a, items, s) : a.form.table ? launch_attention_table(which, a, items, s) : launch_attention_cap(which, a, items, s);
+    const bool cap = a.form.cap > 0.f, slopes = a.form.slopes != nullptr, table = a.form.table != nullptr;
+    if (slopes && table) return launch_attention_all(which, a, items, s);
+    if (slopes) return cap ? launch_attention_cap_slope(which, a, items, s) : launch_attention_slope(which, a, items, s);
+    if (table) return cap ? launch_attention_cap_table(which, a, items, s) : launch_attention_table(which, a, items, s);
+    return cap ? launch_attention_cap(which, a, items, s) : launch_attention_keys(which, a, items, s);
 }
 
 template <int DB>
@@ -239,7 +240,7 @@ hipError_t launch_attention(const AttnArgs &a, size_t bytes, hipStream_t s) { re
 
 void attention_pack(AttnArgs &a)
 {
-    const bool one_head = !a.scored || a.form.table || (a.form.cap > 0.f && a.form.slopes);     // a table's columns lie in a wave's lanes; several forms share its kernels
+    const bool one_head = !a.scored || a.form.table;         // a table's columns lie in a wave's lanes, of one head
     a.pack = one_head || (int64_t)a.max_q * a.group > kOwnRows ? 1 : a.group;
     a.few = a.scored && most_rows(kForward, a) <= kWaveRows;
 }

@@ -1,4 +1,4 @@
-// The kernels of attention with scores of several forms at once.
+// The kernels of attention with scores that fall with the distance and have a learned bias by its bucket, capped or not.
 #include "attention_kernels.h"
 
 namespace samo {

@@ -362,7 +362,13 @@ struct KeyTiles {
 // The table's columns and borders live in the wave's lanes: the bucket of a distance that the lanes agree on is the number of set bits of a comparison.
 constexpr int kMaxBuckets = SAMO_ATTENTION_MAX_BUCKETS;
 enum { kSame, kLinear, kAcross, kLaid };
-enum { kPlain, kKeys, kCap, kSlope, kTable, kAll };        // which parts there can be: none (kKeys: but the first keys), one, any; kernels of their own
+// Which parts there are, kernels of their own: none (kKeys: but the first keys), one, two; kAll: slopes and a table, with a cap or without.  With one kernel
+// for all of them, both passes, us: 8192 tokens in 4, 32 heads of 128 on 8, slopes 1040 and 770, cap and slopes 1313 and CAPSLOPE_US.
+enum { kPlain, kKeys, kCap, kSlope, kTable, kCapSlope, kCapTable, kAll };
+constexpr bool has_cap(int form) { return form == kCap || form >= kCapSlope; }
+constexpr bool has_slope(int form) { return form == kSlope || form == kCapSlope || form == kAll; }
+constexpr bool has_table(int form) { return form == kTable || form >= kCapTable; }
+constexpr bool packs(int form) { return form != kPlain && !has_table(form); }
 struct Bias {
     int kind, column;                        // column: of all the block's pairs, the second half behind kMaxBuckets; -1 where they differ
     int sign;                                // kAcross: of the distance from row to row
@@ -371,9 +377,8 @@ struct Bias {
 };
 template <int FORM>
 struct Form {
-    static constexpr bool kCapped = FORM == kCap || FORM == kAll, kSloped = FORM == kSlope || FORM == kAll, kTabled = FORM == kTable || FORM == kAll,
-                          kBiased = kSloped || kTabled;
-    bool capped = kCapped, tabled = kTabled, two_sided = false;
+    static constexpr bool kCapped = has_cap(FORM), kSloped = has_slope(FORM), kTabled = has_table(FORM), kBiased = kSloped || kTabled, tabled = kTabled;
+    bool capped = kCapped, two_sided = false;
     float unit, slope = 0.f;
     float c0, c1, c2, c3, small, into;       // the tanh's polynomial of a product, the largest product that it is for, and scale / cap
     int border = kFar;                       // lane l: where bucket l + 1 begins
@@ -395,16 +400,15 @@ struct Form {
             small = into > 0x1p-17f && into < 0x1p17f ? kSmall / into : 0.f;       // where into^7 and what it is multiplied with are numbers
         }
         const float of_bias = capped ? 1.f / F.cap : 1.f / A.scale;
-        if constexpr (kSloped) slope = F.slopes ? F.slopes[head] * of_bias : 0.f;
+        if constexpr (kSloped) slope = F.slopes[head] * of_bias;
         if constexpr (kTabled) {
-            tabled = F.table != nullptr;
             two_sided = F.two_sided != 0;
             const int columns = two_sided ? 2 * F.buckets : F.buckets;
             const _Float16 *table = F.table + (int64_t)head * columns;
-            border = tabled && lane < F.buckets - 1 ? min(max(F.borders[lane], 0), kFar) : kFar;
+            border = lane < F.buckets - 1 ? min(max(F.borders[lane], 0), kFar) : kFar;
             single = __builtin_ctzll(~__ballot(border == lane + 1));
-            past = tabled && lane < F.buckets ? (float)table[lane] * of_bias : 0.f;
-            ahead = tabled && two_sided && lane < F.buckets ? (float)table[F.buckets + lane] * of_bias : 0.f;
+            past = lane < F.buckets ? (float)table[lane] * of_bias : 0.f;
+            ahead = two_sided && lane < F.buckets ? (float)table[F.buckets + lane] * of_bias : 0.f;
         }
     }
     static constexpr int kFar = 1 << 30;     // behind every distance
@@ -456,7 +460,7 @@ struct Form {
             b1 = bucket(two_sided ? max(-lo, hi) : max(hi, 0));
             if (one_side && b0 == b1) {
                 b.column = behind ? kMaxBuckets + b0 : b0;
-                if (!kSloped || slope == 0.f) {
+                if (!kSloped) {
                     b.same = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, behind ? ahead : past), b0));
                     return;
                 }
@@ -510,12 +514,20 @@ struct Form {
     __device__ __forceinline__ bool starts(const Bias &b) const { return kBiased && b.kind != kSame && !capped; }
     __device__ __forceinline__ f32x16 with_bias(f32x16 s, const Bias &b, const float *room, int block) const
     {
-        if constexpr (kBiased)
-            if (capped && b.kind != kSame) {
-                const f32x16 x = biases(b, room, block);
+        if constexpr (kBiased) {
+            if (!capped || b.kind == kSame) return s;
+            if (kSloped && b.kind == kLinear) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] += x[i];
+                for (int i = 0; i < 16; ++i) s[i] += fmaf(b.step, (float)(32 * block + 8 * (i >> 2) + (i & 3)), b.base);
+            } else if (kSloped && b.kind == kAcross) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = fmaf(b.step, fabsf(b.base + b.sign * (float)(32 * block + 8 * (i >> 2) + (i & 3))), s[i]);
+            } else if constexpr (kTabled) {
+                const float *at = room + 31 + 32 * block - (int)(threadIdx.x & 31);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] += at[acc_row(i)];
             }
+        }
         return s;
     }
 };
@@ -525,7 +537,7 @@ constexpr int kBiasRoom = 96;                // floats of a wave's biases
 // 32 buckets, 8 x 1024 in both directions, 12 heads of 64, 84 us with two and 68 with three (768 workgroups are one round then); four would spill in the forward
 // pass (4093 tokens in 7, 16 heads, both passes 109 us with three there, 113 with four).
 enum { kForward, kDq, kDkv };
-constexpr int waves_of(int ks, int form) { return form == kPlain || form == kAll || ks > 4 ? 2 : ks == 2 && form != kTable ? 4 : 3; }
+constexpr int waves_of(int ks, int form) { return form == kPlain || form == kAll || ks > 4 ? 2 : ks == 2 && !has_table(form) ? 4 : 3; }
 struct NoForm {};
 template <int FORM>
 __device__ __forceinline__ auto form_of(const AttnArgs &A, int head)
@@ -647,13 +659,13 @@ struct BucketSums {
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
+    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
     __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
     // Few queries of heads that share keys: a tile's rows are pack heads of each query, so that a tile of keys is read and multiplied once for all of them
     // (one token of 5 sequences behind 4000, 32 heads of 128 on 8: 30 us head by head, PACKED_US packed).
-    constexpr bool kPacks = FORM == kKeys || FORM == kCap || FORM == kSlope;
+    constexpr bool kPacks = packs(FORM);
     const int pack = kPacks ? A.pack : 1;
     Place at;
     if (!pick(A, pack > 1 ? A.kv_heads : A.heads, at)) return;
@@ -786,8 +798,8 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_ke
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnArgs A)
 {
-    constexpr bool kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
-    constexpr bool kPacks = FORM == kKeys || FORM == kCap || FORM == kSlope;
+    constexpr bool kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
+    constexpr bool kPacks = packs(FORM);
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS), kWaves = kAttnThreads / 64;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[kWaves][2 * kTile];            // a wave's K, V
     __shared__ float biases[kTabled ? kWaves : 1][kBiasRoom];
@@ -935,7 +947,7 @@ __global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnA
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_dq_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
+    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];
     __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
@@ -1077,7 +1089,7 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 template <int KS, int SIDES, int FORM>
 __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kBiased = FORM >= kSlope, kCapped = FORM == kCap || FORM == kAll, kTabled = FORM == kTable || FORM == kAll;
+    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
     constexpr bool kWide = KS > 6;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide ? kOwnRows * PITCH : 0)];       // Q, dO; two tiles each; V

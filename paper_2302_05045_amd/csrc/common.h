@@ -287,6 +287,8 @@ hipError_t launch_attention_keys(int which, const AttnArgs &a, int64_t items, hi
 hipError_t launch_attention_cap(int which, const AttnArgs &a, int64_t items, hipStream_t s);
 hipError_t launch_attention_slope(int which, const AttnArgs &a, int64_t items, hipStream_t s);
 hipError_t launch_attention_table(int which, const AttnArgs &a, int64_t items, hipStream_t s);
+hipError_t launch_attention_cap_slope(int which, const AttnArgs &a, int64_t items, hipStream_t s);
+hipError_t launch_attention_cap_table(int which, const AttnArgs &a, int64_t items, hipStream_t s);
 hipError_t launch_attention_all(int which, const AttnArgs &a, int64_t items, hipStream_t s);
 
 // The gated feed-forward block (glu.hip).

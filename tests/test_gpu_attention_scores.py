@@ -135,8 +135,9 @@ def check(lens_q, lens_k, heads, kv_heads, dim, causal=True, window=0, cap=0.0, 
 
 
 FORMS = [dict(cap=5.0), dict(cap=50.0), dict(slopes=True), dict(buckets=32, far=128), dict(buckets=8, far=20, two_sided=True), dict(first=True),
-         dict(cap=20.0, slopes=True, buckets=16, far=60, first=True)]
-NAMES = ["cap 5", "cap 50", "slopes", "buckets", "both sides", "first keys", "all"]
+         dict(cap=20.0, slopes=True, buckets=16, far=60, first=True), dict(cap=10.0, slopes=True), dict(cap=10.0, buckets=32, far=100),
+         dict(slopes=True, buckets=32, far=128)]
+NAMES = ["cap 5", "cap 50", "slopes", "buckets", "both sides", "first keys", "all", "cap and slopes", "cap and buckets", "slopes and buckets"]
 
 
 def with_first(form, lens):
@@ -425,7 +426,8 @@ def test_borders_of_the_logarithm():
         assert torch.equal((n[:, None] >= borders).sum(1), want), (buckets, far)
 
 
-@pytest.mark.parametrize("form", [dict(cap=20.0), dict(slopes=True), dict(first=True), dict(slopes=True, first=True)], ids=["cap", "slopes", "first keys", "slopes and first keys"])
+@pytest.mark.parametrize("form", [dict(cap=20.0), dict(slopes=True), dict(first=True), dict(cap=10.0, slopes=True, first=True)],
+                         ids=["cap", "slopes", "first keys", "cap, slopes and first keys"])
 @pytest.mark.parametrize("heads,kv,queries", [(8, 2, 1), (32, 8, 1), (7, 1, 3), (12, 4, 20), (6, 2, 42), (6, 2, 43), (128, 1, 1), (64, 1, 2), (100, 1, 1)])
 def test_heads_that_share_a_tile_with_their_queries(heads, kv, queries, form):
     """A tile's rows are all heads of a query where a sequence's are at most 128: with one query, several, as many as fit and one more."""

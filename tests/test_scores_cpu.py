@@ -82,7 +82,7 @@ def test_bucket_borders():
             cpu(buckets, far)
 
 
-@pytest.mark.parametrize("form", ["keys", "cap", "slope", "table", "all"])
+@pytest.mark.parametrize("form", ["keys", "cap", "slope", "table", "cap_slope", "cap_table", "all"])
 def test_m0_is_touched_only_by_the_copies_into_lds_in_the_forms_kernels(tmp_path, form):
     test_operators_cpu.test_m0_is_touched_only_by_the_copies_into_lds(tmp_path, "attention_%s.hip" % form)
 
