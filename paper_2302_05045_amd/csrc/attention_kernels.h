@@ -363,7 +363,7 @@ struct KeyTiles {
 constexpr int kMaxBuckets = SAMO_ATTENTION_MAX_BUCKETS;
 enum { kSame, kLinear, kAcross, kLaid };
 // Which parts there are, kernels of their own: none (kKeys: but the first keys), one, two; kAll: slopes and a table, with a cap or without.  With one kernel
-// for all of them, both passes, us: 8192 tokens in 4, 32 heads of 128 on 8, slopes 1040 and 770, cap and slopes 1313 and CAPSLOPE_US.
+// for the last three, both passes, us: 8192 tokens in 4, 32 heads of 128 on 8, cap and slopes 1313 and 1114; 16 heads of 64, cap and 32 buckets 385 and 331.
 enum { kPlain, kKeys, kCap, kSlope, kTable, kCapSlope, kCapTable, kAll };
 constexpr bool has_cap(int form) { return form == kCap || form >= kCapSlope; }
 constexpr bool has_slope(int form) { return form == kSlope || form == kCapSlope || form == kAll; }
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_ke
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
     __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
     // Few queries of heads that share keys: a tile's rows are pack heads of each query, so that a tile of keys is read and multiplied once for all of them
-    // (one token of 5 sequences behind 4000, 32 heads of 128 on 8: 30 us head by head, PACKED_US packed).
+    // (one token of 5 sequences behind 4001, 32 heads of 128 on 8: 30 us head by head, 20 so, 15 by attention_few_kernel).
     constexpr bool kPacks = packs(FORM);
     const int pack = kPacks ? A.pack : 1;
     Place at;
@@ -1086,13 +1086,15 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 // Four products a tile: 1220 us for those 8192 tokens, 900 TFLOP/s; 4 x 2048, 32 heads of 80 (one wave to its keys): 240 us.
 // Two waves to a SIMD have 256 registers each.  Heads of more than 96 fill half of them with their sums: there the rows of V stay in LDS, from where
 // they are read for every block.
+// So do the rows of K where the scores are of another form, which takes registers of its own: 8192 tokens in 4, 32 heads of 128 on 8, both passes, us, with K in
+// registers / in LDS: slopes 753 / 734, capped 860 / 827, 32 buckets 909 / 799, capped with slopes 1114 (in part spilled) / 828.
 template <int KS, int SIDES, int FORM>
 __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {
     constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
-    constexpr bool kWide = KS > 6;
+    constexpr bool kWide = KS > 6, kLean = kWide && FORM != kPlain;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide ? kOwnRows * PITCH : 0)];       // Q, dO; two tiles each; V
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide + kLean) * kOwnRows * PITCH];       // Q, dO; two tiles each; V, K
     __shared__ __attribute__((aligned(16))) float stats[2][2][kTileRows];         // lse, delta
     __shared__ float biases[kTabled ? SIDES * kAttnThreads / 64 : 1][kBiasRoom];
     Place at;
@@ -1144,12 +1146,15 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
         if (SIDES == 1) bring_one(second_operand, 1, shared, t, buffer);
     };
     if (kWide)
-        for (int part = side; part < 2; part += SIDES) Tiles<KS>(V).bring(k_first + part * kTileRows, lds_at + 4 * kTile + part * kTileRows * PITCH);
+        for (int part = side; part < 2; part += SIDES) {
+            Tiles<KS>(V).bring(k_first + part * kTileRows, lds_at + 4 * kTile + part * kTileRows * PITCH);
+            if (kLean) Tiles<KS>(K).bring(k_first + part * kTileRows, lds_at + 4 * kTile + (kOwnRows + part * kTileRows) * PITCH);
+        }
     if (count > 0) bring(shared, t, 0);
-    half8 own[KS], ownv[kWide ? 1 : KS];
-    load_own<KS>(K, w_first, own);
+    half8 own[kLean ? 1 : KS], ownv[kWide ? 1 : KS];
+    if constexpr (!kLean) load_own<KS>(K, w_first, own);
     if constexpr (!kWide) load_own<KS>(V, w_first, ownv);
-    const unsigned char *v_rows = lds + 4 * kTile + (wave & 3) * kWaveRows * PITCH;
+    const unsigned char *v_rows = lds + 4 * kTile + (wave & 3) * kWaveRows * PITCH, *k_rows = v_rows + kOwnRows * PITCH;
     const Span seen(M.first_query(key), M.end_query(key));
     f32x16 dk[DB], dv[DB];
     clear(dk);
@@ -1187,7 +1192,8 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
             }
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), own[ks], s[0], 0, 0, 0);
+                const half8 k = kLean ? read_rows<PITCH>(k_rows, 0, ks) : own[kLean ? 0 : ks];
+                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(qt, qb, ks), k, s[0], 0, 0, 0);
                 const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
                 dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
             }
