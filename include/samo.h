@@ -501,7 +501,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * Sums of dz are fp32 within 32 queries of a part, double over those; their order is fixed.  The slopes are constants and have no gradient.
  * The tanh is within 2^-20 of itself in blocks of 32 queries and 32 keys whose |x| are all up to half the cap (scale / cap between 2^-17 and 2^17), within
  * 2^-22 elsewhere.  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
- * A call of at most 128 rows a sequence, max_q times the heads that share keys, holds them in one tile, and of at most 32 rows its workgroups' waves share the
+ * A call of at most 128 rows a sequence, max_q times the heads that share keys, holds them in one tile, and of at most 32 rows and more than 128 keys its waves share the
  * keys: blocks of queries and keys (where what is not finite reaches) are those rows and 64 keys then.  heads < 2^21 with d_dtable.
  * Everything else, alignment and limits, is as for samo_attention; slopes, borders and first_keys 4-byte, table and dtable 2-byte aligned.
  * samo_attention_scored_workspace_bytes: what the backward call needs (delta, and for d_dtable the parts of its sums) on the current device. */

@@ -242,7 +242,8 @@ void attention_pack(AttnArgs &a)
 {
     const bool one_head = !a.scored || a.form.table;         // a table's columns lie in a wave's lanes, of one head
     a.pack = one_head || (int64_t)a.max_q * a.group > kOwnRows ? 1 : a.group;
-    a.few = a.scored && most_rows(kForward, a) <= kWaveRows;
+    // Up to two tiles of keys are one chain either way, and the waves' sums need no joining: 61 tokens in 9 sequences, 16 heads of 64, 6.7 us, with few 7.5.
+    a.few = a.scored && most_rows(kForward, a) <= kWaveRows && a.max_k > 2 * kTileRows;
 }
 
 int64_t attention_table_bytes(const AttnArgs &a)

@@ -267,7 +267,7 @@ struct AttnArgs {
     float *parts;                           // NULL: a launch is not split
     f32x2 *part_stats;
     int pack;                               // forward: heads of a query that a tile's rows hold, 1 or group
-    int few;                                // forward: a sequence's rows are at most 32, and scored
+    int few;                                // forward, scored: a sequence's rows are at most 32, behind more than two tiles of keys
     int scored;                             // whether form is looked at
     AttnForm form;
 };
