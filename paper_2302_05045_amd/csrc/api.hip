@@ -2,6 +2,7 @@
 // Every entry point validates on the host first and enqueues only if all
 // arguments are acceptable, so the error paths can be exercised without a GPU.
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -1320,11 +1321,13 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
 // ---------------------------------------------------------------- attention with scores of another form
 namespace {
 
+constexpr float kLeastScale = 0x1p-60f, kMostScale = 0x1p60f;     // biases are held in units of it
 constexpr float kLeastCap = 1.f / 1024.f, kMostCap = 256.f;       // the tanh is within 2^-22, so that a score is within 2^-14
 
 samo_status check_scores(const samo_attention_scores *s, bool backward, AttnArgs *a)
 {
     if (!s) return SAMO_ERR_NULL;
+    if (a->scale < kLeastScale || a->scale > kMostScale) return SAMO_ERR_ARG;
     if (s->cap != 0.f && !(s->cap >= kLeastCap && s->cap <= kMostCap)) return SAMO_ERR_ARG;
     if ((reinterpret_cast<uintptr_t>(s->d_slopes) | reinterpret_cast<uintptr_t>(s->d_borders) | reinterpret_cast<uintptr_t>(s->d_first_keys)) & 3u)
         return SAMO_ERR_ALIGN;
@@ -1506,7 +1509,7 @@ samo_status check_norm(const samo_norm_desc *d, bool backward, NormArgs *a)
     if (!d) return SAMO_ERR_NULL;
     if (d->tokens < 0 || d->tokens > INT32_MAX || d->hidden < 8 || d->hidden > kMaxHidden || d->hidden % 8) return SAMO_ERR_SIZE;
     if (d->kind != SAMO_NORM_RMS && d->kind != SAMO_NORM_LAYER) return SAMO_ERR_ARG;
-    if (!(std::isfinite(d->eps) && d->eps > 0.f) || (d->d_y && !std::isfinite(d->scale))) return SAMO_ERR_ARG;
+    if (!(std::isfinite(d->eps) && d->eps >= FLT_MIN) || (d->d_y && !std::isfinite(d->scale))) return SAMO_ERR_ARG;
     const void *vectors[] = {d->d_weight, d->d_bias, d->d_y_weight, d->d_y_bias, d->d_gate, d->d_y, d->d_stats, d->d_stream, d->d_new_stream, d->d_out};
     for (const void *p : vectors)
         if (misaligned(p)) return SAMO_ERR_ALIGN;

@@ -354,7 +354,7 @@ struct KeyTiles {
 // Scores of another form (SCORED): z = cap tanh(x / cap) + bias(d), x the scaled product.  All of it in units of `unit` and log 2: a product, or its tanh,
 // and a bias are added and enter the exponent by the same multiplication as a plain product.  Without a cap the bias is what the matrix instructions
 // start from, so that it costs the making of its 16 registers; with one it is added behind the tanh.  Biases of a block of queries and keys, whose
-// distances are those of its diagonals, come in three kinds:
+// distances are those of its diagonals, come in four kinds:
 //   kSame    one number, where all distances have one bucket: nothing to do for an element (most blocks of long sequences)
 //   kLinear  a slope, the block on one side of the diagonal: one multiplication and addition for each element
 //   kAcross  a slope, the block across the diagonal: one more
@@ -397,7 +397,7 @@ struct Form {
             c1 = -0.333263189f * into * square;
             c2 = 0.131902963f * into * square * square;
             c3 = -0.0444022268f * into * square * square * square;
-            small = into > 0x1p-17f && into < 0x1p17f ? kSmall / into : 0.f;       // where into^7 and what it is multiplied with are numbers
+            small = into > 0x1p-17f && into < 0x1p17f ? kSmall / into : -1.f;       // where into^7 and what it is multiplied with are numbers
         }
         const float of_bias = capped ? 1.f / F.cap : 1.f / A.scale;
         if constexpr (kSloped) slope = F.slopes[head] * of_bias;
@@ -999,7 +999,7 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_dq
         if (A.form.dtable_parts) buckets.start(skewed[wave]);
     float c = A.scale * kLog2e;
     if constexpr (SCORED) c = form.unit;
-    float lse = 0.f;
+    float lse = SCORED ? INFINITY : 0.f;                     // behind the rows P is zero, whatever the bias: the table's sums run over all lanes
     if (query < seq.q_len) {
         lse = A.lse[stat] * kLog2e;
         if (lane < 32 && at.part == 0) A.delta[stat] = delta;

@@ -520,3 +520,50 @@ def test_rows_past_two_gibibytes():
             samo.samo_attention(q, k, v, a, lse, scores=samo.Scores(**form))
             samo.samo_attention(q, kk, vv, b, lse, scores=samo.Scores(**form))
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n", [1, 33, 130, 200])
+def test_biases_above_the_range_of_the_exponent(n, dim):
+    """exp(300) is no fp32 number: every score has its bias taken off with the row's largest, also beside the last row of a sequence, where lanes have no row
+    whose largest to take.  A bias that all keys have is none."""
+    q, k, v, do = (torch.randn(n, 2, dim, device=DEV).half() for _ in range(4))
+    borders = samo.samo_bucket_borders(8, 40)
+    res = []
+    for value in (0.0, 300.0, -300.0):
+        scores = samo.Scores(table=torch.full((2, 8), value, device=DEV).half(), borders=borders)
+        out, lse, dtable, grads = torch.zeros_like(q), torch.zeros(2, n, device=DEV), torch.zeros(2, 8, device=DEV).half(), [torch.zeros_like(q) for _ in range(3)]
+        samo.samo_attention(q, k, v, out, lse, scores=scores)
+        samo.samo_attention_backward(do, q, k, v, out, lse, *grads, scores=scores, dtable=dtable)
+        res.append([out, *grads, dtable])
+        assert float((lse - value).abs().max()) < 20.0
+    # fp32 holds a score beside 300 to 2^-16: P, and what is formed from it, within 2^-14 of its own
+    for other in res[1:]:
+        for a, b in zip(res[0], other):
+            assert torch.isfinite(b).all()
+            assert float((a.double() - b.double()).norm()) <= 2.0 ** -10 * float(a.double().norm()) + 1e-3
+
+
+@pytest.mark.parametrize("scale, cap", [(2.0 ** 20, 1.0), (2.0 ** 60, 2.0 ** -10), (2.0 ** -20, 1.0), (2.0 ** -60, 256.0)])
+def test_scales_far_from_the_cap(scale, cap):
+    """Powers of scale / cap that are no fp32 numbers: a product of zero has a score of zero, one of 1 or more the cap where scale / cap is 2^20 or more, and
+    almost none where it is 2^-20 or less."""
+    n, dim = 70, 64
+    q, k, v, do = (torch.randn(n, 2, dim, device=DEV).half() for _ in range(4))
+    q[:, 0], k[:, 1] = 0, 1
+    q[:, 1] = torch.randn(n, device=DEV).sign()[:, None].half()
+    out, lse, grads = torch.zeros_like(q), torch.zeros(2, n, device=DEV), [torch.zeros_like(q) for _ in range(3)]
+    scores = samo.Scores(cap=cap)
+    samo.samo_attention(q, k, v, out, lse, causal=True, scale=scale, scores=scores)
+    samo.samo_attention_backward(do, q, k, v, out, lse, *grads, causal=True, scale=scale, scores=scores)
+    # every score of a row is the same: values' means, and the logarithm of their number beside the score
+    counts = torch.arange(1, n + 1, device=DEV).double()
+    means = v.double().cumsum(0) / counts[:, None, None]
+    score = torch.zeros(2, n, device=DEV).double()
+    score[1] = q[:, 1, 0].double() * (cap if scale / cap > 1 else 64 * scale)
+    # P to fp16, weights below 1, and out to fp16: 2^-11 each of numbers up to the largest value
+    assert float((out.double() - means).abs().max()) <= 2.0 ** -9 * float(v.abs().max())
+    assert float((lse.double() - counts.log() - score).abs().max()) <= 2.0 ** -14 * 2
+    # dq is scale sum dS k: of q = 0, where the tanh's slope is 1, sums of about 1 times 2^20 pass fp16's 2^16 and are its infinities
+    for g in grads:
+        assert not torch.isnan(g).any() and (scale > 1 or torch.isfinite(g).all())

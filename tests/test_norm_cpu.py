@@ -22,7 +22,7 @@ def norm(**kw):
 
 @pytest.mark.parametrize("kw,want", [
     (dict(tokens=-1), SIZE), (dict(tokens=2 ** 31), SIZE), (dict(hidden=0), SIZE), (dict(hidden=12), SIZE), (dict(hidden=16392), SIZE), (dict(hidden=-8), SIZE),
-    (dict(kind=2), ARG), (dict(kind=-1), ARG), (dict(eps=0.0), ARG), (dict(eps=-1.0), ARG), (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG),
+    (dict(kind=2), ARG), (dict(kind=-1), ARG), (dict(eps=0.0), ARG), (dict(eps=2.0 ** -127), ARG), (dict(eps=-1.0), ARG), (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG),
     (dict(scale=float("nan")), ARG),
 ])
 def test_norm_refuses(kw, want):

@@ -44,6 +44,8 @@ def test_scored_attention_refuses_what_plain_attention_refuses():
     assert L.samo_attention_scored_workspace_bytes(ctypes.byref(attention()), None, ctypes.byref(need)) == NULL
     # the first keys are those of a causal mask
     assert L.samo_attention_scored(ctypes.byref(attention(causal=0)), ctypes.byref(scores(d_first_keys=FAKE)), None) == ARG
+    for scale in (2.0 ** -61, 2.0 ** 61):
+        assert L.samo_attention_scored(ctypes.byref(attention(scale=scale)), ctypes.byref(c), None) == ARG
     # a table's gradient needs a table; results that overlap
     assert L.samo_attention_scored_backward(ctypes.byref(attention()), ctypes.byref(scores(d_table=None, d_dtable=FAKE)), FAKE, 1 << 20, None) == NULL
     assert L.samo_attention_scored(ctypes.byref(attention(out=samo.Heads(FAKE, 0, 64))), ctypes.byref(c), None) == SIZE
