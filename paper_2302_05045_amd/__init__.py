@@ -6,14 +6,15 @@ C ABI declared in ``include/samo.h``, and returns.  All arithmetic and data
 movement happens in the library's HIP kernels.  Memory is allocated where results are
 returned (the index build) and, as scratch given back in stream order, by the index
 build (an eighth of the masks), by weight gradients of small layers, by attention (the backward
-pass, and both where few heads and rows are split) and by the gated block's backward pass with few tiles, unless they are given a
-workspace.  In a capture whose memory is not torch's they go without, or refuse if they cannot.  There is no CPU fallback: if the shared library has not been built,
+pass, and both where few heads and rows are split), by the gated block's backward pass with few tiles and by that of the norms (the vectors'
+gradients), unless they are given a workspace.  In a capture whose memory is not torch's they go without, or refuse if they cannot.  There is no CPU fallback: if the shared library has not been built,
 importing the first symbol raises.
 
 Names and semantics follow ``samo.h`` one to one (Section III of the paper):
 ``samo_build_index``, ``samo_decompress``, ``samo_gather_grads``,
 ``samo_adam_step``, ``samo_fused_step`` and the ``*_batched`` forms on a ``Plan``; for the layers around them
-``samo_attention``, ``samo_glu`` (each with ``_backward``) and the optimizer phase on 8-bit states, ``samo_step8`` and ``Plan8``.
+``samo_attention`` (with ``Scores``: capped, with distance slopes, bias tables or keys seen from everywhere), ``samo_glu``, ``samo_norm`` (each with
+``_backward``) and the optimizer phase on 8-bit states, ``samo_step8`` and ``Plan8``.
 """
 from __future__ import annotations
 
