@@ -352,8 +352,8 @@ struct KeyTiles {
 };
 
 // Scores of another form (SCORED): z = cap tanh(x / cap) + bias(d), x the scaled product.  All of it in units of `unit` and log 2: a product, or its tanh,
-// and a bias are added and enter the exponent by the same multiplication as a plain product.  Without a cap the bias is what the matrix instructions
-// start from, so that it costs the making of its 16 registers; with one it is added behind the tanh.  Biases of a block of queries and keys, whose
+// and a bias are added and enter the exponent by the same multiplication as a plain product.  Slopes without a cap are what the matrix instructions
+// start from, so that they cost the making of 16 registers; with one, and of a table (late), the bias is added to what they leave.  Biases of a block of queries and keys, whose
 // distances are those of its diagonals, come in four kinds:
 //   kSame    one number, where all distances have one bucket: nothing to do for an element (most blocks of long sequences)
 //   kLinear  a slope, the block on one side of the diagonal: one multiplication and addition for each element
@@ -368,6 +368,9 @@ enum { kPlain, kKeys, kCap, kSlope, kTable, kCapSlope, kCapTable, kAll };
 constexpr bool has_cap(int form) { return form == kCap || form >= kCapSlope; }
 constexpr bool has_slope(int form) { return form == kSlope || form == kCapSlope || form == kAll; }
 constexpr bool has_table(int form) { return form == kTable || form >= kCapTable; }
+// Biases of a table alone are found while the products are under way and added to them, not what they start from: both passes, us, before / behind,
+// 8192 tokens in 4, 32 buckets: 16 heads of 64 277 / 273, 32 of 128 on 8 830 / 820, capped 958 / 944.  (A token of 3 sequences, attention_few_kernel: 16.4 / 17.0, so before.)
+constexpr bool late(int form) { return has_table(form) && !has_slope(form); }
 constexpr bool packs(int form) { return form != kPlain && !has_table(form); }
 struct Bias {
     int kind, column;                        // column: of all the block's pairs, the second half behind kMaxBuckets; -1 where they differ
@@ -375,6 +378,7 @@ struct Bias {
     int diagonal;                            // where they differ: of the lane's diagonal, row - column + 31 (blocks of 32 rows)
     float same, step, base;                  // kSame; kLinear: from row to row, and at the lane's first; kAcross: the slope, and the lane's first distance
 };
+__device__ __forceinline__ float of_lane(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * lane, __builtin_bit_cast(int, x))); }
 template <int FORM>
 struct Form {
     static constexpr bool kCapped = has_cap(FORM), kSloped = has_slope(FORM), kTabled = has_table(FORM), kBiased = kSloped || kTabled, tabled = kTabled;
@@ -485,8 +489,11 @@ struct Form {
             if (tabled) {
                 int at = max(b0, min(n, single));
                 for (int i = max(b0, single); i < b1; ++i) at += n >= __builtin_amdgcn_readlane(border, i);
-                const int before = __builtin_amdgcn_ds_bpermute(4 * at, __builtin_bit_cast(int, past)), behind = __builtin_amdgcn_ds_bpermute(4 * at, __builtin_bit_cast(int, ahead));
-                bias += __builtin_bit_cast(float, two_sided && d < 0 ? behind : before);
+                bias += of_lane(past, at);
+                if (two_sided) {
+                    const float behind = of_lane(ahead, at), before = bias;
+                    bias = d < 0 ? behind + (kSloped ? -slope * fabsf((float)d) : 0.f) : before;
+                }
                 if (part == 0) b.diagonal = two_sided && d < 0 ? kMaxBuckets + at : at;
             }
             if (e < ROWS + 31) room[e] = bias;
@@ -515,7 +522,7 @@ struct Form {
     __device__ __forceinline__ f32x16 with_bias(f32x16 s, const Bias &b, const float *room, int block) const
     {
         if constexpr (kBiased) {
-            if (!capped || b.kind == kSame) return s;
+            if (b.kind == kSame) return s;
             if (kSloped && b.kind == kLinear) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] += fmaf(b.step, (float)(32 * block + 8 * (i >> 2) + (i & 3)), b.base);
@@ -569,7 +576,6 @@ __device__ __forceinline__ float scan_of_column(float x, int column)
     scan_step<0x143, 0xc>(x, column);
     return x;
 }
-__device__ __forceinline__ float of_lane(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * lane, __builtin_bit_cast(int, x))); }
 
 // The table's gradient: lane l holds the sums of dS over the pairs of bucket l so far.  A block whose pairs have one column adds to its lanes' own sums, which meet
 // when the column changes.  Of another one the diagonals are added: half of its rows at a time go to LDS, each shifted by its number, so that a
@@ -659,7 +665,7 @@ struct BucketSums {
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
+    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM), kLate = late(FORM);
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
     __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
@@ -720,7 +726,7 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_ke
         f32x16 s[2];
         clear(s);
         [[maybe_unused]] Bias bias = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
-        if constexpr (kBiased) {
+        if constexpr (kBiased && !kLate) {
             const int base = w_first + M.shift - k0;
             if (kPacks && pack > 1) bias = form.template plan<kTileRows, -1>(nullptr, base, query + M.shift - k0, (w_row + kWaveRows - 1) / pack - w_first);
             else bias = form.template plan<kTileRows, -1>(biases[kTabled ? wave : 0], base);
@@ -733,11 +739,13 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_ke
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(kt, kb, ks), own[ks], s[kb], 0, 0, 0);
+        if constexpr (kLate) bias = form.template plan<kTileRows, -1>(biases[wave], w_first + M.shift - k0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             if constexpr (kCapped)
                 if (form.capped) s[kb] = form.tanhs(s[kb]);
-            if constexpr (kCapped && kBiased) s[kb] = form.with_bias(s[kb], bias, biases[kTabled ? wave : 0], kb);
+            if constexpr (kBiased)
+                if (kLate || form.capped) s[kb] = form.with_bias(s[kb], bias, biases[kTabled ? wave : 0], kb);
         }
         if (!M.all(w_first, w_last, k0, k0 + kTileRows - 1)) {
 #pragma unroll
@@ -859,7 +867,8 @@ __global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnA
         for (int kb = 0; kb < 2; ++kb) {
             if constexpr (kCapped)
                 if (form.capped) s[kb] = form.tanhs(s[kb]);
-            if constexpr (kCapped && kBiased) s[kb] = form.with_bias(s[kb], bias, biases[kTabled ? wave : 0], kb);
+            if constexpr (kBiased)
+                if (form.capped) s[kb] = form.with_bias(s[kb], bias, biases[kTabled ? wave : 0], kb);
         }
         if (!M.all(0, last, k0, k0 + kTileRows - 1)) {
 #pragma unroll
@@ -947,7 +956,7 @@ __global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnA
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_dq_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
+    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM), kLate = late(FORM);
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];
     __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
@@ -1025,10 +1034,9 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_dq
             clear(dp);
             [[maybe_unused]] Bias bias = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
             float less = lse;
-            if constexpr (kBiased) {
+            if constexpr (kBiased && !kLate) {
                 bias = form.template plan<32, -1>(biases[kTabled ? wave : 0], w_first + M.shift - k1);
                 if (form.starts(bias)) s[0] = form.biases(bias, biases[kTabled ? wave : 0], 0);
-                less = fmaf(-bias.same, c, lse);
             }
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -1036,9 +1044,12 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_dq
                 dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(vt, kb, ks), down[ks], dp[0], 0, 0, 0);
             }
             [[maybe_unused]] f32x16 t;
-            if constexpr (kCapped) {
+            if constexpr (kLate) bias = form.template plan<32, -1>(biases[wave], w_first + M.shift - k1);
+            if constexpr (kCapped)
                 if (form.capped) s[0] = t = form.tanhs(s[0]);
-                if constexpr (kBiased) s[0] = form.with_bias(s[0], bias, biases[kTabled ? wave : 0], 0);
+            if constexpr (kBiased) {
+                if (kLate || form.capped) s[0] = form.with_bias(s[0], bias, biases[kTabled ? wave : 0], 0);
+                less = fmaf(-bias.same, c, lse);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -less)) * (dp[0][i] - delta);
@@ -1091,7 +1102,7 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 template <int KS, int SIDES, int FORM>
 __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
+    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM), kLate = late(FORM);
     constexpr bool kWide = KS > 6, kLean = kWide && FORM != kPlain;
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile + (kWide + kLean) * kOwnRows * PITCH];       // Q, dO; two tiles each; V, K
@@ -1185,10 +1196,9 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
             clear(dp);
             [[maybe_unused]] Bias bias = {kSame, -1, 0, -1, 0.f, 0.f, 0.f};
             [[maybe_unused]] float more = 0.f;
-            if constexpr (kBiased) {
+            if constexpr (kBiased && !kLate) {
                 bias = form.template plan<32, 1>(biases[kTabled ? wave : 0], q1 + M.shift - w_first);
                 if (form.starts(bias)) s[0] = form.biases(bias, biases[kTabled ? wave : 0], 0);
-                more = bias.same * c;
             }
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -1197,6 +1207,11 @@ __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(
                 const half8 v = kWide ? read_rows<PITCH>(v_rows, 0, ks) : ownv[kWide ? 0 : ks];
                 dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(read_rows<PITCH>(dot, qb, ks), v, dp[0], 0, 0, 0);
             }
+            if constexpr (kLate) {
+                bias = form.template plan<32, 1>(biases[wave], q1 + M.shift - w_first);
+                if constexpr (!kCapped) s[0] = form.with_bias(s[0], bias, biases[wave], 0);
+            }
+            if constexpr (kBiased) more = bias.same * c;
             if constexpr (kCapped)
                 if (form.capped) {                           // dP - delta, times the cap's slope
                     s[0] = form.tanhs(s[0]);
