@@ -1,4 +1,5 @@
 """Refusals of attention with scores of another form on the host, before anything is launched, and the sizes of its workspaces."""
+import concurrent.futures
 import ctypes
 
 import pytest
@@ -84,9 +85,20 @@ def test_bucket_borders():
             cpu(buckets, far)
 
 
-@pytest.mark.parametrize("form", ["keys", "cap", "slope", "table", "cap_slope", "cap_table", "all"])
-def test_m0_is_touched_only_by_the_copies_into_lds_in_the_forms_kernels(tmp_path, form):
-    test_operators_cpu.test_m0_is_touched_only_by_the_copies_into_lds(tmp_path, "attention_%s.hip" % form)
+FORMS = ["keys", "cap", "slope", "table", "cap_slope", "cap_table", "all"]
+
+
+@pytest.fixture(scope="module")
+def compiled(tmp_path_factory):
+    """What became of each form's source, compiled side by side."""
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:
+        check = test_operators_cpu.test_m0_is_touched_only_by_the_copies_into_lds
+        yield {form: pool.submit(check, tmp_path_factory.mktemp(form), "attention_%s.hip" % form) for form in FORMS}
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_m0_is_touched_only_by_the_copies_into_lds_in_the_forms_kernels(compiled, form):
+    compiled[form].result()
 
 
 def test_a_table_of_too_many_heads_is_refused():
