@@ -560,7 +560,7 @@ samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, cons
  * Arithmetic is fp32, out is formed from s' before its rounding, sums over a row and over the tokens are fp32 in a fixed order; each result is rounded once.
  * The backward pass forms N(s') from the stored s' and the stats.  Squares are fp32: rows of 2^62 and more have no finite norm.
  * d_new_stream may be d_stream and d_dstream d_dnew (in place); other results overlap nothing.  hidden: a multiple of 8 up to 16384; tokens below 2^31,
- * 0 of them give vectors of zeros; eps is 2^-126 or more (the reciprocal root takes smaller numbers as zero).
+ * 0 of them give vectors of zeros (d_y may be NULL then, with a block or without); eps is 2^-126 or more (the reciprocal root takes smaller numbers as zero).
  * d_workspace: samo_norm_workspace_bytes on the current device, 16-byte aligned, for the vectors' gradients (0 bytes where none is wanted); in use until
  * the stream has passed the call. */
 enum { SAMO_NORM_RMS = 0, SAMO_NORM_LAYER = 1 };

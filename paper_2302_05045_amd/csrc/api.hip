@@ -1517,15 +1517,16 @@ samo_status check_norm(const samo_norm_desc *d, bool backward, NormArgs *a)
     a->tokens = d->tokens;
     a->hidden = d->hidden;
     a->layer = d->kind == SAMO_NORM_LAYER;
-    a->y_norm = d->d_y && d->y_norm != 0;
+    const bool block = d->d_y && d->tokens > 0;      // without tokens all sums are zero, whatever the vectors hold
+    a->y_norm = block && d->y_norm != 0;
     a->stream_fp32 = d->stream_fp32 != 0;
     a->eps = d->eps;
-    a->scale = d->d_y ? d->scale : 0.f;
+    a->scale = block ? d->scale : 0.f;
     a->stream = d->d_stream;
     a->y = halves(d->d_y);
     a->weight = halves(d->d_weight);
     a->bias = halves(d->d_bias);
-    a->gate = d->d_y ? halves(d->d_gate) : nullptr;
+    a->gate = block ? halves(d->d_gate) : nullptr;
     a->y_weight = a->y_norm ? halves(d->d_y_weight) : nullptr;
     a->y_bias = a->y_norm ? halves(d->d_y_bias) : nullptr;
     a->new_stream = d->d_new_stream;
@@ -1535,7 +1536,8 @@ samo_status check_norm(const samo_norm_desc *d, bool backward, NormArgs *a)
     const void *more[] = {d->d_dout, d->d_dnew, d->d_dstream, d->d_dy, d->d_dweight, d->d_dbias, d->d_dy_weight, d->d_dy_bias, d->d_dgate};
     for (const void *p : more)
         if (misaligned(p)) return SAMO_ERR_ALIGN;
-    if ((!a->y_norm && (d->d_dy_weight || d->d_dy_bias)) || (!d->d_y && (d->d_dgate || d->d_dy))) return SAMO_ERR_ARG;
+    const bool may_be = d->d_y || d->tokens == 0;    // a y of no elements has no address
+    if ((!(may_be && d->y_norm) && (d->d_dy_weight || d->d_dy_bias)) || (!may_be && (d->d_dgate || d->d_dy))) return SAMO_ERR_ARG;
     a->dout = halves(d->d_dout);
     a->dnew = d->d_dnew;
     a->dstream = d->d_dstream;

@@ -381,3 +381,25 @@ def test_native_and_python_descriptors_agree():
                 continue
             if done:
                 assert all(getattr(native, name) == getattr(python, name) for name in fields), at
+
+
+@pytest.mark.parametrize("kind,after", KINDS)
+def test_no_tokens_give_vectors_of_zeros(kind, after):
+    """A micro-batch without tokens, whatever is around it: zeros, also where a vector holds what is not finite; by native code and in Python."""
+    h = 72
+    some = lambda *at: torch.ones(h, device=DEV).half().index_fill_(0, torch.tensor(at, device=DEV, dtype=torch.long), float("inf"))
+    names = ["weight", "bias"] + ["gate"] * bool(after) + ["y_weight", "y_bias"] * (after == "norm")
+    norm = samo.Norm(kind=kind, y_norm=after == "norm", scale=0.5, **{n: some(3, 5) for n in names})
+    for stream32 in (False, True):
+        rows, stats = torch.zeros(0, h, device=DEV).half(), torch.zeros(0, 4, device=DEV)
+        stream = rows.float() if stream32 else rows
+        y = rows if after else None
+        samo.samo_norm(norm, stream, rows, y=y, new_stream=stream if after else None, stats=stats)
+        for native in (samo._marshal, None):
+            grads = samo.NormGrads(**{n: torch.full((h,), float("nan"), device=DEV).half() for n in names})
+            kept, samo._marshal = samo._marshal, native
+            try:
+                samo.samo_norm_backward(norm, rows, stream, stats, stream, dnew=stream, y=y, dy=y, grads=grads)
+            finally:
+                samo._marshal = kept
+            assert all(torch.all(getattr(grads, n) == 0) for n in names)

@@ -72,3 +72,22 @@ def test_norm_workspace():
     assert ask(d_dgate=FAKE, d_dy_weight=FAKE, d_dy_bias=FAKE, d_dweight=FAKE, d_dbias=FAKE) == 4 * row
     assert ask(d_dgate=FAKE, y_norm=0) == row and ask(d_dweight=FAKE, tokens=0) == 0
     assert ask(d_dweight=FAKE, tokens=1 << 20) <= 4 * 64 * 4096
+
+
+@pytest.mark.parametrize("y_norm", [0, 1])
+def test_no_tokens_refuse_no_gradient_of_the_block(y_norm):
+    """Tensors of no elements have no address: a block's output that is empty is not one that is missing, and no workspace is needed."""
+    L, need = samo.lib(), ctypes.c_size_t()
+    vectors = ["d_dweight", "d_dbias", "d_dgate", "d_dy_weight", "d_dy_bias"]
+    none = {n: None for n in ["d_stream", "d_y", "d_new_stream", "d_out", "d_stats", "d_dout", "d_dnew", "d_dstream", "d_dy"] + vectors}
+
+    def ask(wanted):
+        need.value = 7
+        kw = dict(none, **{n: FAKE * (50 + i) for i, n in enumerate(wanted)})
+        return L.samo_norm_workspace_bytes(ctypes.byref(norm(tokens=0, y_norm=y_norm, **kw)), ctypes.byref(need))
+
+    there = vectors if y_norm else vectors[:3]
+    for wanted in [[n] for n in there] + [there]:
+        assert ask(wanted) == OK and need.value == 0, wanted
+    for name in () if y_norm else vectors[3:]:               # there is no norm behind the block, with tokens or without
+        assert ask([name]) == ARG and need.value == 7, name
