@@ -490,7 +490,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * each part where it is given:
  *   scale           2^-60 to 2^60
  *   cap             0: none; otherwise 2^-10 to 256
- *   d_slopes        float[heads], finite
+ *   d_slopes        float[heads], finite; the bias of a distance is within 2^-20 of itself
  *   d_table         fp16[heads * columns], head by head, finite; d_borders int32[buckets - 1], ascending from 1 or more: a distance's bucket is the number
  *                   of borders up to it.  1 to SAMO_ATTENTION_MAX_BUCKETS buckets.  two_sided == 0: columns = buckets, column(d) = bucket(max(d, 0));
  *                   otherwise columns = 2 buckets, column(d) = bucket(d) and, where the key lies behind (d < 0), buckets + bucket(-d).

@@ -356,12 +356,14 @@ struct KeyTiles {
 // start from, so that they cost the making of 16 registers; with one, and of a table (late), the bias is added to what they leave.  Biases of a block of queries and keys, whose
 // distances are those of its diagonals, come in four kinds:
 //   kSame    one number, where all distances have one bucket: nothing to do for an element (most blocks of long sequences)
-//   kLinear  a slope, the block on one side of the diagonal: one multiplication and addition for each element
-//   kAcross  a slope, the block across the diagonal: one more
+//   kLinear  a slope, the block on one side of the diagonal and kNear or more from it: one multiplication and addition for each element.  The line begins
+//            at most 63 distances from an element's, so that its rounding is that of a bias of twice the size at most
+//   kAcross  a slope, the block nearer: one more, and each bias by itself, exact on the diagonal whatever the slope
 //   kLaid    buckets that differ: the wave works out its diagonals' biases, a lane each, and lays them into LDS
 // The table's columns and borders live in the wave's lanes: the bucket of a distance that the lanes agree on is the number of set bits of a comparison.
 constexpr int kMaxBuckets = SAMO_ATTENTION_MAX_BUCKETS;
 enum { kSame, kLinear, kAcross, kLaid };
+constexpr int kNear = 64;
 // Which parts there are, kernels of their own: none (kKeys: but the first keys), one, two; kAll: slopes and a table, with a cap or without.  With one kernel
 // for the last three, both passes, us: 8192 tokens in 4, 32 heads of 128 on 8, cap and slopes 1313 and 1114; 16 heads of 64, cap and 32 buckets 385 and 331.
 enum { kPlain, kKeys, kCap, kSlope, kTable, kCapSlope, kCapTable, kAll };
@@ -472,7 +474,7 @@ struct Form {
         } else {
             if constexpr (kSloped) {
                 const float first = (float)(own + SIGN * 4 * (lane >> 5));
-                const bool one_side = lo >= 0 || hi <= 0;
+                const bool one_side = lo >= kNear || hi <= -kNear;
                 const float down = one_side && lo < 0 ? slope : -slope;
                 b.kind = one_side ? kLinear : kAcross;
                 b.step = one_side ? SIGN * down : down;

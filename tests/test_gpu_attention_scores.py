@@ -567,3 +567,53 @@ def test_scales_far_from_the_cap(scale, cap):
     # dq is scale sum dS k: of q = 0, where the tanh's slope is 1, sums of about 1 times 2^20 pass fp16's 2^16 and are its infinities
     for g in grads:
         assert not torch.isnan(g).any() and (scale > 1 or torch.isfinite(g).all())
+
+
+def check_slopes(dim, lens_q, lens_k, kv, slopes):
+    """The tolerances of check(); the exponents' offs are those of the keys that count: 2^-20 sum P |bias|."""
+    heads = len(slopes)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(dim)
+    rnd = lambda n, h: torch.randn((n, h, dim), generator=gen, device=DEV).half()
+    tq, tk = sum(lens_q), sum(lens_k)
+    q, k, v, do = rnd(tq, heads), rnd(tk, kv), rnd(tk, kv), rnd(tq, heads)
+    out, lse, dq, dk, dv = torch.zeros_like(q), torch.zeros(heads, tq, device=DEV), torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    slope = torch.tensor(slopes, device=DEV)
+    starts = lambda ns: torch.tensor(np.concatenate([[0], np.cumsum(ns)]), dtype=torch.int32, device=DEV)
+    args = dict(q_start=starts(lens_q), k_start=starts(lens_k), max_q=max(lens_q), max_k=max(lens_k), scores=samo.Scores(slopes=slope))
+    samo.samo_attention(q, k, v, out, lse, **args)
+    samo.samo_attention_backward(do, q, k, v, out, lse, dq, dk, dv, **args)
+    q0 = k0 = 0
+    for n, m in zip(lens_q, lens_k):
+        seen = seen_of(n, m, True, 0)
+        d = torch.arange(n, device=DEV)[:, None] + (m - n) - torch.arange(m, device=DEV)[None, :]
+        grads = {}
+        for h in range(heads):
+            g = h * kv // heads
+            a = [q[q0:q0 + n, h], k[k0:k0 + m, g], v[k0:k0 + m, g], do[q0:q0 + n, h]]
+            r, b = reference(*a, dim ** -0.5, seen, 0.0, slope[h], None, None, d)
+            z = torch.where(seen, a[0].double() @ a[1].double().T * dim ** -0.5 - slope[h].double() * d.abs(), -math.inf)
+            off = (torch.softmax(z, 1) * (slope[h].double() * d).abs()).sum(1) * 2.0 ** -20
+            bound = 2.0 ** -23 * (dim + 8) * b["s"] + 2.0 ** -20 * (1 + r["lse"].abs()) + off
+            err = (lse[h, q0:q0 + n].double() - r["lse"]).abs()
+            assert torch.all(err <= bound), ("lse", slopes[h], n, m, float(err.max()), float((err / bound).max()))
+            for name, got, most in (("out", out, 1.25), ("dq", dq, 3.0)):
+                err = (got[q0:q0 + n, h].double() - r[name]).abs()
+                assert torch.all(err <= most * U * b[name] + U * r[name].abs() + 2.0 ** -25), (name, slopes[h], n, m)
+            for name in ("dk", "dv"):
+                x, c = grads.get((name, g), (0, 0))
+                grads[name, g] = (x + r[name], c + b[name])
+        for (name, g), (want, size) in grads.items():
+            err = ((dk if name == "dk" else dv)[k0:k0 + m, g].double() - want).abs()
+            assert torch.all(err <= 3.0 * U * size + U * want.abs() + 2.0 ** -25), (name, n, m, g)
+        q0, k0 = q0 + n, k0 + m
+
+
+SLOPED = [(64, [300, 1, 70], [300, 1, 70], 6), (128, [130], [200], 2), (80, [1, 2], [300, 70], 2), (64, [40], [400], 6),
+          (64, [1, 1], [64, 640], 6), (64, [1, 2], [640, 65], 2), (128, [70, 33], [133, 64], 2), (96, [100], [131], 6)]       # a block's corner on the diagonal
+
+
+@pytest.mark.parametrize("dim, lens_q, lens_k, kv", SLOPED)
+def test_steep_slopes(dim, lens_q, lens_k, kv):
+    """A slope's bias is within 2^-20 of itself at every distance, so that next to a query it stays what it is however steep the slope."""
+    check_slopes(dim, lens_q, lens_k, kv, [0.35, -0.01, 30.3, 700.1, 5000.7, 20000.3])
