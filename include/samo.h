@@ -490,7 +490,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * each part where it is given:
  *   scale           2^-60 to 2^60
  *   cap             0: none; otherwise 2^-10 to 256
- *   d_slopes        float[heads], finite; the bias of a distance is within 2^-20 of itself
+ *   d_slopes        float[heads], up to 2^30 in size; the bias of a distance is within 2^-20 of itself
  *   d_table         fp16[heads * columns], head by head, finite; d_borders int32[buckets - 1], ascending from 1 or more: a distance's bucket is the number
  *                   of borders up to it.  1 to SAMO_ATTENTION_MAX_BUCKETS buckets.  two_sided == 0: columns = buckets, column(d) = bucket(max(d, 0));
  *                   otherwise columns = 2 buckets, column(d) = bucket(d) and, where the key lies behind (d < 0), buckets + bucket(-d).
@@ -504,6 +504,8 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * 2^-22 elsewhere.  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
  * A call of at most 128 rows a sequence, max_q times the heads that share keys, holds them in one tile, and of at most 32 rows and more than 128 keys its waves share the
  * keys: blocks of queries and keys (where what is not finite reaches) are those rows and 64 keys then.  heads < 2^21 with d_dtable.
+ * Scores and lse are fp32.  z - lse, the exponent of the backward pass's P, is off by up to 2^-18 |lse|: of account where biases make lse large, as in a row
+ * that sees far keys only (2^-6 at 2^12; from 2^20 on its gradients need be no numbers).
  * Everything else, alignment and limits, is as for samo_attention; slopes, borders and first_keys 4-byte, table and dtable 2-byte aligned.
  * samo_attention_scored_workspace_bytes: what the backward call needs (delta, and for d_dtable the parts of its sums) on the current device. */
 #define SAMO_ATTENTION_MAX_BUCKETS 64

@@ -364,6 +364,9 @@ struct KeyTiles {
 constexpr int kMaxBuckets = SAMO_ATTENTION_MAX_BUCKETS;
 enum { kSame, kLinear, kAcross, kLaid };
 constexpr int kNear = 64;
+// Where a row's largest score so far, in log 2, is beyond this, its product with `unit` is off by more than 2^-8 and the exponents are taken from the
+// difference of the scores (slopes only: a cap and a table keep scores below it, but for those of plain products).
+constexpr float kFarScore = 0x1p16f;
 // Which parts there are, kernels of their own: none (kKeys: but the first keys), one, two; kAll: slopes and a table, with a cap or without.  With one kernel
 // for the last three, both passes, us: 8192 tokens in 4, 32 heads of 128 on 8, cap and slopes 1313 and 1114; 16 heads of 64, cap and 32 buckets 385 and 331.
 enum { kPlain, kKeys, kCap, kSlope, kTable, kCapSlope, kCapTable, kAll };
@@ -542,6 +545,18 @@ struct Form {
 };
 constexpr int kBiasRoom = 96;                // floats of a wave's biases
 
+// Scores of rows whose largest is far from zero as differences from it, and what is to be taken off them then.
+__device__ __forceinline__ void from_top(f32x16 (&s)[2], float top, float &against)
+{
+    if (!__ballot(fabsf(against) > kFarScore)) return;
+    top = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] -= top;
+    against = 0.f;
+}
+
 // Waves to a SIMD that the registers of the forms' kernels leave room for, forward and dQ.  Heads of 33 to 64: three without a spilled register; dQ of
 // 32 buckets, 8 x 1024 in both directions, 12 heads of 64, 84 us with two and 68 with three (768 workgroups are one round then); four would spill in the forward
 // pass (4093 tokens in 7, 16 heads, both passes 109 us with three there, 113 with four).
@@ -667,7 +682,7 @@ struct BucketSums {
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_kernel(const AttnArgs A)
 {
-    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM), kLate = late(FORM);
+    constexpr bool SCORED = FORM != kPlain, kCapped = has_cap(FORM), kTabled = has_table(FORM), kSloped = has_slope(FORM), kBiased = kTabled || kSloped, kLate = late(FORM);
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * kTile];       // K, V; two tiles each
     __shared__ float biases[kTabled ? kAttnThreads / 64 : 1][kBiasRoom];
@@ -762,7 +777,7 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_ke
         if constexpr (kBiased) most += bias.same;
         // Only where a row's largest score passes what its exponents are taken against by 2^8 are the sums so far brought down: P stays
         // below 2^8 otherwise, which fp16 holds as well as numbers below 1.
-        if (__ballot(most * c > top * c + 8.f)) {
+        if (__ballot(kSloped ? (most - top) * c > 8.f : most * c > top * c + 8.f)) {
             const float next = fmaxf(top, most);
             const float down = next == top ? 1.f : __builtin_amdgcn_exp2f((top - next) * c);
             top = next;
@@ -774,6 +789,7 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_ke
         }
         float against = top == -INFINITY ? 0.f : top * c;    // a row that has seen no key yet
         if constexpr (kBiased) against -= bias.same * c;
+        if constexpr (kSloped) from_top(s, top, against);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -808,7 +824,7 @@ __global__ void __launch_bounds__(kAttnThreads, waves_of(KS, FORM)) attention_ke
 template <int KS, int FORM>
 __global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnArgs A)
 {
-    constexpr bool kCapped = has_cap(FORM), kTabled = has_table(FORM), kBiased = kTabled || has_slope(FORM);
+    constexpr bool kCapped = has_cap(FORM), kTabled = has_table(FORM), kSloped = has_slope(FORM), kBiased = kTabled || kSloped;
     constexpr bool kPacks = packs(FORM);
     constexpr int DB = blocks_of(KS), PITCH = pitch_of(KS), kTile = tile_bytes(KS), kWaves = kAttnThreads / 64;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[kWaves][2 * kTile];            // a wave's K, V
@@ -892,6 +908,7 @@ __global__ void __launch_bounds__(kAttnThreads) attention_few_kernel(const AttnA
             for (int i = 0; i < 16; ++i) out[db][i] *= down;
         float against = top == -INFINITY ? 0.f : top * c;
         if constexpr (kBiased) against -= bias.same * c;
+        if constexpr (kSloped) from_top(s, top, against);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll

@@ -617,3 +617,26 @@ SLOPED = [(64, [300, 1, 70], [300, 1, 70], 6), (128, [130], [200], 2), (80, [1, 
 def test_steep_slopes(dim, lens_q, lens_k, kv):
     """A slope's bias is within 2^-20 of itself at every distance, so that next to a query it stays what it is however steep the slope."""
     check_slopes(dim, lens_q, lens_k, kv, [0.35, -0.01, 30.3, 700.1, 5000.7, 20000.3])
+
+
+@pytest.mark.parametrize("dim, lens_q, lens_k, kv", SLOPED)
+def test_scores_that_slopes_take_far_from_zero(dim, lens_q, lens_k, kv):
+    """Scores of 2^28 to 2^38 at the first keys of a row, which are met first: their rounded products are no exponents, and none of it stays."""
+    check_slopes(dim, lens_q, lens_k, kv, [0.35, 7e5 + 0.3, 1.1e7, 1.0e8, 2.0 ** 30, 1.0e9])
+
+
+@pytest.mark.parametrize("cap, buckets", [(0.0, 0), (20.0, 0), (20.0, 8)])
+@pytest.mark.parametrize("queries", [1, 40])
+def test_far_keys_alone(queries, cap, buckets):
+    """Slopes that grow with the distance (or fall) so that a row's largest score is far from zero: lse within 2^-18 of itself, out that of the one key that
+    is left, nothing that is not finite."""
+    heads, dim, n = 4, 64, 700
+    q, k, v = (torch.randn(m, heads, dim, device=DEV).half() for m in (queries, n, n))
+    slope = torch.tensor([-2.0 ** 10, -2.0 ** 20, -2.0 ** 24, -2.0 ** 30], device=DEV)
+    table = torch.randn(heads, buckets, device=DEV).half() if buckets else None
+    scores = samo.Scores(cap=cap, slopes=slope, table=table, borders=samo.samo_bucket_borders(buckets, 40) if buckets else None)
+    out, lse = torch.zeros_like(q), torch.zeros(heads, queries, device=DEV)
+    samo.samo_attention(q, k, v, out, lse, scores=scores)
+    want = -slope.double()[:, None] * (torch.arange(queries, device=DEV) + n - queries)[None, :]       # the first key, score and table aside
+    assert torch.all((lse.double() - want).abs() <= 2.0 ** -18 * want.abs() + 64.0)
+    assert float((out.double() - v[0].double()).abs().max()) <= 2.0 ** -10 * float(v[0].abs().max())
