@@ -499,7 +499,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * Backward: dz = P (dP - delta), dS = dz (1 - (cap tanh(x / cap) / cap)^2) enters dq and dk, and
  *   d_dtable        fp16[heads * columns] or NULL: the sums of dz over the pairs of every column, rounded once; all of it is written, columns of no pair
  *                   as zero.  With a loss scale in dout it is the scaled gradient, as any g.
- * Sums of dz are fp32 within 32 queries of a part, double over those; their order is fixed.  The slopes are constants and have no gradient.
+ * Sums of dz are fp32 within 128 queries of a part, double over those; their order is fixed.  The slopes are constants and have no gradient.
  * The tanh is within 2^-20 of itself in blocks of 32 queries and 32 keys whose |x| are all up to half the cap (scale / cap between 2^-17 and 2^17), within
  * 2^-22 elsewhere.  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
  * A call of at most 128 rows a sequence, max_q times the heads that share keys, holds them in one tile, and of at most 32 rows and more than 128 keys its waves share the
