@@ -502,8 +502,9 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
  * Sums of dz are fp32 within 128 queries of a part, double over those; their order is fixed.  The slopes are constants and have no gradient.
  * The tanh is within 2^-20 of itself in blocks of 32 queries and 32 keys whose |x| are all up to half the cap (scale / cap between 2^-17 and 2^17), within
  * 2^-22 elsewhere.  1 - tanh^2 is formed from it: of little account where a row's largest scores are not all at the cap.
- * A call of at most 128 rows a sequence, max_q times the heads that share keys, holds them in one tile, and of at most 32 rows and more than 128 keys its waves share the
- * keys: blocks of queries and keys (where what is not finite reaches) are those rows and 64 keys then.  heads < 2^21 with d_dtable.
+ * A call of at most 128 rows a sequence, max_q times the heads that share keys (with a table max_q alone: a tile has the queries of one head then), holds them in
+ * one tile, and of at most 32 rows and more than 128 keys its waves share the keys: blocks of queries and keys (where what is not finite reaches) are those
+ * rows and 64 keys then.  heads < 2^21 with d_dtable.
  * Scores and lse are fp32.  z - lse, the exponent of the backward pass's P, is off by up to 2^-18 |lse|: of account where biases make lse large, as in a row
  * that sees far keys only (2^-6 at 2^12; from 2^20 on its gradients need be no numbers).
  * Everything else, alignment and limits, is as for samo_attention; slopes, borders and first_keys 4-byte, table and dtable 2-byte aligned.
