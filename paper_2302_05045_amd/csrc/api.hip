@@ -1322,7 +1322,7 @@ samo_status samo_attention_backward(const samo_attention_desc *h_desc, void *d_w
 namespace {
 
 constexpr float kLeastScale = 0x1p-60f, kMostScale = 0x1p60f;     // biases are held in units of it
-constexpr float kLeastCap = 1.f / 1024.f, kMostCap = 256.f;       // the tanh is within 2^-22, so that a score is within 2^-14
+constexpr float kLeastCap = 1.f / 1024.f, kMostCap = 256.f;       // the tanh is within 2^-20 of itself up to a half, 2^-22 above, so that a score is within 2^-13
 
 samo_status check_scores(const samo_attention_scores *s, bool backward, AttnArgs *a)
 {

@@ -640,3 +640,24 @@ def test_far_keys_alone(queries, cap, buckets):
     want = -slope.double()[:, None] * (torch.arange(queries, device=DEV) + n - queries)[None, :]       # the first key, score and table aside
     assert torch.all((lse.double() - want).abs() <= 2.0 ** -18 * want.abs() + 64.0)
     assert float((out.double() - v[0].double()).abs().max()) <= 2.0 ** -10 * float(v[0].abs().max())
+
+
+@pytest.mark.parametrize("cap", [2.0 ** -10, 1.0, 30.0, 256.0])
+@pytest.mark.parametrize("into", [1.0, 2.0 ** -7, 2.0 ** 9])
+def test_the_tanh(cap, into):
+    """Of one key lse is its score, cap tanh(x / cap); x is exact, a single product.  Up to half the cap the tanh is within 2^-20 of itself: a polynomial
+    off by 5.5e-7, its coefficients (scaled by powers of two here) and four operations by 2^-25 and 2^-24 each, the largest of them once.  Above it is
+    within 2^-22.  The score goes into units of log 2 and back by four roundings, 2^-22 of itself."""
+    n, dim = 8192, 16
+    t = torch.cat([0.5 * 2.0 ** (-12 * torch.rand(n // 2, device=DEV)), 0.5 + 11.5 * torch.rand(n // 2, device=DEV)])
+    q, k, v = (torch.zeros(n, 1, dim, device=DEV).half() for _ in range(3))
+    q[:, 0, 3], k[:, 0, 3] = (t * 8).half() * (2 * torch.randint(0, 2, (n,), device=DEV) - 1), 0.125 / into
+    starts = torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    out, lse = torch.zeros_like(q), torch.zeros(1, n, device=DEV)
+    samo.samo_attention(q, k, v, out, lse, scale=cap * into, q_start=starts, k_start=starts, max_q=1, max_k=1, scores=samo.Scores(cap=cap))
+    x = q[:, 0, 3].double() / 8
+    want = cap * torch.tanh(x)
+    bound = 2.0 ** -22 * want.abs() + torch.where(x.abs() <= 0.5, 2.0 ** -20 * want.abs(), 2.0 ** -22 * cap)
+    off = (lse[0].double() - want).abs()
+    assert torch.all(off <= bound), float((off / bound).max())
+    assert float(off.max()) <= 2.0 ** -21 * cap               # a score within 2^-13 at the largest cap
