@@ -561,7 +561,8 @@ samo_status samo_glu_backward(const uint16_t *d_dh, const uint16_t *d_gate, cons
  *   d_dstream (of the stream's type) = dnew + the gradient through the norm,   d_dy (with d_y),
  *   and of each vector the sum over the tokens, fp16[hidden], rounded once; NULL: not wanted.  With a loss scale in dout they are the scaled gradients.
  * Arithmetic is fp32, out is formed from s' before its rounding, sums over a row and over the tokens are fp32 in a fixed order; each result is rounded once.
- * The backward pass forms N(s') from the stored s' and the stats.  Squares are fp32: rows of 2^62 and more have no finite norm.
+ * The backward pass forms N(s') from the stored s' and the stats.  Squares are fp32: a row whose squares add up to 2^128 (at 16384 elements, of 2^57 each)
+ * has no norm.
  * d_new_stream may be d_stream and d_dstream d_dnew (in place); other results overlap nothing.  hidden: a multiple of 8 up to 16384; tokens below 2^31,
  * 0 of them give vectors of zeros (d_y may be NULL then, with a block or without); eps is 2^-126 or more (the reciprocal root takes smaller numbers as zero).
  * d_workspace: samo_norm_workspace_bytes on the current device, 16-byte aligned, for the vectors' gradients (0 bytes where none is wanted); in use until
