@@ -6,7 +6,8 @@ namespace samo {
 namespace {
 
 // Whole rows from the sums of their parts, added in order: a wave has 32 rows, and 32 dims of them, as the kernel that left them had.
-// Parts of out are weighed by how far their exponents were taken down; one that has seen no key is not read.
+// Parts of out are weighed by how far their exponents were taken down; one that has seen no key does not count.  Four parts are asked for at a time, whatever
+// their number; before, one after the other: a token behind 8191, 32 heads of 128 on 8 (16 parts), 33 us, now 27; two and three parts within 1 % of what they were.
 template <int DB, int WHICH>
 __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs A)
 {
@@ -78,7 +79,8 @@ __global__ void __launch_bounds__(DB * 64) attention_join_kernel(const AttnArgs 
     store_own<1>(to + 32 * db, stride, row, count, A.dim - 32 * db, acc, factor);
 }
 
-// The table's gradient: a head's workgroup adds what the workgroups of dQ left, in order, a column to a thread.
+// The table's gradient: a head's workgroup adds what the workgroups of dQ left, in order, a column to a thread.  A chain of loads, a row of every eight each:
+// 4.7 us of 7 ragged sequences, 16 heads and 32 buckets, but 9.3 of 256 sequences of 64 tokens and 55 of 256 of 512 (dQ and dK, dV: 1480).
 constexpr int kTableThreads = 1024, kTableRows = kTableThreads / (2 * kMaxBuckets);
 __global__ void __launch_bounds__(kTableThreads) table_gradient_kernel(const float *parts, int64_t slots, int columns, _Float16 *to)
 {
@@ -112,10 +114,10 @@ int64_t sums_bytes(int which, const AttnArgs &a, int splits)
 // What a launch costs with its keys (for dK and dV: queries) in so many parts, us.  A workgroup works through tiles of 64; the device's share of all of them,
 // and as the launch ends half the longest workgroup besides; the longest one by itself; and for parts a second kernel and the sums, written and read.
 // A tile by itself takes 1.25 us with heads of 64 and 1.5 with 128, 1.4 and 2.3 where two workgroups share a compute unit; the backward pass's
-// a quarter more.  Measured against the parts taken, whole calls, us: one token behind 8191, 32 heads of 128 on 8, 181 with one part, 36 with 8, 33 with 16;
-// 2000 tokens in 3 sequences behind 3000 each, 16 heads of 64, 72 and 57 with three; 4096 tokens, 8 heads of 128, 89 and 59 with three; 1024 tokens of
-// 16 heads of 96 23 and 25 with two, which it takes; 2048 in 4 sequences, 16 heads of 64, 13 and 23 with two; one token each behind 8 contexts of 2048, 32 heads of
-// 128, 62, 50 with two and 57 with four.
+// a quarter more.  Measured against the parts taken, whole calls, us: one token behind 8191, 32 heads of 128 on 8, 181 with one part, 34 with 8, 27 with 16;
+// 2000 tokens in 3 sequences behind 3000 each, 16 heads of 64, 72 and 54 with three; 4096 tokens, 8 heads of 128, 90 and 57 with three; 1024 tokens of
+// 16 heads of 96 23 and 25 with two, which it takes; 2048 in 4 sequences, 16 heads of 64, 13 and 23 with two; one token each behind 8 contexts of 2047, 32 heads of
+// 128, 59, 50 with two and 53 with four.
 // Where every workgroup has as much to do, the rounds that they take count whole.
 double launch_us(int which, const AttnArgs &a, int64_t items, int splits)
 {

@@ -365,7 +365,7 @@ constexpr int kMaxBuckets = SAMO_ATTENTION_MAX_BUCKETS;
 enum { kSame, kLinear, kAcross, kLaid };
 constexpr int kNear = 64;
 // Where a row's largest score so far, in log 2, is beyond this, its product with `unit` is off by more than 2^-8 and the exponents are taken from the
-// difference of the scores (slopes only: a cap and a table keep scores below it, but for those of plain products).
+// difference of the scores (slopes only: a table's biases are below 2^17 in log 2, a cap's scores below 2^9).
 constexpr float kFarScore = 0x1p16f;
 // Which parts there are, kernels of their own: none (kKeys: but the first keys), one, two; kAll: slopes and a table, with a cap or without.  With one kernel
 // for the last three, both passes, us: 8192 tokens in 4, 32 heads of 128 on 8, cap and slopes 1313 and 1114; 16 heads of 64, cap and 32 buckets 385 and 331.
@@ -557,9 +557,9 @@ __device__ __forceinline__ void from_top(f32x16 (&s)[2], float top, float &again
     against = 0.f;
 }
 
-// Waves to a SIMD that the registers of the forms' kernels leave room for, forward and dQ.  Heads of 33 to 64: three without a spilled register; dQ of
-// 32 buckets, 8 x 1024 in both directions, 12 heads of 64, 84 us with two and 68 with three (768 workgroups are one round then); four would spill in the forward
-// pass (4093 tokens in 7, 16 heads, both passes 109 us with three there, 113 with four).
+// Waves to a SIMD that the registers of the forms' kernels leave room for, forward and dQ.  Heads of 33 to 64: three, without a spilled register but in dQ of a
+// cap with a table (2 of 168); dQ of 32 buckets, 8 x 1024 in both directions, 12 heads of 64, 84 us with two and 68 with three (768 workgroups are one
+// round then); four would spill in the forward pass (4093 tokens in 7, 16 heads, both passes 109 us with three there, 113 with four).
 enum { kForward, kDq, kDkv };
 constexpr int waves_of(int ks, int form) { return form == kPlain || form == kAll || ks > 4 ? 2 : ks == 2 && !has_table(form) ? 4 : 3; }
 struct NoForm {};
@@ -1120,6 +1120,8 @@ __device__ const float infinite_lse[1] = {INFINITY};         // a probability of
 // they are read for every block.
 // So do the rows of K where the scores are of another form, which takes registers of its own: 8192 tokens in 4, 32 heads of 128 on 8, both passes, us, with K in
 // registers / in LDS: slopes 753 / 734, capped 860 / 827, 32 buckets 909 / 799, capped with slopes 1114 (in part spilled) / 828.
+// What still spills: a cap with a table 1 or 2 registers of heads of 65 to 80, 10 (6 where two waves share) of 81 to 96, 2 of more; a cap with slopes 1, all
+// three 2 and 6 of 81 to 96; dQ of all three 6 of heads above 96.
 template <int KS, int SIDES, int FORM>
 __global__ void __launch_bounds__(SIDES * kAttnThreads, 2) attention_dkv_kernel(const AttnArgs A)
 {

@@ -415,6 +415,10 @@ __global__ void __launch_bounds__(kJoinThreads) norm_join_kernel(const NormArgs 
 // Backward: 8 waves a compute unit, of narrow rows 4 workgroups, at least two rows each: what covers the loads' latency with a row under way, and few enough
 // to leave few rows of sums.  Both passes, rms before and after with a gate, us, at 4 / 8 / 12 waves a compute unit and more: 8192 x 4096 - / 125 / 125, 130 at 16;
 // 2048 x 2560 on fp32 - / 34 / 40; 8192 x 2048 (layer, biases) - / 74 / 76, 89 at 24; 8192 x 512 27 / 30 / 35; 1003 x 1024 (layer) one row each 22, two 19.
+// Wider rows: the backward kernel's sums and vectors do not fit its registers.  It spills 20 registers of rows of 4104 to 8192 on an fp32 stream with norms on
+// both sides and biases; above 8192 with norms on both sides 16 and 24 (fp16, fp32), with biases 53 and 73, behind a plain block 0 and 11, 31 and 60.
+// TB/s, forward and backward with the vectors' sums, rms / layer with biases: 8192 x 5120 fp16 5.2 and 4.9 / 3.4 and 4.8, fp32 5.2 and 5.2 / 4.2 and 3.3;
+// 8192 x 8192 5.5 and 4.8 / 4.3 and 4.6, 5.4 and 5.2 / 5.2 and 3.7; 4096 x 16384 4.5 and 3.2 / 3.8 and 1.7, 5.3 and 3.5 / 4.5 and 2.1.
 // Forward: 16 waves; of rows of 7 and 8 waves and 8 elements 4 workgroups: 8192 x 4096 125 us with 4, 131 with 2; 2048 x 8192 74 and 70; 8192 x 2560 86 with 6, 83 with 3.
 struct NormShape {
     int v, threads, grid;
