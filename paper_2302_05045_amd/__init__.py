@@ -1173,7 +1173,7 @@ class Scores(NamedTuple):
     """The form of attention's scores where they are not plain products (samo_attention_scores):
     z = cap tanh(scale q k / cap) - slopes[head] |d| + table[head, column(d)], d the distance i - j counted from the sequence's end.
 
-    cap: 0 for none.  slopes: float32 (heads).  table: float16 (heads, buckets), with two_sided (heads, 2 * buckets), the second half for keys that lie
+    cap: 0 for none.  slopes: float32 (heads), up to 2^30.  table: float16 (heads, buckets), with two_sided (heads, 2 * buckets), the second half for keys that lie
     behind the query; borders: int32 (buckets - 1), the distances at which the next bucket begins (samo_bucket_borders; None for one bucket).
     first_keys: int32 (sequences), causal only: so many keys at a sequence's begin are seen by all of its queries."""
     cap: float = 0.0
