@@ -545,16 +545,17 @@ struct Form {
 };
 constexpr int kBiasRoom = 96;                // floats of a wave's biases
 
-// Scores of rows whose largest is far from zero as differences from it, and what is to be taken off them then.
+// Scores of rows whose largest is far from zero as differences from it, and what is to be taken off them then.  Other rows of the wave stay as they are.
 __device__ __forceinline__ void from_top(f32x16 (&s)[2], float top, float &against)
 {
-    if (!__ballot(fabsf(against) > kFarScore)) return;
-    top = top == -INFINITY ? 0.f : top;
+    const bool far = fabsf(against) > kFarScore;
+    if (!__ballot(far)) return;
+    top = far ? top : 0.f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[kb][i] -= top;
-    against = 0.f;
+    against = far ? 0.f : against;
 }
 
 // Waves to a SIMD that the registers of the forms' kernels leave room for, forward and dQ.  Heads of 33 to 64: three, without a spilled register but in dQ of a
