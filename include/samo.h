@@ -452,7 +452,8 @@ samo_status samo_state8_unpack_batched(const samo_plan8 *plan, void *stream);
  * the last `window` of those.  A query that sees no key has out = 0, lse = -infinity and no gradient.  scale > 0.
  * dim is a multiple of 8 up to 128; lengths from 0, q_tokens and k_tokens up to 2^30 - 128.  P = exp(S - lse) and dS = P (dP - delta) are rounded to
  * fp16 where they enter a product (as the tensors themselves are), sums and softmax are fp32; the order of the sums is fixed.  delta, the row's sum of
- * dout out, is fp32 of the rounded out.  dS is rounded before scale is applied: from 65504 on it is infinite, as a gradient in fp16 is, and what
+ * dout out, is fp32 of the rounded out.  Scores are fp32: a row whose largest is beyond 2^20 in size keeps few bits of P,
+ * and one beyond 2^27 need not have a finite one.  dS is rounded before scale is applied: from 65504 on it is infinite, as a gradient in fp16 is, and what
  * is formed from it not finite (a smaller loss scale is due), though scale times it might have fitted.
  * Masked scores are replaced, and products are formed by blocks of 32 queries and 64 keys (the gradients': 32), counted from a sequence's first token;
  * a pair of blocks that the mask hides entirely is left out.  So a key or value that is not finite changes no lse of a query that does not see it, but
